@@ -404,6 +404,105 @@ int tlf_gs_expand(const float* d_y, const int32_t* d_slot, int32_t rows, int32_t
 int tlf_ste(const int32_t* d_depth, const float* d_score, const float* d_grad_value, int32_t n, float* d_value,
             float* d_grad_score, void* d_stream);
 
+/* ---------------------------------------------------------------------------
+ * Training operators of the block's FFN half: RMSNorm, the gated FFN and their
+ * gradients (Appendix A; SwiGLU as in tlf_layer_weights), and AdamW.
+ *
+ * As above: no context, caller-owned device buffers of the current device,
+ * work enqueued on `stream` without waiting, TLF_E_INVALID_ARG or
+ * TLF_E_UNSUPPORTED before anything is enqueued, TLF_E_HIP for a failed
+ * launch.  Nothing is allocated, so every call may be captured into a graph.
+ * Tensors are row-major and contiguous, 16-byte aligned unless said otherwise;
+ * outputs overlap nothing else.  Gradients overwrite their buffers.  Results
+ * are the same to the bit from call to call.
+ * ------------------------------------------------------------------------- */
+
+/* RMSNorm of rows, with the AdaLN scale of each row's group (Section 3.1):
+ *   r = 1 / sqrt(mean(x^2) + eps),  y = x r (1 + gamma[group])
+ *   d_x      [rows][d], TLF_DTYPE_F32 or TLF_DTYPE_BF16 (x_dtype);
+ *   d_gamma  [groups][d] float32, or NULL with groups = 0: y = x r;
+ *   d_group  [rows] int32, the row's gamma (a depth's modulation, say); a row
+ *            whose group lies outside [0, groups) takes none.  May be NULL when
+ *            groups <= 1: every row takes gamma 0;
+ *   d_y      [rows][d] (y_dtype);
+ *   d_rstd   [rows] float32, receives r (tlf_rms_norm_grad reads it), or NULL;
+ *            4-byte aligned, as d_group.
+ * d a multiple of 4, at most TLF_NORM_MAX_D; groups at most TLF_NORM_MAX_GROUPS. */
+#define TLF_NORM_MAX_D 4096
+#define TLF_NORM_MAX_GROUPS 16
+int tlf_rms_norm(const void* d_x, int32_t x_dtype, const float* d_gamma, const int32_t* d_group, int32_t groups,
+                 int32_t rows, int32_t d, float eps, void* d_y, int32_t y_dtype, float* d_rstd, void* stream);
+
+/* Gradients of tlf_rms_norm for the same x, gamma and group and the r it wrote:
+ *   h = dy (1 + gamma[group]),  dx = r (h - x r^2 mean(h x)),
+ *   dgamma[k] = sum over the rows of group k of dy x r
+ *   d_dy [rows][d] in y's dtype; d_dx [rows][d] in x's dtype or NULL;
+ *   d_dgamma [groups][d] float32 or NULL (zeros for a group without rows).
+ *   d_workspace: tlf_rms_norm_grad_ws_bytes bytes, used during the call only;
+ *   may be NULL when d_dgamma is. */
+int tlf_rms_norm_grad_ws_bytes(int32_t groups, int32_t rows, int32_t d, size_t* ws_bytes);
+int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_t x_dtype, const float* d_gamma,
+                      const int32_t* d_group, int32_t groups, const float* d_rstd, int32_t rows, int32_t d, void* d_dx,
+                      float* d_dgamma, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Gated FFN (Appendix A with SwiGLU): y = a W_down^T with a = silu(g) u and
+ * g | u = x [W_gate | W_up]^T.
+ *   dtype         of x, the weights and every output; products are summed in
+ *                 float32, and g, u, a and the results are rounded to dtype;
+ *   d_x           [rows][d];
+ *   d_w_gate_up   [2f][d]: rows gate | up (as tlf_layer_weights);
+ *   d_w_down      [d][f];
+ *   d_gu          [rows][2f], receives g | u, or NULL if no gradient follows;
+ *   d_a           [rows][f], receives a (read by the second product);
+ *   d_y           [rows][d].
+ * d and f multiples of 64, at most TLF_FFN_MAX_WIDTH. */
+#define TLF_FFN_MAX_WIDTH 16384
+int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
+            int32_t f, void* d_gu, void* d_a, void* d_y, void* stream);
+
+/* Gradients of tlf_ffn from the g | u and a that it wrote:
+ *   da = dy W_down,  dg = da u s (1 + g (1 - s)),  du = da g s,  s = 1 / (1 + exp(-g)),
+ *   dx = [dg | du] W_gate_up,  dW_gate_up = [dg | du]^T x,  dW_down = dy^T a
+ *   d_dy [rows][d]; d_dx [rows][d], d_dw_gate_up [2f][d], d_dw_down [d][f], any
+ *   of them NULL (its products are then not computed).  rows = 0: the weights'
+ *   gradients are zeros.
+ *   d_workspace: tlf_ffn_grad_ws_bytes bytes, used during the call only. */
+int tlf_ffn_grad_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes);
+int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, const void* d_w_down, const void* d_gu,
+                 const void* d_a, int32_t dtype, int32_t rows, int32_t d, int32_t f, void* d_dx, void* d_dw_gate_up,
+                 void* d_dw_down, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* One tensor of an AdamW step.  The float arrays need the alignment of their
+ * elements only (whole tensors aligned to 16 bytes move in 16-byte vectors). */
+#define TLF_ADAMW_BLOCK 256
+typedef struct tlf_adamw_tensor {
+  float* d_param;       /* [n], updated */
+  void* d_copy;         /* [n] bf16, receives the updated parameter rounded, or NULL */
+  const void* d_grad;   /* [n] of grad_dtype */
+  void* d_m;            /* [n] first moment: float32, or e4m3 (OCP, finite) codes */
+  void* d_v;            /* [n] second moment: float32, or e5m2 codes */
+  float* d_m_scale;     /* 8 bits: [ceil(n / TLF_ADAMW_BLOCK)]; element e stands for code e times scale e / BLOCK */
+  float* d_v_scale;     /* likewise */
+  int64_t n;
+  int64_t step;         /* t >= 1: how many steps this tensor has had, this one included */
+  double weight_decay;
+  int32_t grad_dtype;   /* TLF_DTYPE_F32 or TLF_DTYPE_BF16 */
+  int32_t state_bits;   /* 32 or 8 */
+} tlf_adamw_tensor;
+
+/* One AdamW step of `count` tensors (Appendix A's recipe), few launches for all:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * Moments of zeros (codes and scales too) are a fresh state.  With 8 bits the
+ * step uses the new moments before they are rounded; a block's scale is its
+ * largest |m| / 448 or v / 57344, and a v > 0 keeps at least the smallest code
+ * above zero.  A gradient that is not finite spoils the moments of its element
+ * (8 bits: of its block).
+ *   h_tensors: host array, read during the call; no tensor appears twice.
+ * The step counts and rates are values of the call: a captured call replays them. */
+int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
+              void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -147,6 +147,22 @@ __device__ __forceinline__ void split4(float4 v, uint2& hi, uint2& lo) {
   lo = make_uint2(pack_bf16x2(v.x - hx, v.y - hy), pack_bf16x2(v.z - hz, v.w - hw));
 }
 
+// Four consecutive elements as float32.
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+template <typename T> struct Vec4;
+template <> struct Vec4<float> {
+  static __device__ __forceinline__ f32x4 load(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
+  static __device__ __forceinline__ void store(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+};
+template <> struct Vec4<bf16> {
+  static __device__ __forceinline__ f32x4 load(const bf16* p) {
+    return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(p), f32x4);
+  }
+  static __device__ __forceinline__ void store(bf16* p, f32x4 v) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  }
+};
+
 // Eight consecutive float32 values as the hi and lo fragments of a bf16 MFMA operand.
 __device__ __forceinline__ void split_frag(const float* p, bf16x8& hi, bf16x8& lo) {
   uint2 h0, l0, h1, l1;

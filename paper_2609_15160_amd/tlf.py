@@ -94,13 +94,30 @@ class CacheStats(ctypes.Structure):
 
 EXPORTS = ("tlf_init", "tlf_prefill", "tlf_decode_step", "tlf_cache_stats", "tlf_set_profiling", "tlf_destroy",
            "tlf_status_str", "tlf_gs_plan", "tlf_gs_plan_ws", "tlf_gs_plan_noalloc", "tlf_gs_gather",
-           "tlf_gs_scatter", "tlf_gs_expand", "tlf_ste", "tlf_probe_read")
+           "tlf_gs_scatter", "tlf_gs_expand", "tlf_ste", "tlf_probe_read", "tlf_rms_norm",
+           "tlf_rms_norm_grad_ws_bytes", "tlf_rms_norm_grad", "tlf_ffn", "tlf_ffn_grad_ws_bytes", "tlf_ffn_grad",
+           "tlf_adamw")
 
 PROBE_READ_GRAIN = 32768
 
 GS_PLAN_CHUNK_ROWS = 2048
 GS_PLAN_MAX_ROWS = 8388608
 GS_PLAN_NOALLOC_MAX_ROWS = 8388608
+
+
+NORM_MAX_D = 4096
+NORM_MAX_GROUPS = 16
+FFN_MAX_WIDTH = 16384
+ADAMW_BLOCK = 256
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [
+        ("d_param", ctypes.c_void_p), ("d_copy", ctypes.c_void_p), ("d_grad", ctypes.c_void_p),
+        ("d_m", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_m_scale", ctypes.c_void_p),
+        ("d_v_scale", ctypes.c_void_p), ("n", ctypes.c_int64), ("step", ctypes.c_int64),
+        ("weight_decay", ctypes.c_double), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+    ]
 
 
 def gs_plan_ws_bytes(rows: int) -> int:
@@ -163,6 +180,17 @@ def load(path: str = LIB_PATH):
     lib.tlf_gs_expand.restype = ctypes.c_int
     lib.tlf_ste.argtypes = [vp, vp, vp, i32, vp, vp, vp]
     lib.tlf_ste.restype = ctypes.c_int
+    sz, psz, f64 = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t), ctypes.c_double
+    lib.tlf_rms_norm.argtypes = [vp, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp, i32, vp, vp]
+    lib.tlf_rms_norm_grad_ws_bytes.argtypes = [i32, i32, i32, psz]
+    lib.tlf_rms_norm_grad.argtypes = [vp, i32, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.tlf_ffn.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.tlf_ffn_grad_ws_bytes.argtypes = [i32, i32, i32, i32, psz]
+    lib.tlf_ffn_grad.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.tlf_adamw.argtypes = [ctypes.POINTER(AdamwTensor), i32, f64, f64, f64, f64, vp]
+    for fn in (lib.tlf_rms_norm, lib.tlf_rms_norm_grad_ws_bytes, lib.tlf_rms_norm_grad, lib.tlf_ffn,
+               lib.tlf_ffn_grad_ws_bytes, lib.tlf_ffn_grad, lib.tlf_adamw):
+        fn.restype = ctypes.c_int
     _lib = lib
     return lib
 

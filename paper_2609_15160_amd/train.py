@@ -203,3 +203,279 @@ def ste(score: torch.Tensor, depth: torch.Tensor) -> torch.Tensor:
     if score.dtype != torch.float32 or depth.dtype != torch.int32 or score.shape != depth.shape:
         raise ValueError("ste: float32 score and int32 depth of one shape expected")
     return _Ste.apply(score.contiguous(), depth.contiguous())
+
+
+# ---------------------------------------------------------------------------
+# The block's FFN half: RMSNorm, the gated FFN, and the optimizer's step
+# ---------------------------------------------------------------------------
+
+_DTYPE = {torch.float32: tlf.DTYPE_F32, torch.bfloat16: tlf.DTYPE_BF16}
+
+
+def _on(t: torch.Tensor):
+    """The tensor's device made current for a call (its current stream is then the one that _stream gives)."""
+    return torch.cuda.device(t.device)
+
+
+def _same_device(t, *others):
+    for o in others:
+        if o is not None and o.device != t.device:
+            raise ValueError(f"tensors on {t.device} and {o.device}: one device expected")
+
+
+def _wants_grad(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _workspace(fn, *args, device):
+    need = ctypes.c_size_t()
+    _check(fn(*args, ctypes.byref(need)), fn.__name__)
+    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gamma, group, eps, dtype, grad):
+        rows, d = x.shape
+        groups = 0 if gamma is None else gamma.numel() // d
+        y = torch.empty((rows, d), dtype=dtype, device=x.device)
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if grad else None
+        with _on(x):
+            _check(tlf.load().tlf_rms_norm(_ptr(x), _DTYPE[x.dtype], _ptr(gamma), _ptr(group), groups, rows, d, eps,
+                                           _ptr(y), _DTYPE[dtype], _ptr(rstd), _stream()), "tlf_rms_norm")
+        if grad:
+            ctx.save_for_backward(x, gamma, group, rstd)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, gamma, group, rstd = ctx.saved_tensors
+        rows, d = x.shape
+        groups = 0 if gamma is None else gamma.numel() // d
+        dy = _aligned(dy)
+        dx = torch.empty_like(x) if ctx.needs_input_grad[0] else None
+        dgamma = torch.empty_like(gamma) if ctx.needs_input_grad[1] else None
+        lib = tlf.load()
+        ws, n = None, 0
+        if dgamma is not None:
+            ws, n = _workspace(lib.tlf_rms_norm_grad_ws_bytes, groups, rows, d, device=x.device)
+        with _on(x):
+            _check(lib.tlf_rms_norm_grad(_ptr(dy), _DTYPE[dy.dtype], _ptr(x), _DTYPE[x.dtype], _ptr(gamma),
+                                         _ptr(group), groups, _ptr(rstd), rows, d, _ptr(dx), _ptr(dgamma), _ptr(ws),
+                                         n, _stream()), "tlf_rms_norm_grad")
+        return dx, dgamma, None, None, None, None
+
+
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    """`t` contiguous and from a 16-byte boundary, copied where it is not."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+def rms_norm(x: torch.Tensor, gamma: torch.Tensor = None, group: torch.Tensor = None, eps: float = 1e-5,
+             dtype: torch.dtype = None) -> torch.Tensor:
+    """RMSNorm of the rows of x ([rows, d], float32 or bfloat16) times 1 + gamma, with gradients to x and gamma.
+
+    gamma is None, one [d] or [1, d] scale, or [groups, d] scales of which row r takes number group[r] (int32 [rows];
+    a row whose number is none of them takes no scale): the AdaLN modulation of each token's depth.  The result has
+    `dtype` (x's by default)."""
+    if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
+        raise ValueError("rms_norm: expected a float32 or bfloat16 [rows, d] CUDA tensor")
+    dtype = dtype or x.dtype
+    if dtype not in _DTYPE:
+        raise ValueError(f"rms_norm: dtype {dtype}, expected float32 or bfloat16")
+    d = x.shape[1]
+    if gamma is not None:
+        if gamma.dtype != torch.float32 or gamma.dim() not in (1, 2) or gamma.shape[-1] != d:
+            raise ValueError(f"rms_norm: gamma {tuple(gamma.shape)} {gamma.dtype}, expected float32 [d] or [groups, d]")
+        if group is None and gamma.numel() != d:
+            raise ValueError("rms_norm: several scales need each row's group")
+    if group is not None:
+        if gamma is None or group.dtype != torch.int32 or group.shape != (x.shape[0],):
+            raise ValueError("rms_norm: group is int32 [rows] and goes with gamma")
+        group = group.contiguous()
+    _same_device(x, gamma, group)
+    return _RmsNorm.apply(_aligned(x), None if gamma is None else _aligned(gamma), group, float(eps), dtype,
+                          _wants_grad(x, gamma))
+
+
+class _Ffn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate_up, w_down, grad):
+        rows, d = x.shape
+        f = w_down.shape[1]
+        new = lambda *s: torch.empty(s, dtype=x.dtype, device=x.device)  # noqa: E731
+        gu = new(rows, 2 * f) if grad else None
+        a, y = new(rows, f), new(rows, d)
+        with _on(x):
+            _check(tlf.load().tlf_ffn(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _DTYPE[x.dtype], rows, d, f, _ptr(gu),
+                                      _ptr(a), _ptr(y), _stream()), "tlf_ffn")
+        if grad:
+            ctx.save_for_backward(x, w_gate_up, w_down, gu, a)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, w_gate_up, w_down, gu, a = ctx.saved_tensors
+        rows, d = x.shape
+        f = w_down.shape[1]
+        dy = _aligned(dy)
+        outs = [torch.empty_like(t) if need else None
+                for t, need in zip((x, w_gate_up, w_down), ctx.needs_input_grad)]
+        lib = tlf.load()
+        ws, n = _workspace(lib.tlf_ffn_grad_ws_bytes, _DTYPE[x.dtype], rows, d, f, device=x.device)
+        with _on(x):
+            _check(lib.tlf_ffn_grad(_ptr(dy), _ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(gu), _ptr(a),
+                                    _DTYPE[x.dtype], rows, d, f, *[_ptr(o) for o in outs], _ptr(ws), n, _stream()),
+                   "tlf_ffn_grad")
+        return (*outs, None)
+
+
+def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch.Tensor:
+    """The block's gated FFN, W_down (silu(W_gate x) * (W_up x)) of the rows of x ([rows, d]), with gradients.
+
+    w_gate_up is [2f, d] (rows gate | up), w_down [d, f]; all three float32 or all bfloat16, d and f multiples of 64."""
+    if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
+        raise ValueError("ffn: expected a float32 or bfloat16 [rows, d] CUDA tensor")
+    d, f = x.shape[1], w_down.shape[-1]
+    if w_gate_up.shape != (2 * f, d) or w_down.shape != (d, f):
+        raise ValueError(f"ffn: x {tuple(x.shape)}, w_gate_up {tuple(w_gate_up.shape)}, w_down {tuple(w_down.shape)}; "
+                         "expected [rows, d], [2f, d], [d, f]")
+    if w_gate_up.dtype != x.dtype or w_down.dtype != x.dtype:
+        raise ValueError("ffn: x and the weights are of one dtype")
+    _same_device(x, w_gate_up, w_down)
+    return _Ffn.apply(_aligned(x), _aligned(w_gate_up), _aligned(w_down), _wants_grad(x, w_gate_up, w_down))
+
+
+def _moment(state, like, dtype8, name):
+    """(moment tensor, scales or None) of one parameter, checked."""
+    t, s = state if isinstance(state, (tuple, list)) else (state, None)
+    if t.numel() != like.numel() or not t.is_contiguous() or t.dtype != (torch.float32 if s is None else dtype8):
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected a contiguous float32 tensor or a pair of "
+                         f"{dtype8} codes and float32 scales, of the parameter's size")
+    if s is not None and (s.dtype != torch.float32 or not s.is_contiguous() or
+                          s.numel() != -(-t.numel() // tlf.ADAMW_BLOCK)):
+        raise ValueError(f"{name}: one contiguous float32 scale per {tlf.ADAMW_BLOCK} elements expected")
+    return t, s
+
+
+def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.95), eps: float = 1e-8,
+           weight_decay=0.0, copies=None) -> None:
+    """One AdamW step over many tensors, in place (tlf_adamw; few launches for all of them).
+
+    params       contiguous float32 CUDA tensors, updated
+    grads        their gradients, contiguous float32 or bfloat16
+    exp_avgs     first moments, updated: a float32 tensor, or 8 bits as (torch.float8_e4m3fn codes, float32 scales)
+    exp_avg_sqs  second moments, updated: a float32 tensor, or (torch.float8_e5m2 codes, float32 scales)
+    step         the step's number from 1, or one number for each tensor; a value, as the rates are, so a step that is
+                 captured into a graph is refused: its replays would repeat the corrections of one step
+    weight_decay one value or one for each tensor
+    copies       bfloat16 tensors that receive the updated parameters rounded, or None
+    """
+    n = len(params)
+    steps = [step] * n if isinstance(step, int) else list(step)
+    decays = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+    copies = [None] * n if copies is None else list(copies)
+    if not n == len(grads) == len(exp_avgs) == len(exp_avg_sqs) == len(steps) == len(decays) == len(copies):
+        raise ValueError("adamw_: one gradient, pair of moments, step, decay and copy for each parameter")
+    if n == 0:
+        return
+    table = (tlf.AdamwTensor * n)()
+    dev = params[0].device
+    for k, (p, g, c) in enumerate(zip(params, grads, copies)):
+        if p.dtype != torch.float32 or not p.is_cuda or not p.is_contiguous():
+            raise ValueError("adamw_: parameters are contiguous float32 CUDA tensors")
+        if g.dtype not in _DTYPE or g.shape != p.shape or not g.is_contiguous():
+            raise ValueError(f"adamw_: gradient {tuple(g.shape)} {g.dtype} of parameter {tuple(p.shape)}: contiguous "
+                             "float32 or bfloat16 of its shape expected")
+        if c is not None and (c.dtype != torch.bfloat16 or c.shape != p.shape or not c.is_contiguous()):
+            raise ValueError("adamw_: copies are contiguous bfloat16 tensors of the parameters' shapes")
+        m, ms = _moment(exp_avgs[k], p, torch.float8_e4m3fn, "exp_avg")
+        v, vs = _moment(exp_avg_sqs[k], p, torch.float8_e5m2, "exp_avg_sq")
+        if (ms is None) != (vs is None):
+            raise ValueError("adamw_: both moments in 8 bits or both in float32")
+        for t in (p, g, c, m, v, ms, vs):
+            if t is not None and t.device != dev:
+                raise ValueError("adamw_: tensors on one device expected")
+        table[k] = tlf.AdamwTensor(p.data_ptr(), c.data_ptr() if c is not None else None, g.data_ptr(), m.data_ptr(),
+                                   v.data_ptr(), ms.data_ptr() if ms is not None else None,
+                                   vs.data_ptr() if vs is not None else None, p.numel(), steps[k], decays[k],
+                                   _DTYPE[g.dtype], 32 if ms is None else 8)
+    with torch.cuda.device(dev):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("adamw_: the step number and rates are values and cannot be captured into a graph")
+        _check(tlf.load().tlf_adamw(table, n, lr, betas[0], betas[1], eps, _stream()), "tlf_adamw")
+    # a graph that saved a parameter or copy for its backward pass has to notice the update
+    torch.autograd.graph.increment_version([*params, *(c for c in copies if c is not None)])
+
+
+class AdamW:
+    """AdamW over leaf tensors, with moments of 32 or 8 bits.
+
+    params: contiguous float32 or bfloat16 CUDA leaves.  A bfloat16 one is trained through a float32 master that the
+    optimizer holds (masters[k]); the leaf receives it rounded.  step() updates every parameter that has a gradient,
+    each with its own count of steps.  weight_decay is one value or one for each parameter.  lr may be set between
+    steps.  state_dict and load_state_dict carry the masters, moments and counts."""
+
+    def __init__(self, params, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0,
+                 state_bits: int = 32):
+        self.params = list(params)
+        self.lr, self.betas, self.eps = lr, tuple(betas), eps
+        n = len(self.params)
+        self.weight_decay = [weight_decay] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        if state_bits not in (8, 32) or len(self.weight_decay) != n:
+            raise ValueError("AdamW: state_bits 8 or 32, weight_decay one value or one for each parameter")
+        if len({id(p) for p in self.params}) != n:
+            raise ValueError("AdamW: a parameter appears twice")
+        for p in self.params:
+            if p.dtype not in _DTYPE or not p.is_cuda or not p.is_contiguous() or not p.is_leaf:
+                raise ValueError("AdamW: contiguous float32 or bfloat16 CUDA leaves expected")
+        self.state_bits = state_bits
+        self.masters = [p.detach().float() if p.dtype == torch.bfloat16 else None for p in self.params]
+        self.exp_avgs = [self._zeros(p, torch.float8_e4m3fn) for p in self.params]
+        self.exp_avg_sqs = [self._zeros(p, torch.float8_e5m2) for p in self.params]
+        self.steps = [0] * n
+
+    def _zeros(self, p, dtype8):
+        if self.state_bits == 32:
+            return torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+        return (torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(dtype8),
+                torch.zeros(-(-p.numel() // tlf.ADAMW_BLOCK), dtype=torch.float32, device=p.device))
+
+    @torch.no_grad()
+    def step(self) -> None:
+        have = [k for k, p in enumerate(self.params) if p.grad is not None]
+        by = {}
+        for k in have:
+            by.setdefault(self.params[k].device, []).append(k)
+        for at in by.values():
+            pick = lambda v: [v[k] for k in at]  # noqa: E731
+            real = [self.params[k].detach() if self.masters[k] is None else self.masters[k] for k in at]
+            copies = [None if self.masters[k] is None else self.params[k].detach() for k in at]
+            adamw_(real, [self.params[k].grad.contiguous() for k in at], pick(self.exp_avgs), pick(self.exp_avg_sqs),
+                   [self.steps[k] + 1 for k in at], self.lr, self.betas, self.eps, pick(self.weight_decay), copies)
+            for k in at:
+                self.steps[k] += 1
+
+    def zero_grad(self) -> None:
+        for p in self.params:
+            p.grad = None
+
+    def state_dict(self) -> dict:
+        return {"steps": list(self.steps), "masters": list(self.masters), "exp_avgs": list(self.exp_avgs),
+                "exp_avg_sqs": list(self.exp_avg_sqs), "state_bits": self.state_bits}
+
+    @torch.no_grad()
+    def load_state_dict(self, state: dict) -> None:
+        if state["state_bits"] != self.state_bits or len(state["steps"]) != len(self.params):
+            raise ValueError("AdamW: the state is of other parameters or another state_bits")
+        self.steps = list(state["steps"])
+        flat = lambda v: [t for s in v for t in (s if isinstance(s, tuple) else (s,)) if t is not None]  # noqa: E731
+        for key in ("masters", "exp_avgs", "exp_avg_sqs"):
+            mine, given = flat(getattr(self, key)), flat(state[key])
+            if [(t.shape, t.dtype) for t in mine] != [(t.shape, t.dtype) for t in given]:
+                raise ValueError(f"AdamW: {key} do not fit the parameters")
+            for t, s in zip(mine, given):
+                t.copy_(s)
