@@ -448,27 +448,34 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
 /* Gated FFN (Appendix A with SwiGLU): y = a W_down^T with a = silu(g) u and
  * g | u = x [W_gate | W_up]^T.
  *   dtype         of x, the weights and every output; products are summed in
- *                 float32, and g, u, a and the results are rounded to dtype;
+ *                 float32, and a and the results are rounded to dtype;
  *   d_x           [rows][d];
  *   d_w_gate_up   [2f][d]: rows gate | up (as tlf_layer_weights);
  *   d_w_down      [d][f];
- *   d_gu          [rows][2f], receives g | u, or NULL if no gradient follows;
+ *   d_kept        tlf_ffn_kept_bytes bytes, receives what tlf_ffn_grad needs of g
+ *                 and u (u silu'(g) and silu(g), in an order of its own; bf16: in 16
+ *                 bits with 9 bits of mantissa and magnitudes up to 2^32), or NULL if
+ *                 no gradient follows;
  *   d_a           [rows][f], receives a (read by the second product);
  *   d_y           [rows][d].
  * d and f multiples of 64, at most TLF_FFN_MAX_WIDTH. */
 #define TLF_FFN_MAX_WIDTH 16384
+static inline size_t tlf_ffn_kept_bytes(int32_t dtype, int32_t rows, int32_t f) {
+  return rows <= 0 || f <= 0 ? 0
+                             : ((size_t)rows + 15) / 16 * 16 * 2u * (size_t)f * (dtype == TLF_DTYPE_BF16 ? 2u : 4u);
+}
 int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
-            int32_t f, void* d_gu, void* d_a, void* d_y, void* stream);
+            int32_t f, void* d_kept, void* d_a, void* d_y, void* stream);
 
-/* Gradients of tlf_ffn from the g | u and a that it wrote:
- *   da = dy W_down,  dg = da u s (1 + g (1 - s)),  du = da g s,  s = 1 / (1 + exp(-g)),
+/* Gradients of tlf_ffn from the `kept` and a that it wrote:
+ *   da = dy W_down,  dg = da u silu'(g),  du = da silu(g) (rounded to dtype),
  *   dx = [dg | du] W_gate_up,  dW_gate_up = [dg | du]^T x,  dW_down = dy^T a
  *   d_dy [rows][d]; d_dx [rows][d], d_dw_gate_up [2f][d], d_dw_down [d][f], any
  *   of them NULL (its products are then not computed).  rows = 0: the weights'
  *   gradients are zeros.
  *   d_workspace: tlf_ffn_grad_ws_bytes bytes, used during the call only. */
 int tlf_ffn_grad_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes);
-int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, const void* d_w_down, const void* d_gu,
+int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, const void* d_w_down, const void* d_kept,
                  const void* d_a, int32_t dtype, int32_t rows, int32_t d, int32_t f, void* d_dx, void* d_dw_gate_up,
                  void* d_dw_down, void* d_workspace, size_t ws_bytes, void* stream);
 

@@ -2,8 +2,12 @@
 // tlf_ffn and tlf_ffn_grad and their kernels:
 //
 //   g | u = x [W_gate | W_up]^T,  a = silu(g) u,  y = a W_down^T
-//   da = dy W_down,  dg = da u s (1 + g (1 - s)),  du = da g s,  s = 1 / (1 + exp(-g))
+//   dg = da q, du = da p with da = dy W_down, p = silu(g), q = u silu'(g) = u s (1 + g (1 - s)),
+//   s = 1 / (1 + exp(-g));
 //   dx = [dg | du] [W_gate ; W_up],  d[W_gate ; W_up] = [dg | du]^T x,  dW_down = dy^T a
+//
+// The forward pass keeps q and p instead of g and u: the gradient then takes
+// two products per element and no exponential, and one rounding each.
 //
 // Both projections, the activation and the product are one kernel (a tile
 // holds the same columns of gate and up), the activation's derivative is the
@@ -12,6 +16,8 @@
 // with k or with m (n) contiguous, so no operand is transposed in memory.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "common.h"
 #include "tlf.h"
@@ -28,10 +34,12 @@ __device__ __forceinline__ unsigned lds_offset(const void* p) {
 }
 
 // 16 bytes per lane from base + off into 64 consecutive 16-byte places from LDS
-// byte `lds` (wave-uniform, in M0; a write of M0 needs one wait state before
-// the load).  Counts toward vmcnt; the compiler does not wait for it.
+// byte `lds` (wave-uniform, in M0).  Counts toward vmcnt; the compiler does not
+// wait for it.  It does not look into the text for hazards either: a scalar
+// write of M0 must be one wait state ahead of the load, and a vector write of
+// the scalar base (a spilled one comes back by v_readlane) five.
 __device__ __forceinline__ void stage16(const void* base, unsigned off, unsigned lds) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
 }
 
 // At most N of this wave's vector-memory operations outstanding and its LDS
@@ -40,73 +48,135 @@ template <int N> __device__ __forceinline__ void wait_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// This wave's LDS operations done, then the barrier.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 enum Epi {
   E_STORE = 0,   // out[m][n] = C
-  E_SWIGLU = 1,  // columns are gate and up: out[m][f] = silu(g) u, gu[m][f], gu[m][F + f] = g, u
-  E_DSWIGLU = 2, // C = da: dgu[m][f], dgu[m][F + f] from it and the stored g, u
-  E_PART = 3     // float32 partial sums of one K range: part[range][m][n]
+  E_SWIGLU = 1,  // columns are gate and up: out[m][f] = silu(g) u; kept: q, p
+  E_DSWIGLU = 2  // C = da: out[m][f], out[m][F + f] = da q, da p
 };
 
 struct FArgs {
   const void* A;  // k contiguous: [M][lda]; m contiguous: [K][lda]
   const void* B;  // k contiguous: [N][ldb]; n contiguous: [K][ldb]
   int64_t lda, ldb, ldo;
-  int M, N, K;        // E_SWIGLU: N = F
-  void* out;          // E_STORE, E_SWIGLU
-  void* gu;           // E_SWIGLU: written unless NULL; E_DSWIGLU: dgu, written
-  const void* gu_in;  // E_DSWIGLU
-  float* part;        // E_PART
-  int splits;         // K ranges (E_PART)
+  int M, N, K;    // E_SWIGLU: N = F
+  void* out;
+  void* kept;     // E_SWIGLU: written unless NULL; E_DSWIGLU: read
+  float* part;    // split tiles (SPLIT): their parts
 };
+
+// q and p between the passes.  float32: as they are.  bf16: 16 bits, of which 6
+// are exponent and 9 mantissa: rounded to bf16 their 2^-8 would be the larger
+// part of the gradients' error (dx and dW_gate_up 0.0030 from 64 bits relative
+// to their norm, 0.0024 with 2^-10), and what the exponent gives up are
+// magnitudes past 2^32 (kept as the largest, 4.29e9) and below 2^-39.
+// Times 2^-96 such a float's two highest exponent bits are zeros, so a code is
+// the float's sign and bits 14 to 28; exponent code 63 is NaN.
+constexpr float kKeptMax = 4290772992.f;  // (2 - 2^-9) 2^31
+__device__ __forceinline__ unsigned kept16(float v) {
+  v = v > kKeptMax ? kKeptMax : v < -kKeptMax ? -kKeptMax : v;
+  unsigned b = __float_as_uint(v * 0x1p-96f);
+  b += 0x1FFFu + ((b >> 14) & 1u);  // nearest, ties to even
+  return ((b >> 14) & 0x7FFFu) | ((b >> 16) & 0x8000u);
+}
+__device__ __forceinline__ float unkept16(unsigned c) {
+  const float v = __uint_as_float(((c & 0x8000u) << 16) | ((c & 0x7FFFu) << 14)) * 0x1p96f;
+  return fabsf(v) < 0x1p32f ? v : __uint_as_float(0x7FC00000u);
+}
+// They lie as the lanes of a 16 x 16 accumulator hold them, [row / 16][f / 16]
+// [lane][4 q, 4 p], so that a wave reads and writes whole lines (row by row it
+// moved 8 bytes per lane in 32-byte pieces).
+template <typename T> struct Kept;
+template <> struct Kept<float> {
+  static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
+    const float* s = reinterpret_cast<const float*>(base) + at * 8;
+    q = Vec4<float>::load(s);
+    p = Vec4<float>::load(s + 4);
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
+    float* s = reinterpret_cast<float*>(base) + at * 8;
+    Vec4<float>::store(s, q);
+    Vec4<float>::store(s + 4, p);
+  }
+};
+template <> struct Kept<bf16> {
+  static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
+    const uint4 c = reinterpret_cast<const uint4*>(base)[at];
+    q = f32x4{unkept16(c.x), unkept16(c.x >> 16), unkept16(c.y), unkept16(c.y >> 16)};
+    p = f32x4{unkept16(c.z), unkept16(c.z >> 16), unkept16(c.w), unkept16(c.w >> 16)};
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
+    reinterpret_cast<uint4*>(base)[at] = make_uint4(kept16(q[0]) | kept16(q[1]) << 16, kept16(q[2]) | kept16(q[3]) << 16,
+                                                    kept16(p[0]) | kept16(p[1]) << 16, kept16(p[2]) | kept16(p[3]) << 16);
+  }
+};
+
+// Two neighbouring accumulators (columns 0..15 and 16..31 of 16 rows, four
+// columns of a row per lane) to row-major memory; `row` is the address of the
+// lane's row at column 0.  bf16: lane rows 0 and 1, 2 and 3 exchange halves, so
+// that a lane has eight columns, 16 bytes, and four lanes 64.
+template <typename T> __device__ __forceinline__ void store_pair(T* row, f32x4 u, f32x4 v, int lane);
+template <> __device__ __forceinline__ void store_pair<float>(float* row, f32x4 u, f32x4 v, int lane) {
+  Vec4<float>::store(row + (lane >> 4) * 4, u);
+  Vec4<float>::store(row + 16 + (lane >> 4) * 4, v);
+}
+template <> __device__ __forceinline__ void store_pair<bf16>(bf16* row, f32x4 u, f32x4 v, int lane) {
+  const auto a = __builtin_amdgcn_permlane16_swap(pack_bf16x2(u[0], u[1]), pack_bf16x2(v[0], v[1]), false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap(pack_bf16x2(u[2], u[3]), pack_bf16x2(v[2], v[3]), false, false);
+  const int g = lane >> 4;
+  *reinterpret_cast<uint4*>(row + (g & 1) * 16 + (g >> 1) * 8) = make_uint4(a[0], b[0], a[1], b[1]);
+}
 
 // 1 / (1 + exp(-g)); the float32 operators take the correctly rounded division
 template <typename T> __device__ __forceinline__ float sigmoid(float g);
 template <> __device__ __forceinline__ float sigmoid<bf16>(float g) { return __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 template <> __device__ __forceinline__ float sigmoid<float>(float g) { return 1.f / (1.f + expf(-g)); }
 
-// One operand of a stage: ROWS rows of m (or n) times 128 bytes of k, in
-// 16-byte chunks that the 64 lanes of a load put into consecutive places.
+// One operand of a step: ROWS rows of m (or n) times KB = 64 or 128 bytes of k,
+// in 16-byte chunks that the 64 lanes of a load put into consecutive places.
 //
-// k contiguous: LDS row = one row's 8 chunks, chunk c at place c ^ (row & 7),
-// so the rows of a fragment's 16-byte reads lie in distinct banks.
-// m contiguous: LDS row = one k with ROWS elements; pieces of 16 elements lie
-// at place c ^ key(k), so that the k of a transposed read do.
-template <typename T, bool TR, int ROWS> struct Operand {
-  static constexpr int EPC = 16 / (int)sizeof(T);  // elements of a chunk
-  static constexpr int BK = 8 * EPC;               // k of a stage
-  static constexpr int BYTES = ROWS * 128;
-  static constexpr int CPP = 16 / EPC;             // chunks of a 16-element piece
-  static constexpr int CPR = ROWS / EPC;           // TR: chunks of an LDS row
-  static __device__ __forceinline__ int key(int k) {
-    const int x = sizeof(T) == 2 ? (k & 3) | ((k >> 3) & 3) << 2 : (k >> 2) & 3;
+// k contiguous: LDS row = one row's chunks, chunk c at place c ^ key(row), so
+// that the 8 rows which a fragment's 16-byte reads take at a time lie in
+// distinct banks.
+// m contiguous: LDS row = one k with ROWS elements; the piece c of 16 elements
+// lies at place c ^ key(k), so that the k of a transposed read do.
+// (No bank conflicts counted for either.)
+template <typename T, bool TR, int ROWS, int KB> struct Operand {
+  static constexpr int EPC = 16 / (int)sizeof(T);        // elements of a chunk
+  static constexpr int BK = KB / (int)sizeof(T);         // k of a step
+  static constexpr int BYTES = ROWS * KB;
+  static constexpr int CPP = 16 / EPC;                   // chunks of a 16-element piece
+  static constexpr int CPR = TR ? ROWS / EPC : KB / 16;  // chunks of an LDS row
+  static __device__ __forceinline__ int key(int line) {
+    if constexpr (!TR) return KB == 64 ? (line >> 1) & 3 : line & 7;
+    const int x = sizeof(T) == 2 ? (line & 3) | ((line >> 3) & 3) << 2 : (line >> 2) & 3;
     return x & (ROWS / 16 - 1);
   }
-  // source of chunk q: row (m relative to the tile) or k of the stage, and the element of it
+  // source of chunk q: row (relative to the tile) or k of the step, and the element of it
   static __device__ __forceinline__ void place(int q, int& line, int& elem) {
-    if constexpr (TR) {
-      line = q / CPR;
-      const int p = q % CPR;
-      elem = ((((p / CPP) ^ key(line)) * CPP) + p % CPP) * EPC;
-    } else {
-      line = q >> 3;
-      elem = ((q & 7) ^ (line & 7)) * EPC;
-    }
+    line = q / CPR;
+    const int c = q % CPR;
+    if constexpr (TR) elem = ((((c / CPP) ^ key(line)) * CPP) + c % CPP) * EPC;
+    else elem = (c ^ key(line)) * EPC;
   }
 };
 
-// Fragment of 16 rows (m) from row r0 and one half of the stage's k.
-template <typename T, bool TR, int ROWS> struct Frag;
-template <bool TR, int ROWS> struct Frag<bf16, TR, ROWS> {
-  bf16x8 v;
-  static __device__ __forceinline__ Frag load(const char* s, int r0, int half, int lane) {
+// Fragment of 16 rows (m) from row r0 and 64 bytes of k, the h-th of the step.
+template <typename T, bool TR, int ROWS, int KB> struct Frag;
+template <bool TR, int ROWS, int KB> struct Frag<bf16, TR, ROWS, KB> {
+  bf16x8 v;  // k = 32 h + 8 (lane / 16) + 0..7
+  static __device__ __forceinline__ Frag load(const char* s, int r0, int h, int lane) {
+    using O = Operand<bf16, TR, ROWS, KB>;
     Frag f;
     const int g = lane >> 4, i = lane & 15;
     if constexpr (!TR) {
-      f.v = *reinterpret_cast<const bf16x8*>(s + (r0 + i) * 128 + (((half * 4 + g) ^ (i & 7)) << 4));
+      f.v = *reinterpret_cast<const bf16x8*>(s + (r0 + i) * KB + (((h * 4 + g) ^ O::key(i)) << 4));
     } else {
       // a group of 16 lanes reads 4 k x 16 m, lane i receives the 4 k of m = i
-      const int k = half * 32 + g * 8 + (i >> 2);
-      const char* p = s + k * (ROWS * 2) + (((r0 >> 4) ^ Operand<bf16, TR, ROWS>::key(k)) << 5) + (i & 3) * 8;
+      const int k = g * 8 + (i >> 2);
+      const char* p = s + (h * 32 + k) * (ROWS * 2) + (((r0 >> 4) ^ O::key(k)) << 5) + (i & 3) * 8;
       union { s16x4 h[2]; bf16x8 v; } u;
       u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
       u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 4 * ROWS * 2));
@@ -115,26 +185,26 @@ template <bool TR, int ROWS> struct Frag<bf16, TR, ROWS> {
     return f;
   }
 };
-template <bool TR, int ROWS> struct Frag<float, TR, ROWS> {
-  float v[4];  // k = 4 (lane / 16) + j of the half for the j-th instruction
-  static __device__ __forceinline__ Frag load(const char* s, int r0, int half, int lane) {
+template <bool TR, int ROWS, int KB> struct Frag<float, TR, ROWS, KB> {
+  float v[4];  // k = 16 h + 4 (lane / 16) + j for the j-th instruction
+  static __device__ __forceinline__ Frag load(const char* s, int r0, int h, int lane) {
+    using O = Operand<float, TR, ROWS, KB>;
     Frag f;
     const int g = lane >> 4, i = lane & 15;
     if constexpr (!TR) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(s + (r0 + i) * 128 + (((half * 4 + g) ^ (i & 7)) << 4));
+      const f32x4 x = *reinterpret_cast<const f32x4*>(s + (r0 + i) * KB + (((h * 4 + g) ^ O::key(i)) << 4));
 #pragma unroll
       for (int j = 0; j < 4; ++j) f.v[j] = x[j];
     } else {
-      const int k = half * 16 + g * 4;
-      const char* p = s + k * (ROWS * 4) + (((r0 >> 4) ^ Operand<float, TR, ROWS>::key(k)) << 6) + i * 4;
+      const char* p = s + (h * 16 + g * 4) * (ROWS * 4) + (((r0 >> 4) ^ O::key(g * 4)) << 6) + i * 4;
 #pragma unroll
       for (int j = 0; j < 4; ++j) f.v[j] = *reinterpret_cast<const float*>(p + j * ROWS * 4);
     }
     return f;
   }
 };
-template <typename T, bool TA, int RA, bool TB, int RB>
-__device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA>& a, const Frag<T, TB, RB>& b, f32x4 c) {
+template <typename T, bool TA, int RA, bool TB, int RB, int KB>
+__device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA, KB>& a, const Frag<T, TB, RB, KB>& b, f32x4 c) {
   if constexpr (sizeof(T) == 2) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
   } else {
@@ -144,8 +214,9 @@ __device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA>& a, const Frag<T, TB,
   }
 }
 
-template <int BM_, int BN_, int WM_, int WN_> struct FShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NTH = WM_ * WN_ * kWave;
+// Tile of BM x BN by WM x WN waves, KB bytes of k per step, RING steps in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int KB_, int RING_> struct FShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, RING = RING_, NTH = WM_ * WN_ * kWave;
 };
 
 // Workgroup L runs on XCD L % 8, and each XCD has its own L2: every XCD gets
@@ -155,223 +226,380 @@ __device__ __forceinline__ int xcd_run(int L, int n) {
   return x * q + min(x, r) + i;
 }
 
-template <typename T, bool TA, bool TB, int EK, typename SH>
-__global__ __launch_bounds__(SH::NTH) void k_ffn(FArgs g) {
-  constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::NTH;
-  constexpr int MT = BM / SH::WM / 16, NT = BN / SH::WN / 16;
-  using OA = Operand<T, TA, BM>;
-  using OB = Operand<T, TB, BN>;
-  using FA = Frag<T, TA, BM>;
-  using FB = Frag<T, TB, BN>;
-  constexpr int BK = OA::BK, STAGE = OA::BYTES + OB::BYTES;
-  constexpr int ACH = BM * 8 / NTH, BCH = BN * 8 / NTH;
-  static_assert(BM * 8 % NTH == 0 && BN * 8 % NTH == 0 && 2 * STAGE <= 160 * 1024, "chunks");
-  static_assert(EK != E_SWIGLU || (NT % 2 == 0 && !TB), "gate and up");
-  __shared__ __align__(16) char lds[2 * STAGE];
+// Tiles of a product, eight row tiles at a time, so that the tiles of a run share columns and rows.
+struct Tiles {
+  int tm, tn;
+  __device__ __forceinline__ void at(int t, int& row, int& col) const {
+    const int band = t / (8 * tn), bh = min(8, tm - band * 8), in = t - band * 8 * tn;
+    row = band * 8 + in % bh;
+    col = in / bh;
+  }
+};
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
-  const int wbase = __builtin_amdgcn_readfirstlane(tid & ~(kWave - 1));
-  constexpr int TN = EK == E_SWIGLU ? BN / 2 : BN;  // columns of N that a tile covers
-  const int tm = (g.M + BM - 1) / BM, tn = (g.N + TN - 1) / TN;
-  int t = xcd_run(blockIdx.x, gridDim.x), split = 0;
-  if constexpr (EK == E_PART) {
-    split = t / (tm * tn);
-    t %= tm * tn;
+// Split of a weight gradient's tiles over G workgroups: workgroup b computes
+// `whole` tiles, then the steps [first(b), first(b + 1)) of the remaining ones
+// taken one after the other, KT steps each.  A tile that falls to several
+// workgroups is left in parts, which k_ffn_join adds in order: the part that
+// begins inside its tile in place 0 of the workgroup, the other one in place 1.
+struct Split {
+  int64_t steps;  // of the remaining tiles
+  int G, KT, whole;
+  __host__ __device__ Split(int64_t tiles, int G_, int KT_) : G(G_), KT(KT_), whole((int)(tiles / G_)) {
+    steps = (tiles - (int64_t)whole * G) * KT;
   }
-  // eight row tiles at a time, so that the tiles of a run share columns and rows
-  const int band = t / (8 * tn), bh = min(8, tm - band * 8), in = t - band * 8 * tn;
-  const int m0 = (band * 8 + in % bh) * BM, n0 = (in / bh) * TN;
-  const int KT = (g.K + BK - 1) / BK;  // stages; the last one of an m-contiguous operand may be short
-  int k0 = 0, k1 = KT;
-  if constexpr (EK == E_PART) {
-    k0 = (int)((int64_t)KT * split / g.splits);
-    k1 = (int)((int64_t)KT * (split + 1) / g.splits);
+  __host__ __device__ int64_t first(int b) const { return steps * b / G; }
+  __host__ __device__ int owner(int64_t step) const {  // the workgroup of a step
+    int b = (int)(step * G / steps);
+    while (first(b + 1) <= step) ++b;
+    while (first(b) > step) --b;
+    return b;
   }
+};
 
-  // byte offsets of this thread's chunks from the stage's first element; rows
-  // and columns past the matrix read the last one (their results are not stored)
-  unsigned ao[ACH], bo[BCH];
+template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct Tile {
+  static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::NTH, KB = SH::KB, RING = SH::RING;
+  static constexpr int MT = BM / SH::WM / 16, NT = BN / SH::WN / 16;
+  using OA = Operand<T, TA, BM, KB>;
+  using OB = Operand<T, TB, BN, KB>;
+  using FA = Frag<T, TA, BM, KB>;
+  using FB = Frag<T, TB, BN, KB>;
+  static constexpr int BK = OA::BK, STEP = OA::BYTES + OB::BYTES;
+  static constexpr int ACH = OA::BYTES / 16 / NTH, BCH = OB::BYTES / 16 / NTH, LPT = ACH + BCH;
+  static constexpr int TN = EK == E_SWIGLU ? BN / 2 : BN;  // columns of N that a tile covers
+  static_assert(OA::BYTES % (16 * NTH) == 0 && OB::BYTES % (16 * NTH) == 0, "chunks");
+  static_assert(NT % 2 == 0 && (EK != E_SWIGLU || (NT % 4 == 0 && !TB)), "pairs of columns, of gate and of up");
+  static constexpr int LDS = RING * STEP;
+
+  // Steps [k0, k1) of the tile at (m0, n0); the sums go to the epilogue, or
+  // (SPLIT, part) to a part.
+  static __device__ __forceinline__ void run(const FArgs& g, int m0, int n0, int k0, int k1, float* part, char* lds) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
+    const int wbase = __builtin_amdgcn_readfirstlane(tid & ~(kWave - 1));
+
+    // byte offsets of this thread's chunks from the step's first element; rows
+    // and columns past the matrix read the last one (their results are not stored)
+    unsigned ao[ACH], bo[BCH];
 #pragma unroll
-  for (int c = 0; c < ACH; ++c) {
-    int line, e;
-    OA::place(tid + c * NTH, line, e);
-    if constexpr (TA) ao[c] = (unsigned)((line * g.lda + min(m0 + e, g.M - OA::EPC)) * sizeof(T));
-    else ao[c] = (unsigned)(((min(m0 + line, g.M - 1) - m0) * g.lda + e) * sizeof(T));
-  }
-#pragma unroll
-  for (int c = 0; c < BCH; ++c) {
-    int line, e;
-    OB::place(tid + c * NTH, line, e);
-    if constexpr (TB) {
-      bo[c] = (unsigned)((line * g.ldb + min(n0 + e, g.N - OB::EPC)) * sizeof(T));
-    } else {
-      int row = line;
-      if constexpr (EK == E_SWIGLU) row = line < TN ? min(n0 + line, g.N - 1) - n0 : g.N + min(n0 + line - TN, g.N - 1) - n0;
-      else row = min(n0 + line, g.N - 1) - n0;
-      bo[c] = (unsigned)((row * g.ldb + e) * sizeof(T));
+    for (int c = 0; c < ACH; ++c) {
+      int line, e;
+      OA::place(tid + c * NTH, line, e);
+      if constexpr (TA) ao[c] = (unsigned)((line * g.lda + min(m0 + e, g.M - OA::EPC)) * sizeof(T));
+      else ao[c] = (unsigned)(((min(m0 + line, g.M - 1) - m0) * g.lda + e) * sizeof(T));
     }
-  }
-  const char* ab = reinterpret_cast<const char*>(g.A) + (TA ? 0 : m0 * g.lda * (int64_t)sizeof(T));
-  const char* bb = reinterpret_cast<const char*>(g.B) + (TB ? 0 : n0 * g.ldb * (int64_t)sizeof(T));
-  const int64_t astep = TA ? BK * g.lda * (int64_t)sizeof(T) : 128, bstep = TB ? BK * g.ldb * (int64_t)sizeof(T) : 128;
-  const unsigned lbase = lds_offset(lds);
-
-  auto issue = [&](int kt) __attribute__((always_inline)) {
-    const unsigned s = lbase + ((kt - k0) & 1) * STAGE;
-    if ((TA || TB) && kt == KT - 1 && g.K % BK != 0) {
-      // short stage: k past the end are zeros
 #pragma unroll
-      for (int c = 0; c < ACH; ++c) {
-        int line, e;
-        OA::place(tid + c * NTH, line, e);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (kt * BK + (TA ? line : e) < g.K) v = *reinterpret_cast<const uint4*>(ab + kt * astep + ao[c]);
-        *reinterpret_cast<uint4*>(lds + ((kt - k0) & 1) * STAGE + (tid + c * NTH) * 16) = v;
+    for (int c = 0; c < BCH; ++c) {
+      int line, e;
+      OB::place(tid + c * NTH, line, e);
+      if constexpr (TB) {
+        bo[c] = (unsigned)((line * g.ldb + min(n0 + e, g.N - OB::EPC)) * sizeof(T));
+      } else {
+        int row = line;
+        if constexpr (EK == E_SWIGLU) row = line < TN ? min(n0 + line, g.N - 1) - n0 : g.N + min(n0 + line - TN, g.N - 1) - n0;
+        else row = min(n0 + line, g.N - 1) - n0;
+        bo[c] = (unsigned)((row * g.ldb + e) * sizeof(T));
       }
-#pragma unroll
-      for (int c = 0; c < BCH; ++c) {
-        int line, e;
-        OB::place(tid + c * NTH, line, e);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (kt * BK + (TB ? line : e) < g.K) v = *reinterpret_cast<const uint4*>(bb + kt * bstep + bo[c]);
-        *reinterpret_cast<uint4*>(lds + ((kt - k0) & 1) * STAGE + OA::BYTES + (tid + c * NTH) * 16) = v;
-      }
-      return;
     }
-    const char* as = ab + kt * astep;
-    const char* bs = bb + kt * bstep;
-#pragma unroll
-    for (int c = 0; c < ACH; ++c) stage16(as, ao[c], s + (c * NTH + wbase) * 16);
-#pragma unroll
-    for (int c = 0; c < BCH; ++c) stage16(bs, bo[c], s + OA::BYTES + (c * NTH + wbase) * 16);
-  };
+    const char* ab = reinterpret_cast<const char*>(g.A) + (TA ? 0 : m0 * g.lda * (int64_t)sizeof(T));
+    const char* bb = reinterpret_cast<const char*>(g.B) + (TB ? 0 : n0 * g.ldb * (int64_t)sizeof(T));
+    const int64_t astep = TA ? BK * g.lda * (int64_t)sizeof(T) : KB, bstep = TB ? BK * g.ldb * (int64_t)sizeof(T) : KB;
+    const unsigned lbase = lds_offset(lds);
 
-  f32x4 acc[MT][NT];
+    // chunks [c0, c1) of A's and B's of step kt into place `slot` of the ring
+    auto issue = [&](int kt, int slot, int c0, int c1) __attribute__((always_inline)) {
+      const char* as = ab + kt * astep;
+      const char* bs = bb + kt * bstep;
+      const unsigned s = lbase + slot * STEP;
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
+      for (int c = 0; c < LPT; ++c) {
+        if (c < c0 || c >= c1) continue;
+        if (c < ACH) stage16(as, ao[c], s + (c * NTH + wbase) * 16);
+        else stage16(bs, bo[c - ACH], s + OA::BYTES + ((c - ACH) * NTH + wbase) * 16);
+      }
+    };
+    // any step, the short last one of a sum over rows too (k past the end are zeros)
+    const int kfull = TA && TB ? min(k1, g.K / BK) : k1;
+    auto issue_any = [&](int kt, int slot) __attribute__((always_inline)) {
+      if ((TA && TB) && kt >= kfull) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int c = 0; c < LPT; ++c) {
+          const bool isa = c < ACH;
+          const int q = tid + (isa ? c : c - ACH) * NTH;
+          int line, e;
+          if (isa) OA::place(q, line, e);
+          else OB::place(q, line, e);
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (kt * BK + line < g.K)
+            v = *reinterpret_cast<const uint4*>(isa ? ab + kt * astep + ao[c] : bb + kt * bstep + bo[c - ACH]);
+          *reinterpret_cast<uint4*>(lds + slot * STEP + (isa ? 0 : OA::BYTES) + q * 16) = v;
+        }
+        // the waits below count loads: of this step there are none left
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      } else {
+        issue(kt, slot, 0, LPT);
+      }
+    };
 
-  auto bcol = [&](int j) __attribute__((always_inline)) {  // LDS row of B's fragment j
-    if constexpr (EK == E_SWIGLU)
-      return (j < NT / 2 ? 0 : TN) + wn * (TN / SH::WN) + (j % (NT / 2)) * 16;
-    else
-      return wn * (BN / SH::WN) + j * 16;
-  };
-  auto fetch = [&](FA (&a)[MT], FB (&b)[NT], int st, int half) __attribute__((always_inline)) {
-    const char* s = lds + st * STAGE;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) b[j] = FB::load(s + OA::BYTES, bcol(j), half, lane);
-#pragma unroll
-    for (int i = 0; i < MT; ++i) a[i] = FA::load(s, wm * (BM / SH::WM) + i * 16, half, lane);
-  };
-  // B is the instruction's first operand, so that a lane holds four consecutive columns of one row
-  auto multiply = [&](FA (&a)[MT], FB (&b)[NT]) __attribute__((always_inline)) {
+    f32x4 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
+      for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    auto bcol = [&](int j) __attribute__((always_inline)) {  // LDS row of B's fragment j
+      if constexpr (EK == E_SWIGLU) return (j < NT / 2 ? 0 : TN) + wn * (TN / SH::WN) + (j % (NT / 2)) * 16;
+      else return wn * (BN / SH::WN) + j * 16;
+    };
+    auto fetch = [&](FA (&a)[MT], FB (&b)[NT], int slot, int h) __attribute__((always_inline)) {
+      const char* s = lds + slot * STEP;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) b[j] = FB::load(s + OA::BYTES, bcol(j), h, lane);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i] = FA::load(s, wm * (BM / SH::WM) + i * 16, h, lane);
+    };
+    // B is the instruction's first operand, so that a lane holds four consecutive columns of one row
+    auto multiply = [&](FA (&a)[MT], FB (&b)[NT], int i) __attribute__((always_inline)) {
+#pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = mma(b[j], a[i], acc[i][j]);
-  };
+    };
 
-  // Two stages and two sets of fragments: while a half stage is multiplied, the
-  // next half's fragments are read.  The barrier in the middle ends every
-  // wave's reads of stage kt and every wave's loads of stage kt + 1; stage kt + 2
-  // then goes where kt was.
-  FA a0[MT], a1[MT];
-  FB b0[NT], b1[NT];
-  if (k0 < k1) {
-    issue(k0);
-    wait_barrier<0>();
-    if (k0 + 1 < k1) issue(k0 + 1);
-    fetch(a0, b0, 0, 0);
-    for (int kt = k0; kt < k1; ++kt) {
-      const int st = (kt - k0) & 1;
-      fetch(a1, b1, st, 1);
-      multiply(a0, b0);
-      wait_barrier<0>();
-      if (kt + 2 < k1) issue(kt + 2);
-      if (kt + 1 < k1) fetch(a0, b0, st ^ 1, 0);
-      multiply(a1, b1);
-    }
-  }
-
-  // lane: row m0 + .. + lane % 16, columns .. + 4 (lane / 16) + 0..3
-  const int rq = lane & 15, cq = (lane >> 4) * 4;
+    if (k0 < k1) {
+      if constexpr (NTH == 512) {
+        // A ring of five steps, loaded two at a time: a row's 128-byte line is then
+        // fetched by neighbouring loads.  Two waves on each SIMD take turns: while
+        // one multiplies a step, the other reads the fragments of its next one, then
+        // they change places at a barrier (waves 4 to 7 start one barrier later).
+        // When either multiplies step k, both have read k - 1, so every other step
+        // loads k + 3 and k + 4 between its products.  When the early waves have
+        // multiplied step k and the late ones have read it, everyone waits for its
+        // own loads of k + 1.
+        static_assert(KB == 64 && RING == 5 && MT == 2 * LPT, "loads between the products");
 #pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const int m = m0 + wm * (BM / SH::WM) + i * 16 + rq;
-    if (m >= g.M) continue;
-    if constexpr (EK == E_SWIGLU) {
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < k1) issue_any(k0 + k, k);
+        if (k0 + 3 < k1) wait_barrier<2 * LPT>();
+        else wait_barrier<0>();
+        auto slot_of = [](int s) __attribute__((always_inline)) { return s >= 5 ? s - 5 : s; };
+        auto turns = [&](auto late_) __attribute__((always_inline)) {
+          constexpr bool late = decltype(late_)::value;
+          FA a[MT];
+          FB b[NT];
+          if (late) wait_reads();
+          int kt = k0, s = 0;
+          for (; kt + 5 < kfull; kt += 2) {
+            fetch(a, b, s, 0);
+            if (late) wait_barrier<2 * LPT>();
+            else wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < NT / 2; ++j) {
-        const int f = n0 + wn * (TN / SH::WN) + j * 16 + cq;
-        if (f >= g.N) continue;
-        const f32x4 gt = acc[i][j], up = acc[i][j + NT / 2];
-        f32x4 h;
+            for (int i = 0; i < MT; ++i) multiply(a, b, i);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (late) wait_reads();
+            else wait_barrier<2 * LPT>();
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(a, b, slot_of(s + 1), 0);
+            if (late) wait_barrier<0>();
+            else wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+            const int s4 = slot_of(s + 4);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) h[r] = gt[r] * sigmoid<T>(gt[r]) * up[r];
-        Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + f, h);
-        if (g.gu) {
-          T* o = reinterpret_cast<T*>(g.gu) + (int64_t)m * 2 * g.N + f;
-          Vec4<T>::store(o, gt);
-          Vec4<T>::store(o + g.N, up);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int n = n0 + wn * (BN / SH::WN) + j * 16 + cq;
-        if (n >= g.N) continue;
-        if constexpr (EK == E_STORE) {
-          Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + n, acc[i][j]);
-        } else if constexpr (EK == E_PART) {
-          Vec4<float>::store(g.part + ((int64_t)split * g.M + m) * g.N + n, acc[i][j]);
-        } else {
-          const int64_t o = (int64_t)m * 2 * g.N + n;
-          const f32x4 gt = Vec4<T>::load(reinterpret_cast<const T*>(g.gu_in) + o);
-          const f32x4 up = Vec4<T>::load(reinterpret_cast<const T*>(g.gu_in) + o + g.N);
-          f32x4 dg, du;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float s = sigmoid<T>(gt[r]), da = acc[i][j][r];
-            dg[r] = da * up[r] * s * (1.f + gt[r] * (1.f - s));
-            du[r] = da * gt[r] * s;
+            for (int i = 0; i < MT; ++i) {
+              multiply(a, b, i);
+              issue(kt + 4 + (i & 1), i & 1 ? s : s4, i / 2, i / 2 + 1);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (late) wait_reads();
+            else wait_barrier<2 * LPT>();
+            __builtin_amdgcn_sched_barrier(0);
+            s = slot_of(s + 2);
           }
-          Vec4<T>::store(reinterpret_cast<T*>(g.gu) + o, dg);
-          Vec4<T>::store(reinterpret_cast<T*>(g.gu) + o + g.N, du);
+          for (; kt < k1; ++kt) {
+            fetch(a, b, s, 0);
+            if (late) wait_barrier<0>();
+            else wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (kt + 4 < k1) issue_any(kt + 4, slot_of(s + 4));
+#pragma unroll
+            for (int i = 0; i < MT; ++i) multiply(a, b, i);
+            __builtin_amdgcn_sched_barrier(0);
+            if (late) wait_reads();
+            else wait_barrier<0>();
+            __builtin_amdgcn_sched_barrier(0);
+            s = slot_of(s + 1);
+          }
+          if (!late) wait_reads();
+        };
+        if (wbase >= 256) turns(std::true_type{});
+        else turns(std::false_type{});
+      } else {
+        // Two sets of fragments: while half a step is multiplied, the next half's
+        // fragments are read.  The barrier in the middle ends every wave's reads of
+        // step kt and every wave's loads of kt + 1; kt + RING then goes where kt was.
+        static_assert(KB == 128, "two halves");
+        FA a0[MT], a1[MT];
+        FB b0[NT], b1[NT];
+#pragma unroll
+        for (int k = 0; k < RING; ++k)
+          if (k0 + k < k1) issue_any(k0 + k, k);
+        if (k0 + RING - 1 < kfull) wait_barrier<(RING - 1) * LPT>();
+        else wait_barrier<0>();
+        fetch(a0, b0, 0, 0);
+        int st = 0;
+        for (int kt = k0; kt < k1; ++kt) {
+          const int sn = st + 1 == RING ? 0 : st + 1;
+          fetch(a1, b1, st, 1);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) multiply(a0, b0, i);
+          if (RING > 2 && kt + RING - 1 < kfull) wait_barrier<(RING - 2) * LPT>();
+          else wait_barrier<0>();
+          if (kt + RING < k1) issue_any(kt + RING, st);
+          if (kt + 1 < k1) fetch(a0, b0, sn, 0);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) multiply(a1, b1, i);
+          st = sn;
+        }
+      }
+    }
+
+    // lane: row m0 + .. + lane % 16, columns .. + 4 (lane / 16) + 0..3
+    if constexpr (SPLIT) {
+      if (part) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) Vec4<float>::store(part + (((wave * MT + i) * NT + j) * kWave + lane) * 4, acc[i][j]);
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int mb = m0 + wm * (BM / SH::WM) + i * 16, m = mb + (lane & 15);
+      if (mb >= g.M) break;
+      const bool in = m < g.M;
+      if constexpr (EK == E_SWIGLU) {
+#pragma unroll
+        for (int j = 0; j < NT / 2; j += 2) {
+          const int f = n0 + wn * (TN / SH::WN) + j * 16;
+          if (f >= g.N) break;
+          f32x4 h[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const f32x4 gt = acc[i][j + x], up = acc[i][j + x + NT / 2];
+            f32x4 q, p;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float s = sigmoid<T>(gt[r]);
+              p[r] = gt[r] * s;
+              q[r] = up[r] * (s * (1.f + gt[r] * (1.f - s)));
+              h[x][r] = p[r] * up[r];
+            }
+            if (g.kept) Kept<T>::store(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (f >> 4) + x) * kWave + lane, q, p);
+          }
+          if (in) store_pair<T>(reinterpret_cast<T*>(g.out) + m * g.ldo + f, h[0], h[1], lane);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NT; j += 2) {
+          const int n = n0 + wn * (BN / SH::WN) + j * 16;
+          if (n >= g.N) break;
+          if constexpr (EK == E_STORE) {
+            if (in) store_pair<T>(reinterpret_cast<T*>(g.out) + m * g.ldo + n, acc[i][j], acc[i][j + 1], lane);
+          } else {
+            f32x4 q[2], p[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              Kept<T>::load(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (n >> 4) + x) * kWave + lane, q[x], p[x]);
+            T* o = reinterpret_cast<T*>(g.out) + m * g.ldo + n;
+            if (in) {
+              store_pair<T>(o, acc[i][j] * q[0], acc[i][j + 1] * q[1], lane);
+              store_pair<T>(o + g.N, acc[i][j] * p[0], acc[i][j + 1] * p[1], lane);
+            }
+          }
         }
       }
     }
   }
+};
+
+template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn(FArgs g) {
+  using TL = Tile<T, TA, TB, EK, SH, false>;
+  __shared__ __align__(16) char lds[TL::LDS];
+  const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + TL::TN - 1) / TL::TN};
+  int row, col;
+  ts.at(xcd_run(blockIdx.x, gridDim.x), row, col);
+  TL::run(g, row * SH::BM, col * TL::TN, 0, (g.K + TL::BK - 1) / TL::BK, nullptr, lds);
 }
 
-// The K ranges' partial sums added in order, rounded once.
-template <typename T> __global__ __launch_bounds__(256) void k_ffn_join(const float* part, int splits, int64_t n, T* out) {
-  const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (e >= n) return;
-  f32x4 v = Vec4<float>::load(part + e);
-  for (int s = 1; s < splits; ++s) v += Vec4<float>::load(part + s * n + e);
-  Vec4<T>::store(out + e, v);
+// Weight gradients: few tiles and a long sum over rows, dealt evenly to the
+// compute units (Split).
+template <typename T, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn_split(FArgs g) {
+  using TL = Tile<T, true, true, E_STORE, SH, true>;
+  __shared__ __align__(16) char lds[TL::LDS];
+  const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + SH::BN - 1) / SH::BN};
+  const Split sp((int64_t)ts.tm * ts.tn, gridDim.x, (g.K + TL::BK - 1) / TL::BK);
+  const int b = xcd_run(blockIdx.x, gridDim.x);
+  int row, col;
+  for (int w = 0; w < sp.whole; ++w) {
+    ts.at(w * sp.G + b, row, col);
+    TL::run(g, row * SH::BM, col * SH::BN, 0, sp.KT, nullptr, lds);
+    __syncthreads();
+  }
+  const int64_t end = sp.first(b + 1);
+  for (int64_t at = sp.first(b); at < end;) {
+    const int t = (int)(at / sp.KT), ka = (int)(at - (int64_t)t * sp.KT), kb = (int)min((int64_t)sp.KT, ka + (end - at));
+    ts.at(sp.whole * sp.G + t, row, col);
+    float* part = ka == 0 && kb == sp.KT ? nullptr : g.part + ((int64_t)b * 2 + (ka == 0)) * (SH::BM * SH::BN);
+    TL::run(g, row * SH::BM, col * SH::BN, ka, kb, part, lds);
+    __syncthreads();
+    at += kb - ka;
+  }
 }
+
+// The parts of the remaining tiles added in order and rounded once; a
+// workgroup per 1024 elements of a tile, in the accumulators' order.
+template <typename T, typename SH> __global__ __launch_bounds__(256) void k_ffn_join(FArgs g, int G, int KT) {
+  constexpr int MT = SH::BM / SH::WM / 16, NT = SH::BN / SH::WN / 16;
+  const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + SH::BN - 1) / SH::BN};
+  const Split sp((int64_t)ts.tm * ts.tn, G, KT);
+  const int t = blockIdx.y;
+  const int64_t s0 = (int64_t)t * KT, s1 = s0 + KT;
+  const int b0 = sp.owner(s0), b1 = sp.owner(s1 - 1);
+  if (b0 == b1) return;  // one workgroup's, stored whole
+  int row, col;
+  ts.at(sp.whole * G + t, row, col);
+  const int v = blockIdx.x * 256 + threadIdx.x, lane = v & 63, f = v >> 6;  // fragment of the tile
+  const int j = f % NT, i = f / NT % MT, wave = f / (NT * MT);
+  const int m = row * SH::BM + wave / SH::WN * (SH::BM / SH::WM) + i * 16 + (lane & 15);
+  const int n = col * SH::BN + wave % SH::WN * (SH::BN / SH::WN) + j * 16 + (lane >> 4) * 4;
+  f32x4 c = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int b = b0; b <= b1; ++b) {
+    if (sp.first(b) == sp.first(b + 1)) continue;
+    c += Vec4<float>::load(g.part + ((int64_t)b * 2 + (sp.first(b) <= s0)) * (SH::BM * SH::BN) + (int64_t)v * 4);
+  }
+  if (m < g.M && n < g.N) Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + n, c);
+}
+
+using Big = FShape<256, 256, 2, 4, 64, 5>;
+using Mid = FShape<128, 128, 2, 2, 128, 2>;
+using Small = FShape<64, 64, 4, 1, 128, 3>;
 
 template <typename T, bool TA, bool TB, int EK, typename SH> hipError_t launch_shape(const FArgs& g, hipStream_t s) {
   constexpr int TN = EK == E_SWIGLU ? SH::BN / 2 : SH::BN;
-  const int64_t tiles = (int64_t)((g.M + SH::BM - 1) / SH::BM) * ((g.N + TN - 1) / TN) * (EK == E_PART ? g.splits : 1);
+  const int64_t tiles = (int64_t)((g.M + SH::BM - 1) / SH::BM) * ((g.N + TN - 1) / TN);
   if (tiles <= 0 || tiles > INT32_MAX) return tiles == 0 ? hipSuccess : hipErrorInvalidValue;
   hipLaunchKernelGGL((k_ffn<T, TA, TB, EK, SH>), dim3((unsigned)tiles), dim3(SH::NTH), 0, s, g);
   return hipGetLastError();
 }
 
-using Big = FShape<256, 256, 2, 4>;
-using Mid = FShape<128, 128, 2, 2>;
-using Small = FShape<64, 64, 2, 2>;
-
 template <typename T, bool TA, bool TB, int EK> hipError_t launch_ffn(const FArgs& g, hipStream_t s) {
   const int64_t mid = (int64_t)((g.M + 127) / 128) * ((g.N + 127) / 128) * (EK == E_SWIGLU ? 2 : 1);
   if constexpr (sizeof(T) == 2) {
-    if (mid * (EK == E_PART ? g.splits : 1) >= 768) return launch_shape<T, TA, TB, EK, Big>(g, s);
+    if (mid >= 768) return launch_shape<T, TA, TB, EK, Big>(g, s);
   }
-  if (mid * (EK == E_PART ? g.splits : 1) >= 200) return launch_shape<T, TA, TB, EK, Mid>(g, s);
+  if (mid >= 200) return launch_shape<T, TA, TB, EK, Mid>(g, s);
   return launch_shape<T, TA, TB, EK, Small>(g, s);
 }
 
@@ -385,46 +613,30 @@ int check(int32_t dtype, int32_t rows, int32_t d, int32_t f) {
   return TLF_OK;
 }
 
-// K ranges of a weight gradient: enough workgroups for every compute unit
-// while a range still has work for its start and its partial sums.
-int grad_splits(int64_t m, int64_t n, int64_t rows) {
-  const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128);
-  const int64_t steps = rows / 512;
-  int64_t s = 512 / tiles;
-  if (s > steps) s = steps;
-  return (int)(s < 1 ? 1 : s > 32 ? 32 : s);
+constexpr int kCus = 256;  // compute units
+
+// How a weight gradient [m][n] summed over `rows` rows is computed.
+struct GradPlan {
+  int shape;  // 0 Small, 1 Mid, 2 Big
+  int G;      // workgroups that the tiles are split over, or 0
+};
+
+GradPlan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
+  auto tiles = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
+  GradPlan p{0, 0};
+  if (half && rows >= 1024) p.shape = 2;
+  else if (tiles(128) >= 200) p.shape = 1;
+  const int64_t nt = tiles(p.shape == 2 ? 256 : p.shape == 1 ? 128 : 64), KT = (rows + 31) / 32;
+  const int G = p.shape == 2 ? kCus : 2 * kCus;
+  const int64_t over = nt % G;
+  if (over != 0 && KT * (G - over) > 40 * G && nt * KT >= G) p.G = G;
+  return p;
 }
 
-template <typename T>
-int ffn_forward(const void* x, const void* wgu, const void* wd, int rows, int d, int f, void* gu, void* a, void* y,
-                hipStream_t s) {
-  FArgs p{};
-  p.A = x; p.B = wgu; p.lda = d; p.ldb = d; p.ldo = f;
-  p.M = rows; p.N = f; p.K = d; p.out = a; p.gu = gu;
-  if (launch_ffn<T, false, false, E_SWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
-  FArgs q{};
-  q.A = a; q.B = wd; q.lda = f; q.ldb = f; q.ldo = d;
-  q.M = rows; q.N = d; q.K = f; q.out = y;
-  return launch_ffn<T, false, false, E_STORE>(q, s) == hipSuccess ? TLF_OK : TLF_E_HIP;
-}
-
-template <typename T>
-hipError_t weight_grad(const void* a, int m, const void* b, int n, int rows, void* out, float* part, hipStream_t s) {
-  FArgs p{};
-  p.A = a; p.B = b; p.lda = m; p.ldb = n; p.ldo = n;
-  p.M = m; p.N = n; p.K = rows; p.out = out; p.part = part; p.splits = grad_splits(m, n, rows);
-  if (p.splits == 1) return launch_ffn<T, true, true, E_STORE>(p, s);
-  hipError_t e = launch_ffn<T, true, true, E_PART>(p, s);
-  if (e != hipSuccess) return e;
-  const int64_t all = (int64_t)m * n;
-  hipLaunchKernelGGL(k_ffn_join<T>, dim3((unsigned)((all + 1023) / 1024)), dim3(256), 0, s, part, p.splits, all,
-                     reinterpret_cast<T*>(out));
-  return hipGetLastError();
-}
-
-size_t part_bytes(int64_t m, int64_t n, int64_t rows) {
-  const int s = grad_splits(m, n, rows);
-  return s > 1 ? (size_t)(m * n * s) * sizeof(float) : 0;
+size_t part_bytes(int32_t dtype, int64_t m, int64_t n, int64_t rows) {
+  const GradPlan p = grad_plan(dtype == TLF_DTYPE_BF16, m, n, rows);
+  const size_t b = p.shape == 2 ? 256 : p.shape == 1 ? 128 : 64;
+  return (size_t)p.G * 2 * b * b * sizeof(float);
 }
 
 size_t dgu_bytes(int32_t dtype, int64_t rows, int64_t f) {
@@ -432,14 +644,50 @@ size_t dgu_bytes(int32_t dtype, int64_t rows, int64_t f) {
 }
 
 template <typename T>
-int ffn_backward(const void* dy, const void* x, const void* wgu, const void* wd, const void* gu, const void* a, int rows,
+int ffn_forward(const void* x, const void* wgu, const void* wd, int rows, int d, int f, void* kept, void* a, void* y,
+                hipStream_t s) {
+  FArgs p{};
+  p.A = x; p.B = wgu; p.lda = d; p.ldb = d; p.ldo = f;
+  p.M = rows; p.N = f; p.K = d; p.out = a; p.kept = kept;
+  if (launch_ffn<T, false, false, E_SWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
+  FArgs q{};
+  q.A = a; q.B = wd; q.lda = f; q.ldb = f; q.ldo = d;
+  q.M = rows; q.N = d; q.K = f; q.out = y;
+  return launch_ffn<T, false, false, E_STORE>(q, s) == hipSuccess ? TLF_OK : TLF_E_HIP;
+}
+
+template <typename T, typename SH> hipError_t launch_grad(const FArgs& p, int G, hipStream_t s) {
+  if (G == 0) return launch_shape<T, true, true, E_STORE, SH>(p, s);
+  const int64_t tiles = (int64_t)((p.M + SH::BM - 1) / SH::BM) * ((p.N + SH::BN - 1) / SH::BN);
+  const int KT = (p.K + SH::KB / (int)sizeof(T) - 1) / (SH::KB / (int)sizeof(T));
+  hipLaunchKernelGGL((k_ffn_split<T, SH>), dim3(G), dim3(SH::NTH), 0, s, p);
+  const int rest = (int)(tiles % G);
+  if (rest > 0)
+    hipLaunchKernelGGL((k_ffn_join<T, SH>), dim3(SH::BM * SH::BN / 1024, rest), dim3(256), 0, s, p, G, KT);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t weight_grad(const void* a, int m, const void* b, int n, int rows, void* out, float* part, hipStream_t s) {
+  FArgs p{};
+  p.A = a; p.B = b; p.lda = m; p.ldb = n; p.ldo = n;
+  p.M = m; p.N = n; p.K = rows; p.out = out; p.part = part;
+  const GradPlan plan = grad_plan(sizeof(T) == 2, m, n, rows);
+  if constexpr (sizeof(T) == 2) {
+    if (plan.shape == 2) return launch_grad<T, Big>(p, plan.G, s);
+  }
+  return plan.shape == 1 ? launch_grad<T, Mid>(p, plan.G, s) : launch_grad<T, Small>(p, plan.G, s);
+}
+
+template <typename T>
+int ffn_backward(const void* dy, const void* x, const void* wgu, const void* wd, const void* kept, const void* a, int rows,
                  int d, int f, void* dx, void* dwgu, void* dwd, char* ws, hipStream_t s) {
   void* dgu = ws;
   float* part = reinterpret_cast<float*>(ws + dgu_bytes(sizeof(T) == 2 ? TLF_DTYPE_BF16 : TLF_DTYPE_F32, rows, f));
   if (rows > 0 && (dx || dwgu)) {
     FArgs p{};
-    p.A = dy; p.B = wd; p.lda = d; p.ldb = f;
-    p.M = rows; p.N = f; p.K = d; p.gu = dgu; p.gu_in = gu;
+    p.A = dy; p.B = wd; p.lda = d; p.ldb = f; p.ldo = 2 * f;
+    p.M = rows; p.N = f; p.K = d; p.out = dgu; p.kept = const_cast<void*>(kept);
     if (launch_ffn<T, false, true, E_DSWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
   }
   if (dx) {
@@ -460,27 +708,27 @@ int ffn_backward(const void* dy, const void* x, const void* wgu, const void* wd,
 extern "C" {
 
 int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
-            int32_t f, void* d_gu, void* d_a, void* d_y, void* stream) {
+            int32_t f, void* d_kept, void* d_a, void* d_y, void* stream) {
   const int st = tlf::check(dtype, rows, d, f);
   if (st != TLF_OK) return st;
   if (rows == 0) return TLF_OK;
   if (!d_x || !d_w_gate_up || !d_w_down || !d_a || !d_y) return TLF_E_INVALID_ARG;
-  for (const void* p : {d_x, d_w_gate_up, d_w_down, (const void*)d_gu, (const void*)d_a, (const void*)d_y})
+  for (const void* p : {d_x, d_w_gate_up, d_w_down, (const void*)d_kept, (const void*)d_a, (const void*)d_y})
     if (!tlf::aligned16(p)) return TLF_E_INVALID_ARG;
   return dtype == TLF_DTYPE_BF16
-             ? tlf::ffn_forward<bf16>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_gu, d_a, d_y, (hipStream_t)stream)
-             : tlf::ffn_forward<float>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_gu, d_a, d_y, (hipStream_t)stream);
+             ? tlf::ffn_forward<bf16>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (hipStream_t)stream)
+             : tlf::ffn_forward<float>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (hipStream_t)stream);
 }
 
 int tlf_ffn_grad_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes) {
   const int st = tlf::check(dtype, rows, d, f);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  const size_t gu = tlf::part_bytes(2 * (int64_t)f, d, rows), dn = tlf::part_bytes(d, f, rows);
+  const size_t gu = tlf::part_bytes(dtype, 2 * (int64_t)f, d, rows), dn = tlf::part_bytes(dtype, d, f, rows);
   *ws_bytes = tlf::dgu_bytes(dtype, rows, f) + (gu > dn ? gu : dn);
   return TLF_OK;
 }
 
-int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, const void* d_w_down, const void* d_gu,
+int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, const void* d_w_down, const void* d_kept,
                  const void* d_a, int32_t dtype, int32_t rows, int32_t d, int32_t f, void* d_dx, void* d_dw_gate_up,
                  void* d_dw_down, void* d_workspace, size_t ws_bytes, void* stream) {
   size_t need = 0;
@@ -488,17 +736,17 @@ int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, con
   if (st != TLF_OK) return st;
   if (!d_dx && !d_dw_gate_up && !d_dw_down) return TLF_OK;
   if (rows > 0) {
-    if (!d_dy || !d_x || !d_w_gate_up || !d_w_down || !d_gu || !d_a) return TLF_E_INVALID_ARG;
+    if (!d_dy || !d_x || !d_w_gate_up || !d_w_down || !d_kept || !d_a) return TLF_E_INVALID_ARG;
     if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
   }
-  for (const void* p : {d_dy, d_x, d_w_gate_up, d_w_down, d_gu, d_a, (const void*)d_dx, (const void*)d_dw_gate_up,
+  for (const void* p : {d_dy, d_x, d_w_gate_up, d_w_down, d_kept, d_a, (const void*)d_dx, (const void*)d_dw_gate_up,
                         (const void*)d_dw_down, (const void*)d_workspace})
     if (!tlf::aligned16(p)) return TLF_E_INVALID_ARG;
   if (rows == 0) d_dx = nullptr;  // no rows; the weights' gradients are zeros
   return dtype == TLF_DTYPE_BF16
-             ? tlf::ffn_backward<bf16>(d_dy, d_x, d_w_gate_up, d_w_down, d_gu, d_a, rows, d, f, d_dx, d_dw_gate_up,
+             ? tlf::ffn_backward<bf16>(d_dy, d_x, d_w_gate_up, d_w_down, d_kept, d_a, rows, d, f, d_dx, d_dw_gate_up,
                                        d_dw_down, (char*)d_workspace, (hipStream_t)stream)
-             : tlf::ffn_backward<float>(d_dy, d_x, d_w_gate_up, d_w_down, d_gu, d_a, rows, d, f, d_dx, d_dw_gate_up,
+             : tlf::ffn_backward<float>(d_dy, d_x, d_w_gate_up, d_w_down, d_kept, d_a, rows, d, f, d_dx, d_dw_gate_up,
                                         d_dw_down, (char*)d_workspace, (hipStream_t)stream);
 }
 

@@ -111,6 +111,11 @@ FFN_MAX_WIDTH = 16384
 ADAMW_BLOCK = 256
 
 
+def ffn_kept_bytes(dtype: int, rows: int, f: int) -> int:
+    """Bytes that tlf_ffn keeps for tlf_ffn_grad (tlf_ffn_kept_bytes in tlf.h)."""
+    return (rows + 15) // 16 * 16 * 2 * f * (2 if dtype == DTYPE_BF16 else 4)
+
+
 class AdamwTensor(ctypes.Structure):
     _fields_ = [
         ("d_param", ctypes.c_void_p), ("d_copy", ctypes.c_void_p), ("d_grad", ctypes.c_void_p),

@@ -306,19 +306,21 @@ class _Ffn(torch.autograd.Function):
         rows, d = x.shape
         f = w_down.shape[1]
         new = lambda *s: torch.empty(s, dtype=x.dtype, device=x.device)  # noqa: E731
-        gu = new(rows, 2 * f) if grad else None
+        kept = None
+        if grad:
+            kept = torch.empty(tlf.ffn_kept_bytes(_DTYPE[x.dtype], rows, f), dtype=torch.uint8, device=x.device)
         a, y = new(rows, f), new(rows, d)
         with _on(x):
-            _check(tlf.load().tlf_ffn(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _DTYPE[x.dtype], rows, d, f, _ptr(gu),
+            _check(tlf.load().tlf_ffn(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _DTYPE[x.dtype], rows, d, f, _ptr(kept),
                                       _ptr(a), _ptr(y), _stream()), "tlf_ffn")
         if grad:
-            ctx.save_for_backward(x, w_gate_up, w_down, gu, a)
+            ctx.save_for_backward(x, w_gate_up, w_down, kept, a)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, w_gate_up, w_down, gu, a = ctx.saved_tensors
+        x, w_gate_up, w_down, kept, a = ctx.saved_tensors
         rows, d = x.shape
         f = w_down.shape[1]
         dy = _aligned(dy)
@@ -327,7 +329,7 @@ class _Ffn(torch.autograd.Function):
         lib = tlf.load()
         ws, n = _workspace(lib.tlf_ffn_grad_ws_bytes, _DTYPE[x.dtype], rows, d, f, device=x.device)
         with _on(x):
-            _check(lib.tlf_ffn_grad(_ptr(dy), _ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(gu), _ptr(a),
+            _check(lib.tlf_ffn_grad(_ptr(dy), _ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(kept), _ptr(a),
                                     _DTYPE[x.dtype], rows, d, f, *[_ptr(o) for o in outs], _ptr(ws), n, _stream()),
                    "tlf_ffn_grad")
         return (*outs, None)

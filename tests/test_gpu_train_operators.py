@@ -533,7 +533,8 @@ def test_operators_replayed_from_a_graph():
     gamma = torch.randn(G, d, device="cuda") * 0.1
     group = torch.randint(0, G, (n,), device="cuda", dtype=torch.int32)
     new = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device="cuda")  # noqa: E731
-    y, rstd, gu, a, z = new(n, d), new(n, dt=torch.float32), new(n, 2 * f), new(n, f), new(n, d)
+    y, rstd, a, z = new(n, d), new(n, dt=torch.float32), new(n, f), new(n, d)
+    gu = new(tlf.ffn_kept_bytes(tlf.DTYPE_BF16, n, f), dt=torch.uint8)
     dyn, dwgu, dwd, dx, dgamma = new(n, d), new(2 * f, d), new(d, f), new(n, d), new(G, d, dt=torch.float32)
     size = ctypes.c_size_t()
     assert lib.tlf_ffn_grad_ws_bytes(tlf.DTYPE_BF16, n, d, f, ctypes.byref(size)) == tlf.OK
@@ -591,7 +592,9 @@ def test_rows_behind_the_last_stay_as_they_were():
     n, d, f = 37, 192, 64
     x, wgu, wd, dy = _ffn_inputs(n, d, f, "bf16")
     room = lambda r, c, dt=torch.bfloat16: torch.full((r + 3, c), 7.0, dtype=dt, device="cuda")  # noqa: E731
-    gu, a, y, dx, dwgu, dwd, h = room(n, 2 * f), room(n, f), room(n, d), room(n, d), room(2 * f, d), room(d, f), room(n, d)
+    a, y, dx, dwgu, dwd, h = room(n, f), room(n, d), room(n, d), room(2 * f, d), room(d, f), room(n, d)
+    kept = tlf.ffn_kept_bytes(tlf.DTYPE_BF16, n, f)
+    gu = torch.full((kept + 64,), 7, dtype=torch.uint8, device="cuda")
     rstd = torch.full((n + 3,), 7.0, device="cuda")
     P = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
     s, B = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream), tlf.DTYPE_BF16
@@ -602,6 +605,6 @@ def test_rows_behind_the_last_stay_as_they_were():
     assert lib.tlf_ffn(P(x), P(wgu), P(wd), B, n, d, f, P(gu), P(a), P(y), s) == tlf.OK
     assert lib.tlf_ffn_grad(P(dy), P(x), P(wgu), P(wd), P(gu), P(a), B, n, d, f, P(dx), P(dwgu), P(dwd), P(ws),
                             size.value, s) == tlf.OK
-    for t in (gu, a, y, dx, dwgu, dwd, h):
+    for t in (a, y, dx, dwgu, dwd, h):
         assert (t[-3:] == 7.0).all() and torch.isfinite(t.float()).all()
-    assert (rstd[-3:] == 7.0).all() and (ws[size.value:] == 7).all()
+    assert (rstd[-3:] == 7.0).all() and (ws[size.value:] == 7).all() and (gu[kept:] == 7).all()
