@@ -12,8 +12,9 @@
 // m / s with s = max|m| / 448, v is e5m2 of v / s with s = max v / 57344, so
 // that each block's largest value is the format's largest; a v that is not
 // zero does not become zero (its m / sqrt(v) would grow without bound).  They
-// are computed in float64 up to that rounding: in float32 a value next to a
-// border between two codes would fall to either side.
+// are computed in float64 up to that rounding, each product and sum rounded by
+// itself: in float32 a value next to a border between two codes would fall to
+// either side, and a fused product and sum fall to another side of a tie.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -126,6 +127,11 @@ __device__ __forceinline__ float scaled(double v, double inv, float most) {
   return t > most ? most : t < -most ? -most : t;
 }
 
+__device__ __forceinline__ double moment(double b, double old, double c, double x) {
+#pragma clang fp contract(off)
+  return b * old + c * x;
+}
+
 // One wave per block of 256 elements, four per lane.
 __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
   const int k = tensor_of(a, blockIdx.x);
@@ -170,8 +176,8 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const double g = g4[r];
-      m1[r] = a.b1 * ((double)mo[r] * ms) + c1 * g;
-      v1[r] = a.b2 * ((double)vo[r] * vs) + c2 * (g * g);
+      m1[r] = moment(a.b1, (double)mo[r] * ms, c1, g);
+      v1[r] = moment(a.b2, (double)vo[r] * vs, c2, g * g);
       mm = fmaxf(mm, fabsf((float)m1[r]));
       vm = fmaxf(vm, (float)v1[r]);
       p4[r] = update(p4[r], (float)m1[r], (float)v1[r], t, a.eps);
