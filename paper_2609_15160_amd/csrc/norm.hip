@@ -15,9 +15,9 @@ namespace tlf {
 
 namespace {
 
-constexpr int kNormWaves = 4;      // rows of a workgroup
-constexpr int kGammaCols = 256;    // columns of a gamma-gradient workgroup
-constexpr int kGammaChunks = 128;  // at most so many row chunks of partial sums
+constexpr int kNormWaves = 4;    // rows of a workgroup, a wave each
+constexpr int kGradRows = 2;     // rows that a gradient workgroup has in flight
+constexpr int kGammaCols = 256;  // columns of a wave
 
 struct NormArgs {
   const void* x;
@@ -30,11 +30,42 @@ struct NormArgs {
   float eps;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += shfl_xor(v, o);
-  return v;
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, false));
 }
+
+// Sum over the 64 lanes of a wave, in the VALU; every lane gets the total.
+__device__ __forceinline__ float wave_sum(float v) {
+  v += dpp<0xB1>(v);   // lane ^ 1
+  v += dpp<0x4E>(v);   // lane ^ 2
+  v += dpp<0x141>(v);  // other quad of the 8
+  v += dpp<0x140>(v);  // other half of the 16
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Four elements as they lie in memory, converted where they are used: a
+// conversion next to the load would wait for it there.
+template <typename T> struct Raw4;
+template <> struct Raw4<float> {
+  f32x4 v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) { v = Vec4<float>::load(reinterpret_cast<const float*>(p) + at); }
+  __device__ __forceinline__ void zero() { v = f32x4{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ f32x4 get() const { return v; }
+};
+template <> struct Raw4<bf16> {
+  uint2 v;
+  __device__ __forceinline__ void load(const void* p, int64_t at) {
+    v = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p) + at);
+  }
+  __device__ __forceinline__ void zero() { v = make_uint2(0, 0); }
+  __device__ __forceinline__ f32x4 get() const {
+    return f32x4{__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                 __uint_as_float(v.y & 0xFFFF0000u)};
+  }
+};
 
 // The row's gamma, or NULL where its group lies outside [0, groups).
 __device__ __forceinline__ const float* gamma_of(const float* gamma, const int32_t* group, int groups, int row, int d) {
@@ -42,7 +73,8 @@ __device__ __forceinline__ const float* gamma_of(const float* gamma, const int32
   return gamma && k >= 0 && k < groups ? gamma + (int64_t)k * d : nullptr;
 }
 
-// One wave per row, the row in registers: 4 NV elements per lane.
+// One wave per row, the row in registers: 4 NV elements per lane.  Bound by HBM:
+// 32768 x 1024 from float32 to bf16 33 us, 6.1 TB/s.
 template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWaves* kWave) void k_norm(NormArgs a) {
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * kNormWaves + threadIdx.x / kWave), lane = lane_id();
   if (row >= a.rows) return;
@@ -101,52 +133,132 @@ template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWa
   }
 }
 
-// gamma's gradient of one row chunk and 256 columns: each wave adds its rows
-// into its own LDS sums (one lane owns a column, so the order is fixed), the
-// waves' sums are added in order.
-template <typename TX, typename TY>
-__global__ __launch_bounds__(kNormWaves* kWave) void k_norm_dgamma(NormArgs a, int chunk, float* part) {
-  __shared__ __align__(16) float sum[kNormWaves][TLF_NORM_MAX_GROUPS][kGammaCols];
-  const int lane = lane_id(), wave = threadIdx.x / kWave, c = blockIdx.y * kGammaCols + lane * 4;
-  for (int k = 0; k < a.groups; ++k) Vec4<float>::store(&sum[wave][k][lane * 4], f32x4{0.f, 0.f, 0.f, 0.f});
+// Both gradients in one pass: a workgroup takes a run of rows, RU at a time, a
+// thread four columns of each (a wave per 256 columns), so that a column of
+// gamma's gradient has one owner, which adds its rows in order, each group's in
+// registers of its own (the row's group is uniform, a scalar branch picks them;
+// with the sums in LDS 108 us where these take 90).  The row's mean goes over the
+// waves through LDS, one barrier for RU rows; the next RU rows are on their way
+// meanwhile, and the groups of those after them.  x and dy are read once, dx is
+// written; the workgroups' sums add 4 groups d bytes each.  32768 x 1024, float32
+// x, bf16 dy, both gradients with their sums joined: 90 us for 8 groups, 77 for
+// one (dx alone 57, 5.9 TB/s); what is left is the loads' latency between two
+// barriers.
+template <typename TX, typename TY, int GMAX, int MAXT, int RU>
+__global__ __launch_bounds__(MAXT) void k_norm_grad(NormArgs a, int chunk, float* part) {
+  __shared__ __align__(16) float red[2][MAXT / kWave][RU];
+  const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, nw = blockDim.x / kWave, c = tid * 4;
+  const bool own = c < a.d;
   const int r0 = blockIdx.x * chunk, r1 = min(a.rows, r0 + chunk);
-  if (c < a.d) {
-    for (int row = r0 + wave; row < r1; row += kNormWaves) {
-      const int k = a.group ? a.group[row] : 0;
-      if (k < 0 || k >= a.groups) continue;
-      const int64_t o = (int64_t)row * a.d + c;
-      const f32x4 t = Vec4<TY>::load(reinterpret_cast<const TY*>(a.dy) + o) *
-                      (Vec4<TX>::load(reinterpret_cast<const TX*>(a.x) + o) * a.rstd[row]);
-      float* s = &sum[wave][k][lane * 4];
-      Vec4<float>::store(s, Vec4<float>::load(s) + t);
-    }
-  }
-  __syncthreads();
-  for (int k = wave; k < a.groups; k += kNormWaves) {
-    if (c >= a.d) break;
-    f32x4 t = Vec4<float>::load(&sum[0][k][lane * 4]);
+  const f32x4 zero = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 sum[GMAX], gain = zero;
 #pragma unroll
-    for (int w = 1; w < kNormWaves; ++w) t += Vec4<float>::load(&sum[w][k][lane * 4]);
-    Vec4<float>::store(part + ((int64_t)blockIdx.x * a.groups + k) * a.d + c, t);
+  for (int k = 0; k < GMAX; ++k) sum[k] = zero;
+  if (GMAX == 1 && own) gain = 1.f + Vec4<float>::load(a.gamma + c);
+  struct Row {
+    Raw4<TX> x;
+    Raw4<TY> dy;
+    f32x4 gamma;
+    float r;
+    int k;
+  };
+  auto group_of = [&](int row) __attribute__((always_inline)) { return a.group ? a.group[min(row, r1 - 1)] : 0; };
+  // `group` is made uniform here, a step after its load: at the load it would wait for every load before it
+  auto fetch = [&](int row, int group, Row& o) __attribute__((always_inline)) {
+    const int g = __builtin_amdgcn_readfirstlane(group), k = g >= 0 && g < a.groups ? g : -1;
+    o.k = k;
+    o.r = a.rstd[min(row, r1 - 1)];
+    o.x.zero();
+    o.dy.zero();
+    o.gamma = zero;
+    if (own && row < r1) {
+      o.x.load(a.x, (int64_t)row * a.d + c);
+      o.dy.load(a.dy, (int64_t)row * a.d + c);
+      if (GMAX > 1 && k >= 0) o.gamma = Vec4<float>::load(a.gamma + (int64_t)k * a.d + c);
+    }
+  };
+  Row cur[RU], next[RU];
+  int kn[RU];
+#pragma unroll
+  for (int u = 0; u < RU; ++u) {
+    fetch(r0 + u, group_of(r0 + u), cur[u]);
+    kn[u] = group_of(r0 + RU + u);
   }
+  for (int row = r0, it = 0; row < r1; row += RU, it ^= 1) {
+    f32x4 h[RU];
+    float m[RU];
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      fetch(row + RU + u, kn[u], next[u]);
+      kn[u] = group_of(row + 2 * RU + u);
+    }
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      const f32x4 x = cur[u].x.get();
+      h[u] = cur[u].dy.get();
+      if (GMAX > 1) h[u] *= 1.f + cur[u].gamma;
+      else if (cur[u].k >= 0) h[u] *= gain;
+      m[u] = wave_sum((x[0] * h[u][0] + x[1] * h[u][1]) + (x[2] * h[u][2] + x[3] * h[u][3]));
+    }
+    if (lane == 0) {
+#pragma unroll
+      for (int u = 0; u < RU; ++u) red[it][wave][u] = m[u];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int u = 0; u < RU; ++u) m[u] = red[it][0][u];
+    for (int w = 1; w < nw; ++w)
+#pragma unroll
+      for (int u = 0; u < RU; ++u) m[u] += red[it][w][u];
+#pragma unroll
+    for (int u = 0; u < RU; ++u) {
+      if (row + u >= r1) break;
+      const float r = cur[u].r, s = r * r * (m[u] / (float)a.d);
+      const f32x4 x = cur[u].x.get(), t = cur[u].dy.get() * (x * r);
+      if (own && a.out) Vec4<TX>::store(reinterpret_cast<TX*>(a.out) + (int64_t)(row + u) * a.d + c, r * (h[u] - x * s));
+#pragma unroll
+      for (int k = 0; k < GMAX; ++k)
+        if (cur[u].k == k) sum[k] += t;
+    }
+#pragma unroll
+    for (int u = 0; u < RU; ++u) cur[u] = next[u];
+  }
+  if (!own) return;
+  float* o = part + (int64_t)blockIdx.x * a.groups * a.d + c;
+#pragma unroll
+  for (int k = 0; k < GMAX; ++k)
+    if (k < a.groups) Vec4<float>::store(o + k * a.d, sum[k]);
 }
 
-// The chunks' sums, added in order.
-__global__ __launch_bounds__(256) void k_norm_join(const float* part, int chunks, int n, float* out) {
-  const int e = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (e >= n) return;
+// The workgroups' sums: each of 16 waves adds every 16th one, the waves' sums are added in order.
+__global__ __launch_bounds__(1024) void k_norm_join(const float* part, int chunks, int n, float* out) {
+  __shared__ __align__(16) float sum[16][kGammaCols];
+  const int lane = lane_id(), wave = threadIdx.x / kWave, e = blockIdx.x * kGammaCols + lane * 4;
   f32x4 t = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k = 0; k < chunks; ++k) t += Vec4<float>::load(part + (int64_t)k * n + e);
+  if (e < n) {
+#pragma unroll 4
+    for (int k = wave; k < chunks; k += 16) t += Vec4<float>::load(part + (int64_t)k * n + e);
+  }
+  Vec4<float>::store(&sum[wave][lane * 4], t);
+  __syncthreads();
+  if (wave > 0 || e >= n) return;
+#pragma unroll
+  for (int w = 1; w < 16; ++w) t += Vec4<float>::load(&sum[w][lane * 4]);
   Vec4<float>::store(out + e, t);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-int gamma_chunk(int rows) {
-  int c = (rows + kGammaChunks - 1) / kGammaChunks;
-  return c < 16 ? 16 : c;
+// Rows of a workgroup: 16 waves per compute unit where the rows allow it (8 with
+// twice the rows in flight were slower: 32768 x 1024, 8 groups, 107 against 90
+// us), and 8 rows at least, so that the sums stay a small part of the traffic
+// and few rows still spread (300 x 1024: 16 rows 16 us, 8 rows 12).
+int grad_chunk(int rows, int d) {
+  const int waves = (d + kGammaCols - 1) / kGammaCols, most = 4096 / waves;
+  const int c = (rows + most - 1) / most;
+  return c < 8 ? 8 : c;
 }
-int gamma_chunks(int rows) { return (rows + gamma_chunk(rows) - 1) / gamma_chunk(rows); }
+int grad_chunks(int rows, int d) { return (rows + grad_chunk(rows, d) - 1) / grad_chunk(rows, d); }
 
 bool is_dtype(int32_t t) { return t == TLF_DTYPE_F32 || t == TLF_DTYPE_BF16; }
 
@@ -169,20 +281,27 @@ template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(const Norm
   return hipGetLastError();
 }
 
+template <typename TX, typename TY, int MAXT, int RU>
+void launch_sums(const NormArgs& a, int chunk, int chunks, float* part, hipStream_t s) {
+  const dim3 grid(chunks), block((a.d + kGammaCols - 1) / kGammaCols * kWave);
+  if (a.groups == 1) hipLaunchKernelGGL((k_norm_grad<TX, TY, 1, MAXT, RU>), grid, block, 0, s, a, chunk, part);
+  else if (a.groups <= 8) hipLaunchKernelGGL((k_norm_grad<TX, TY, 8, MAXT, RU>), grid, block, 0, s, a, chunk, part);
+  else hipLaunchKernelGGL((k_norm_grad<TX, TY, TLF_NORM_MAX_GROUPS, MAXT, RU>), grid, block, 0, s, a, chunk, part);
+}
+
 template <typename TX, typename TY> hipError_t launch_grad(const NormArgs& a, void* dx, float* dgamma, float* part, hipStream_t s) {
-  if (dx && a.rows > 0) {
-    NormArgs b = a;
-    b.out = dx;
-    const hipError_t e = launch_rows<TX, TY, true>(b, s);
+  NormArgs b = a;
+  b.out = dx;
+  if (!dgamma) return a.rows > 0 ? launch_rows<TX, TY, true>(b, s) : hipSuccess;
+  const int chunk = grad_chunk(a.rows, a.d), chunks = grad_chunks(a.rows, a.d), n = a.groups * a.d;
+  if (chunks > 0) {
+    if (a.d <= 1024) launch_sums<TX, TY, 256, kGradRows>(b, chunk, chunks, part, s);
+    else if (a.d <= 2048) launch_sums<TX, TY, 512, kGradRows>(b, chunk, chunks, part, s);
+    else launch_sums<TX, TY, 1024, kGradRows>(b, chunk, chunks, part, s);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (dgamma) {
-    const int chunks = gamma_chunks(a.rows), n = a.groups * a.d;
-    if (chunks > 0)
-      hipLaunchKernelGGL((k_norm_dgamma<TX, TY>), dim3(chunks, (a.d + kGammaCols - 1) / kGammaCols),
-                         dim3(kNormWaves * kWave), 0, s, a, gamma_chunk(a.rows), part);
-    hipLaunchKernelGGL(k_norm_join, dim3((n / 4 + 255) / 256), dim3(256), 0, s, part, chunks, n, dgamma);
-  }
+  hipLaunchKernelGGL(k_norm_join, dim3((n + kGammaCols - 1) / kGammaCols), dim3(1024), 0, s, part, chunks, n, dgamma);
   return hipGetLastError();
 }
 
@@ -211,7 +330,7 @@ int tlf_rms_norm(const void* d_x, int32_t x_dtype, const float* d_gamma, const i
 int tlf_rms_norm_grad_ws_bytes(int32_t groups, int32_t rows, int32_t d, size_t* ws_bytes) {
   const int st = tlf::check(TLF_DTYPE_F32, TLF_DTYPE_F32, groups, rows, d);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  *ws_bytes = (size_t)tlf::gamma_chunks(rows) * groups * d * sizeof(float);
+  *ws_bytes = (size_t)tlf::grad_chunks(rows, d) * groups * d * sizeof(float);
   return TLF_OK;
 }
 

@@ -212,9 +212,16 @@ def ste(score: torch.Tensor, depth: torch.Tensor) -> torch.Tensor:
 _DTYPE = {torch.float32: tlf.DTYPE_F32, torch.bfloat16: tlf.DTYPE_BF16}
 
 
-def _on(t: torch.Tensor):
-    """The tensor's device made current for a call (its current stream is then the one that _stream gives)."""
-    return torch.cuda.device(t.device)
+def _run(fn, device: torch.device, *args) -> None:
+    """fn(*args, stream) with `device` current, on that device's current stream; tensors among the arguments stand for
+    their addresses."""
+    args = [a.data_ptr() if isinstance(a, torch.Tensor) else a for a in args]
+    if device.index == torch.cuda.current_device():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    _check(status, fn.__name__)
 
 
 def _same_device(t, *others):
@@ -240,9 +247,8 @@ class _RmsNorm(torch.autograd.Function):
         groups = 0 if gamma is None else gamma.numel() // d
         y = torch.empty((rows, d), dtype=dtype, device=x.device)
         rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if grad else None
-        with _on(x):
-            _check(tlf.load().tlf_rms_norm(_ptr(x), _DTYPE[x.dtype], _ptr(gamma), _ptr(group), groups, rows, d, eps,
-                                           _ptr(y), _DTYPE[dtype], _ptr(rstd), _stream()), "tlf_rms_norm")
+        _run(tlf.load().tlf_rms_norm, x.device, x, _DTYPE[x.dtype], gamma, group, groups, rows, d, eps, y, _DTYPE[dtype],
+             rstd)
         if grad:
             ctx.save_for_backward(x, gamma, group, rstd)
         return y
@@ -260,10 +266,8 @@ class _RmsNorm(torch.autograd.Function):
         ws, n = None, 0
         if dgamma is not None:
             ws, n = _workspace(lib.tlf_rms_norm_grad_ws_bytes, groups, rows, d, device=x.device)
-        with _on(x):
-            _check(lib.tlf_rms_norm_grad(_ptr(dy), _DTYPE[dy.dtype], _ptr(x), _DTYPE[x.dtype], _ptr(gamma),
-                                         _ptr(group), groups, _ptr(rstd), rows, d, _ptr(dx), _ptr(dgamma), _ptr(ws),
-                                         n, _stream()), "tlf_rms_norm_grad")
+        _run(lib.tlf_rms_norm_grad, x.device, dy, _DTYPE[dy.dtype], x, _DTYPE[x.dtype], gamma, group, groups, rstd, rows,
+             d, dx, dgamma, ws, n)
         return dx, dgamma, None, None, None, None
 
 
@@ -305,33 +309,32 @@ class _Ffn(torch.autograd.Function):
     def forward(ctx, x, w_gate_up, w_down, grad):
         rows, d = x.shape
         f = w_down.shape[1]
-        new = lambda *s: torch.empty(s, dtype=x.dtype, device=x.device)  # noqa: E731
-        kept = None
+        code = _DTYPE[x.dtype]
+        # what the backward pass keeps, then a (a multiple of 16 bytes), in one buffer
+        size = tlf.ffn_kept_bytes(code, rows, f) if grad else 0
+        kept = torch.empty(size + rows * f * x.element_size(), dtype=torch.uint8, device=x.device)
+        y = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+        at = kept.data_ptr()
+        _run(tlf.load().tlf_ffn, x.device, x, w_gate_up, w_down, code, rows, d, f, at if grad else None, at + size, y)
         if grad:
-            kept = torch.empty(tlf.ffn_kept_bytes(_DTYPE[x.dtype], rows, f), dtype=torch.uint8, device=x.device)
-        a, y = new(rows, f), new(rows, d)
-        with _on(x):
-            _check(tlf.load().tlf_ffn(_ptr(x), _ptr(w_gate_up), _ptr(w_down), _DTYPE[x.dtype], rows, d, f, _ptr(kept),
-                                      _ptr(a), _ptr(y), _stream()), "tlf_ffn")
-        if grad:
-            ctx.save_for_backward(x, w_gate_up, w_down, kept, a)
+            ctx.save_for_backward(x, w_gate_up, w_down, kept)
         return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, w_gate_up, w_down, kept, a = ctx.saved_tensors
+        x, w_gate_up, w_down, kept = ctx.saved_tensors
         rows, d = x.shape
         f = w_down.shape[1]
         dy = _aligned(dy)
         outs = [torch.empty_like(t) if need else None
                 for t, need in zip((x, w_gate_up, w_down), ctx.needs_input_grad)]
         lib = tlf.load()
-        ws, n = _workspace(lib.tlf_ffn_grad_ws_bytes, _DTYPE[x.dtype], rows, d, f, device=x.device)
-        with _on(x):
-            _check(lib.tlf_ffn_grad(_ptr(dy), _ptr(x), _ptr(w_gate_up), _ptr(w_down), _ptr(kept), _ptr(a),
-                                    _DTYPE[x.dtype], rows, d, f, *[_ptr(o) for o in outs], _ptr(ws), n, _stream()),
-                   "tlf_ffn_grad")
+        code = _DTYPE[x.dtype]
+        ws, n = _workspace(lib.tlf_ffn_grad_ws_bytes, code, rows, d, f, device=x.device)
+        at = kept.data_ptr()
+        _run(lib.tlf_ffn_grad, x.device, dy, x, w_gate_up, w_down, at, at + tlf.ffn_kept_bytes(code, rows, f), code, rows,
+             d, f, *outs, ws, n)
         return (*outs, None)
 
 
@@ -408,7 +411,7 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
     with torch.cuda.device(dev):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("adamw_: the step number and rates are values and cannot be captured into a graph")
-        _check(tlf.load().tlf_adamw(table, n, lr, betas[0], betas[1], eps, _stream()), "tlf_adamw")
+    _run(tlf.load().tlf_adamw, dev, table, n, lr, betas[0], betas[1], eps)
     # a graph that saved a parameter or copy for its backward pass has to notice the update
     torch.autograd.graph.increment_version([*params, *(c for c in copies if c is not None)])
 

@@ -93,6 +93,12 @@ def test_norm_types(xt, yt, rows, d, groups):
     _check_norm(rows, d, groups, xt, yt)
 
 
+@pytest.mark.parametrize("rows,d,groups", [(50, 2048, 16), (70, 2304, 16), (100, 4096, 9), (61, 4096, 16), (5000, 8, 3)])
+def test_norm_many_scales(rows, d, groups):
+    """Sums of 128 to 256 KB, around what fits LDS, and many rows of few columns."""
+    _check_norm(rows, d, groups, "f32", "bf16")
+
+
 def test_norm_without_rows():
     train = _train()
     x, gamma = torch.zeros(0, 128, device="cuda", requires_grad=True), torch.ones(2, 128, device="cuda", requires_grad=True)
