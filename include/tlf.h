@@ -457,15 +457,17 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
  *                 bits with 9 bits of mantissa and magnitudes up to 2^32), or NULL if
  *                 no gradient follows;
  *   d_a           [rows][f], receives a (read by the second product);
- *   d_y           [rows][d].
+ *   d_y           [rows][d];
+ *   d_workspace   tlf_ffn_ws_bytes bytes (may be 0), used during the call only.
  * d and f multiples of 64, at most TLF_FFN_MAX_WIDTH. */
 #define TLF_FFN_MAX_WIDTH 16384
 static inline size_t tlf_ffn_kept_bytes(int32_t dtype, int32_t rows, int32_t f) {
   return rows <= 0 || f <= 0 ? 0
                              : ((size_t)rows + 15) / 16 * 16 * 2u * (size_t)f * (dtype == TLF_DTYPE_BF16 ? 2u : 4u);
 }
+int tlf_ffn_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes);
 int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
-            int32_t f, void* d_kept, void* d_a, void* d_y, void* stream);
+            int32_t f, void* d_kept, void* d_a, void* d_y, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* Gradients of tlf_ffn from the `kept` and a that it wrote:
  *   da = dy W_down,  dg = da u silu'(g),  du = da silu(g) (rounded to dtype),

@@ -214,9 +214,12 @@ __device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA, KB>& a, const Frag<T,
   }
 }
 
-// Tile of BM x BN by WM x WN waves, KB bytes of k per step, RING steps in LDS.
-template <int BM_, int BN_, int WM_, int WN_, int KB_, int RING_> struct FShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, RING = RING_, NTH = WM_ * WN_ * kWave;
+// Tile of BM x BN by WM x WN waves, KB bytes of k per step, RING steps in LDS;
+// WK groups of such waves share the tile's steps (their sums are added in LDS
+// afterwards, in a fixed order).
+template <int BM_, int BN_, int WM_, int WN_, int KB_, int RING_, int WK_> struct FShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, RING = RING_, WK = WK_;
+  static constexpr int GTH = WM * WN * kWave, NTH = GTH * WK;
 };
 
 // Workgroup L runs on XCD L % 8, and each XCD has its own L2: every XCD gets
@@ -236,7 +239,7 @@ struct Tiles {
   }
 };
 
-// Split of a weight gradient's tiles over G workgroups: workgroup b computes
+// Split of a product's tiles over G workgroups: workgroup b computes
 // `whole` tiles, then the steps [first(b), first(b + 1)) of the remaining ones
 // taken one after the other, KT steps each.  A tile that falls to several
 // workgroups is left in parts, which k_ffn_join adds in order: the part that
@@ -257,7 +260,7 @@ struct Split {
 };
 
 template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct Tile {
-  static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::NTH, KB = SH::KB, RING = SH::RING;
+  static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::GTH, KB = SH::KB, RING = SH::RING, WK = SH::WK;
   static constexpr int MT = BM / SH::WM / 16, NT = BN / SH::WN / 16;
   using OA = Operand<T, TA, BM, KB>;
   using OB = Operand<T, TB, BN, KB>;
@@ -268,13 +271,18 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
   static constexpr int TN = EK == E_SWIGLU ? BN / 2 : BN;  // columns of N that a tile covers
   static_assert(OA::BYTES % (16 * NTH) == 0 && OB::BYTES % (16 * NTH) == 0, "chunks");
   static_assert(NT % 2 == 0 && (EK != E_SWIGLU || (NT % 4 == 0 && !TB)), "pairs of columns, of gate and of up");
-  static constexpr int LDS = RING * STEP;
+  static constexpr int LDS = WK * RING * STEP;
+  static_assert((WK - 1) * BM * BN * 4 <= LDS && LDS <= 160 * 1024, "LDS");
 
-  // Steps [k0, k1) of the tile at (m0, n0); the sums go to the epilogue, or
+  // Steps [first, last) of the tile at (m0, n0); the sums go to the epilogue, or
   // (SPLIT, part) to a part.
-  static __device__ __forceinline__ void run(const FArgs& g, int m0, int n0, int k0, int k1, float* part, char* lds) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
+  static __device__ __forceinline__ void run(const FArgs& g, int m0, int n0, int first, int last, float* part, char* lds0) {
+    const int grp = WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NTH);
+    const int tid = threadIdx.x - grp * NTH, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
     const int wbase = __builtin_amdgcn_readfirstlane(tid & ~(kWave - 1));
+    char* lds = lds0 + grp * (RING * STEP);
+    // this group's steps [k0, k1); all groups go through `turns` of them
+    const int turns_n = (last - first + WK - 1) / WK, k0 = min(first + grp * turns_n, last), k1 = min(k0 + turns_n, last);
 
     // byte offsets of this thread's chunks from the step's first element; rows
     // and columns past the matrix read the last one (their results are not stored)
@@ -362,8 +370,8 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
       for (int j = 0; j < NT; ++j) acc[i][j] = mma(b[j], a[i], acc[i][j]);
     };
 
-    if (k0 < k1) {
-      if constexpr (NTH == 512) {
+    if (first < last) {
+      if constexpr (KB == 64) {
         // A ring of five steps, loaded two at a time: a row's 128-byte line is then
         // fetched by neighbouring loads.  Two waves on each SIMD take turns: while
         // one multiplies a step, the other reads the fragments of its next one, then
@@ -372,7 +380,7 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
         // loads k + 3 and k + 4 between its products.  When the early waves have
         // multiplied step k and the late ones have read it, everyone waits for its
         // own loads of k + 1.
-        static_assert(KB == 64 && RING == 5 && MT == 2 * LPT, "loads between the products");
+        static_assert(NTH == 512 && WK == 1 && RING == 5 && MT == 2 * LPT, "loads between the products");
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if (k0 + k < k1) issue_any(k0 + k, k);
@@ -446,22 +454,48 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
           if (k0 + k < k1) issue_any(k0 + k, k);
         if (k0 + RING - 1 < kfull) wait_barrier<(RING - 1) * LPT>();
         else wait_barrier<0>();
-        fetch(a0, b0, 0, 0);
+        if (WK == 1 || k0 < k1) fetch(a0, b0, 0, 0);
         int st = 0;
-        for (int kt = k0; kt < k1; ++kt) {
-          const int sn = st + 1 == RING ? 0 : st + 1;
-          fetch(a1, b1, st, 1);
+        for (int it = 0; it < turns_n; ++it) {
+          const int kt = k0 + it, sn = st + 1 == RING ? 0 : st + 1;
+          const bool on = WK == 1 || kt < k1;
+          if (on) {
+            fetch(a1, b1, st, 1);
 #pragma unroll
-          for (int i = 0; i < MT; ++i) multiply(a0, b0, i);
+            for (int i = 0; i < MT; ++i) multiply(a0, b0, i);
+          }
           if (RING > 2 && kt + RING - 1 < kfull) wait_barrier<(RING - 2) * LPT>();
           else wait_barrier<0>();
           if (kt + RING < k1) issue_any(kt + RING, st);
           if (kt + 1 < k1) fetch(a0, b0, sn, 0);
+          if (on) {
 #pragma unroll
-          for (int i = 0; i < MT; ++i) multiply(a1, b1, i);
+            for (int i = 0; i < MT; ++i) multiply(a1, b1, i);
+          }
           st = sn;
         }
       }
+    }
+    if constexpr (WK > 1) {
+      // groups 1 .. WK - 1 hand their sums to group 0
+      float* sums = reinterpret_cast<float*>(lds0);
+      __syncthreads();
+      if (grp > 0) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            Vec4<float>::store(sums + (grp - 1) * (BM * BN) + (((wave * MT + i) * NT + j) * kWave + lane) * 4, acc[i][j]);
+      }
+      __syncthreads();
+      if (grp > 0) return;
+#pragma unroll
+      for (int k = 1; k < WK; ++k)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[i][j] += Vec4<float>::load(sums + (k - 1) * (BM * BN) + (((wave * MT + i) * NT + j) * kWave + lane) * 4);
     }
 
     // lane: row m0 + .. + lane % 16, columns .. + 4 (lane / 16) + 0..3
@@ -533,10 +567,10 @@ template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch
   TL::run(g, row * SH::BM, col * TL::TN, 0, (g.K + TL::BK - 1) / TL::BK, nullptr, lds);
 }
 
-// Weight gradients: few tiles and a long sum over rows, dealt evenly to the
-// compute units (Split).
-template <typename T, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn_split(FArgs g) {
-  using TL = Tile<T, true, true, E_STORE, SH, true>;
+// Products with few tiles and a long sum (weight gradients: over the rows),
+// dealt evenly to the compute units (Split).
+template <typename T, bool TA, bool TB, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn_split(FArgs g) {
+  using TL = Tile<T, TA, TB, E_STORE, SH, true>;
   __shared__ __align__(16) char lds[TL::LDS];
   const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + SH::BN - 1) / SH::BN};
   const Split sp((int64_t)ts.tm * ts.tn, gridDim.x, (g.K + TL::BK - 1) / TL::BK);
@@ -582,9 +616,10 @@ template <typename T, typename SH> __global__ __launch_bounds__(256) void k_ffn_
   if (m < g.M && n < g.N) Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + n, c);
 }
 
-using Big = FShape<256, 256, 2, 4, 64, 5>;
-using Mid = FShape<128, 128, 2, 2, 128, 2>;
-using Small = FShape<64, 64, 4, 1, 128, 3>;
+using Big = FShape<256, 256, 2, 4, 64, 5, 1>;
+using Mid = FShape<128, 128, 2, 2, 128, 2, 1>;
+using Small = FShape<64, 64, 4, 1, 128, 3, 1>;
+using Deep = FShape<64, 64, 4, 1, 128, 2, 4>;
 
 template <typename T, bool TA, bool TB, int EK, typename SH> hipError_t launch_shape(const FArgs& g, hipStream_t s) {
   constexpr int TN = EK == E_SWIGLU ? SH::BN / 2 : SH::BN;
@@ -594,12 +629,29 @@ template <typename T, bool TA, bool TB, int EK, typename SH> hipError_t launch_s
   return hipGetLastError();
 }
 
-template <typename T, bool TA, bool TB, int EK> hipError_t launch_ffn(const FArgs& g, hipStream_t s) {
-  const int64_t mid = (int64_t)((g.M + 127) / 128) * ((g.N + 127) / 128) * (EK == E_SWIGLU ? 2 : 1);
+constexpr int64_t kCus = 256;  // compute units
+
+int64_t tiles_of(int64_t m, int64_t n, int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); }
+
+// Whether tiles of 256 x 256, one per compute unit at a time, leave less than a
+// third of the compute units' time unused.
+bool big_fits(int64_t tiles) {
+  const int64_t rounds = (tiles + kCus - 1) / kCus;
+  return tiles >= 160 && 3 * tiles >= 2 * kCus * rounds;
+}
+
+// The fused products: Big where it fits, Mid from 300 tiles of its size, else
+// Small.  bf16, us with Small, Mid and Big, gate/up with the product down
+// behind it and da with dx: 1000 x 768 x 2048 29, 29, 42 and 36, 43, 56; 1000 x
+// 2048 x 5504 113, 102, 97 and 144, 127, 138; 8191 x 2048 x 5504 874, 751, 684
+// and 1020, 947, 909.  float32 is bound by its matrix instructions and takes
+// Small (1000 x 256 x 512: 24 and 36, Mid 36 and 51).
+template <typename T, bool TA, bool TB, int EK> hipError_t launch_fused(const FArgs& g, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
-    if (mid >= 768) return launch_shape<T, TA, TB, EK, Big>(g, s);
+    const int64_t n = EK == E_SWIGLU ? 2 * (int64_t)g.N : g.N;
+    if (big_fits(tiles_of(g.M, n, 256))) return launch_shape<T, TA, TB, EK, Big>(g, s);
+    if (tiles_of(g.M, n, 128) >= 300) return launch_shape<T, TA, TB, EK, Mid>(g, s);
   }
-  if (mid >= 200) return launch_shape<T, TA, TB, EK, Mid>(g, s);
   return launch_shape<T, TA, TB, EK, Small>(g, s);
 }
 
@@ -613,58 +665,91 @@ int check(int32_t dtype, int32_t rows, int32_t d, int32_t f) {
   return TLF_OK;
 }
 
-constexpr int kCus = 256;  // compute units
-
-// How a weight gradient [m][n] summed over `rows` rows is computed.
-struct GradPlan {
-  int shape;  // 0 Small, 1 Mid, 2 Big
-  int G;      // workgroups that the tiles are split over, or 0
+// How a product that is only stored is computed.
+enum { P_SMALL = 0, P_MID = 1, P_BIG = 2, P_DEEP = 3 };
+struct Plan {
+  int shape;
+  int G;  // workgroups that the tiles are split over, or 0
 };
 
-GradPlan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
-  auto tiles = [&](int64_t b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-  GradPlan p{0, 0};
-  if (half && rows >= 1024) p.shape = 2;
-  else if (tiles(128) >= 200) p.shape = 1;
-  const int64_t nt = tiles(p.shape == 2 ? 256 : p.shape == 1 ? 128 : 64), KT = (rows + 31) / 32;
-  const int G = p.shape == 2 ? kCus : 2 * kCus;
-  const int64_t over = nt % G;
-  if (over != 0 && KT * (G - over) > 40 * G && nt * KT >= G) p.G = G;
-  return p;
+int tile_of(int shape) { return shape == P_BIG ? 256 : shape == P_MID ? 128 : 64; }
+
+// y and dx, m rows, n columns, `stages` of 128 bytes of k.  Large tiles where
+// they fill the device; 64 x 64 by four waves from 400 tiles on, by 16 waves,
+// which share the sum, below; and where 64 of them or fewer have a long sum, the
+// tiles split over all compute units.  us of the forward pass with Small, Deep
+// and Small split over 256: 1 x 2048 x 5504 43, 32, 25; 333 x 768 x 2048 22, 20,
+// 24; 1000 x 768 x 2048 30, 26, 33; 2000 x 1024 x 2816 60, 64, 60.
+Plan store_plan(bool half, int64_t m, int64_t n, int64_t stages) {
+  if (half && big_fits(tiles_of(m, n, 256))) return {P_BIG, 0};
+  if (half && tiles_of(m, n, 128) >= 300) return {P_MID, 0};
+  const int64_t tiles = tiles_of(m, n, 64);
+  if (tiles >= 400) return {P_SMALL, 0};
+  if (tiles <= 64 && stages > 64) return {P_SMALL, (int)kCus};
+  return {P_DEEP, 0};
 }
 
-size_t part_bytes(int32_t dtype, int64_t m, int64_t n, int64_t rows) {
-  const GradPlan p = grad_plan(dtype == TLF_DTYPE_BF16, m, n, rows);
-  const size_t b = p.shape == 2 ? 256 : p.shape == 1 ? 128 : 64;
-  return (size_t)p.G * 2 * b * b * sizeof(float);
+// A weight gradient [m][n], a sum over `rows` rows.  bf16: large tiles where
+// they fill the device; split over the compute units where those left without a
+// tile would wait longer than the parts cost (100 steps of 32 rows: 2 x 64 MB
+// written and read); else 128 x 128 from 300 tiles on, or 64 x 64.  us of dW_down with
+// Small, Mid, Big and Big split: 1000 x 768 x 2048 12, 16, 29, 34; 3001 x 1024 x
+// 2816 37, 44, 73, 49; 6000 x 768 x 2048 54, 72, 129, 50; 8191 x 2048 x 5504 339,
+// 238, 183, 266.  float32: 64 x 64, split where there are fewer than 256 tiles
+// and 512 rows or more (3001 x 256 x 512: 71 -> 21 us).
+Plan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
+  if (!half) return {P_SMALL, tiles_of(m, n, 64) < kCus && rows >= 512 ? (int)kCus : 0};
+  const int64_t big = tiles_of(m, n, 256);
+  if (big_fits(big)) return {P_BIG, 0};
+  const int64_t over = big % kCus;
+  if (over != 0 && rows / 32 * (kCus - over) > 100 * kCus) return {P_BIG, (int)kCus};
+  return {tiles_of(m, n, 128) >= 300 ? P_MID : P_SMALL, 0};
 }
+
+size_t part_bytes(const Plan& p) { return (size_t)p.G * 2 * tile_of(p.shape) * tile_of(p.shape) * sizeof(float); }
 
 size_t dgu_bytes(int32_t dtype, int64_t rows, int64_t f) {
   return (size_t)(rows * 2 * f) * (dtype == TLF_DTYPE_BF16 ? 2 : 4);
 }
 
-template <typename T>
-int ffn_forward(const void* x, const void* wgu, const void* wd, int rows, int d, int f, void* kept, void* a, void* y,
-                hipStream_t s) {
-  FArgs p{};
-  p.A = x; p.B = wgu; p.lda = d; p.ldb = d; p.ldo = f;
-  p.M = rows; p.N = f; p.K = d; p.out = a; p.kept = kept;
-  if (launch_ffn<T, false, false, E_SWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
-  FArgs q{};
-  q.A = a; q.B = wd; q.lda = f; q.ldb = f; q.ldo = d;
-  q.M = rows; q.N = d; q.K = f; q.out = y;
-  return launch_ffn<T, false, false, E_STORE>(q, s) == hipSuccess ? TLF_OK : TLF_E_HIP;
-}
-
-template <typename T, typename SH> hipError_t launch_grad(const FArgs& p, int G, hipStream_t s) {
-  if (G == 0) return launch_shape<T, true, true, E_STORE, SH>(p, s);
+template <typename T, bool TA, bool TB, typename SH> hipError_t launch_split(const FArgs& p, int G, hipStream_t s) {
+  if (G == 0) return launch_shape<T, TA, TB, E_STORE, SH>(p, s);
   const int64_t tiles = (int64_t)((p.M + SH::BM - 1) / SH::BM) * ((p.N + SH::BN - 1) / SH::BN);
   const int KT = (p.K + SH::KB / (int)sizeof(T) - 1) / (SH::KB / (int)sizeof(T));
-  hipLaunchKernelGGL((k_ffn_split<T, SH>), dim3(G), dim3(SH::NTH), 0, s, p);
+  hipLaunchKernelGGL((k_ffn_split<T, TA, TB, SH>), dim3(G), dim3(SH::NTH), 0, s, p);
   const int rest = (int)(tiles % G);
   if (rest > 0)
     hipLaunchKernelGGL((k_ffn_join<T, SH>), dim3(SH::BM * SH::BN / 1024, rest), dim3(256), 0, s, p, G, KT);
   return hipGetLastError();
+}
+
+template <typename T, bool TA, bool TB> hipError_t launch_store(const FArgs& p, const Plan& plan, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (plan.shape == P_BIG) {
+      if constexpr (TA) return launch_split<T, TA, TB, Big>(p, plan.G, s);
+      else return launch_shape<T, TA, TB, E_STORE, Big>(p, s);
+    }
+    if (plan.shape == P_MID) return launch_shape<T, TA, TB, E_STORE, Mid>(p, s);
+    if constexpr (TA) return launch_shape<T, TA, TB, E_STORE, Small>(p, s);
+  }
+  if constexpr (!TA) {
+    if (plan.shape == P_DEEP) return launch_shape<T, TA, TB, E_STORE, Deep>(p, s);
+  }
+  return launch_split<T, TA, TB, Small>(p, plan.G, s);
+}
+
+template <typename T>
+int ffn_forward(const void* x, const void* wgu, const void* wd, int rows, int d, int f, void* kept, void* a, void* y,
+                float* part, hipStream_t s) {
+  FArgs p{};
+  p.A = x; p.B = wgu; p.lda = d; p.ldb = d; p.ldo = f;
+  p.M = rows; p.N = f; p.K = d; p.out = a; p.kept = kept;
+  if (launch_fused<T, false, false, E_SWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
+  FArgs q{};
+  q.A = a; q.B = wd; q.lda = f; q.ldb = f; q.ldo = d;
+  q.M = rows; q.N = d; q.K = f; q.out = y; q.part = part;
+  const Plan plan = store_plan(sizeof(T) == 2, rows, d, (int64_t)f * (int64_t)sizeof(T) / 128);
+  return launch_store<T, false, false>(q, plan, s) == hipSuccess ? TLF_OK : TLF_E_HIP;
 }
 
 template <typename T>
@@ -672,11 +757,7 @@ hipError_t weight_grad(const void* a, int m, const void* b, int n, int rows, voi
   FArgs p{};
   p.A = a; p.B = b; p.lda = m; p.ldb = n; p.ldo = n;
   p.M = m; p.N = n; p.K = rows; p.out = out; p.part = part;
-  const GradPlan plan = grad_plan(sizeof(T) == 2, m, n, rows);
-  if constexpr (sizeof(T) == 2) {
-    if (plan.shape == 2) return launch_grad<T, Big>(p, plan.G, s);
-  }
-  return plan.shape == 1 ? launch_grad<T, Mid>(p, plan.G, s) : launch_grad<T, Small>(p, plan.G, s);
+  return launch_store<T, true, true>(p, grad_plan(sizeof(T) == 2, m, n, rows), s);
 }
 
 template <typename T>
@@ -688,13 +769,14 @@ int ffn_backward(const void* dy, const void* x, const void* wgu, const void* wd,
     FArgs p{};
     p.A = dy; p.B = wd; p.lda = d; p.ldb = f; p.ldo = 2 * f;
     p.M = rows; p.N = f; p.K = d; p.out = dgu; p.kept = const_cast<void*>(kept);
-    if (launch_ffn<T, false, true, E_DSWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
+    if (launch_fused<T, false, true, E_DSWIGLU>(p, s) != hipSuccess) return TLF_E_HIP;
   }
   if (dx) {
     FArgs p{};
     p.A = dgu; p.B = wgu; p.lda = 2 * f; p.ldb = d; p.ldo = d;
-    p.M = rows; p.N = d; p.K = 2 * f; p.out = dx;
-    if (launch_ffn<T, false, true, E_STORE>(p, s) != hipSuccess) return TLF_E_HIP;
+    p.M = rows; p.N = d; p.K = 2 * f; p.out = dx; p.part = part;
+    const Plan plan = store_plan(sizeof(T) == 2, rows, d, 2 * (int64_t)f * (int64_t)sizeof(T) / 128);
+    if (launch_store<T, false, true>(p, plan, s) != hipSuccess) return TLF_E_HIP;
   }
   if (dwgu && weight_grad<T>(dgu, 2 * f, x, d, rows, dwgu, part, s) != hipSuccess) return TLF_E_HIP;
   if (dwd && weight_grad<T>(dy, d, a, f, rows, dwd, part, s) != hipSuccess) return TLF_E_HIP;
@@ -707,24 +789,41 @@ int ffn_backward(const void* dy, const void* x, const void* wgu, const void* wd,
 
 extern "C" {
 
-int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
-            int32_t f, void* d_kept, void* d_a, void* d_y, void* stream) {
+int tlf_ffn_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes) {
   const int st = tlf::check(dtype, rows, d, f);
+  if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
+  const bool half = dtype == TLF_DTYPE_BF16;
+  *ws_bytes = tlf::part_bytes(tlf::store_plan(half, rows, d, (int64_t)f * (half ? 2 : 4) / 128));
+  return TLF_OK;
+}
+
+int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,
+            int32_t f, void* d_kept, void* d_a, void* d_y, void* d_workspace, size_t ws_bytes, void* stream) {
+  size_t need = 0;
+  const int st = tlf_ffn_ws_bytes(dtype, rows, d, f, &need);
   if (st != TLF_OK) return st;
   if (rows == 0) return TLF_OK;
   if (!d_x || !d_w_gate_up || !d_w_down || !d_a || !d_y) return TLF_E_INVALID_ARG;
-  for (const void* p : {d_x, d_w_gate_up, d_w_down, (const void*)d_kept, (const void*)d_a, (const void*)d_y})
+  if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
+  for (const void* p : {d_x, d_w_gate_up, d_w_down, (const void*)d_kept, (const void*)d_a, (const void*)d_y,
+                        (const void*)d_workspace})
     if (!tlf::aligned16(p)) return TLF_E_INVALID_ARG;
   return dtype == TLF_DTYPE_BF16
-             ? tlf::ffn_forward<bf16>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (hipStream_t)stream)
-             : tlf::ffn_forward<float>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (hipStream_t)stream);
+             ? tlf::ffn_forward<bf16>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (float*)d_workspace,
+                                      (hipStream_t)stream)
+             : tlf::ffn_forward<float>(d_x, d_w_gate_up, d_w_down, rows, d, f, d_kept, d_a, d_y, (float*)d_workspace,
+                                       (hipStream_t)stream);
 }
 
 int tlf_ffn_grad_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes) {
   const int st = tlf::check(dtype, rows, d, f);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  const size_t gu = tlf::part_bytes(dtype, 2 * (int64_t)f, d, rows), dn = tlf::part_bytes(dtype, d, f, rows);
-  *ws_bytes = tlf::dgu_bytes(dtype, rows, f) + (gu > dn ? gu : dn);
+  const bool half = dtype == TLF_DTYPE_BF16;
+  size_t part = 0;  // of the three products that may be split, one after the other
+  for (const tlf::Plan& p : {tlf::store_plan(half, rows, d, 2 * (int64_t)f * (half ? 2 : 4) / 128),
+                             tlf::grad_plan(half, 2 * (int64_t)f, d, rows), tlf::grad_plan(half, d, f, rows)})
+    part = tlf::part_bytes(p) > part ? tlf::part_bytes(p) : part;
+  *ws_bytes = tlf::dgu_bytes(dtype, rows, f) + part;
   return TLF_OK;
 }
 

@@ -95,7 +95,7 @@ class CacheStats(ctypes.Structure):
 EXPORTS = ("tlf_init", "tlf_prefill", "tlf_decode_step", "tlf_cache_stats", "tlf_set_profiling", "tlf_destroy",
            "tlf_status_str", "tlf_gs_plan", "tlf_gs_plan_ws", "tlf_gs_plan_noalloc", "tlf_gs_gather",
            "tlf_gs_scatter", "tlf_gs_expand", "tlf_ste", "tlf_probe_read", "tlf_rms_norm",
-           "tlf_rms_norm_grad_ws_bytes", "tlf_rms_norm_grad", "tlf_ffn", "tlf_ffn_grad_ws_bytes", "tlf_ffn_grad",
+           "tlf_rms_norm_grad_ws_bytes", "tlf_rms_norm_grad", "tlf_ffn_ws_bytes", "tlf_ffn", "tlf_ffn_grad_ws_bytes", "tlf_ffn_grad",
            "tlf_adamw")
 
 PROBE_READ_GRAIN = 32768
@@ -189,11 +189,12 @@ def load(path: str = LIB_PATH):
     lib.tlf_rms_norm.argtypes = [vp, i32, vp, vp, i32, i32, i32, ctypes.c_float, vp, i32, vp, vp]
     lib.tlf_rms_norm_grad_ws_bytes.argtypes = [i32, i32, i32, psz]
     lib.tlf_rms_norm_grad.argtypes = [vp, i32, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, sz, vp]
-    lib.tlf_ffn.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.tlf_ffn_ws_bytes.argtypes = [i32, i32, i32, i32, psz]
+    lib.tlf_ffn.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.tlf_ffn_grad_ws_bytes.argtypes = [i32, i32, i32, i32, psz]
     lib.tlf_ffn_grad.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.tlf_adamw.argtypes = [ctypes.POINTER(AdamwTensor), i32, f64, f64, f64, f64, vp]
-    for fn in (lib.tlf_rms_norm, lib.tlf_rms_norm_grad_ws_bytes, lib.tlf_rms_norm_grad, lib.tlf_ffn,
+    for fn in (lib.tlf_rms_norm, lib.tlf_rms_norm_grad_ws_bytes, lib.tlf_rms_norm_grad, lib.tlf_ffn_ws_bytes, lib.tlf_ffn,
                lib.tlf_ffn_grad_ws_bytes, lib.tlf_ffn_grad, lib.tlf_adamw):
         fn.restype = ctypes.c_int
     _lib = lib

@@ -237,6 +237,8 @@ def _wants_grad(*tensors) -> bool:
 def _workspace(fn, *args, device):
     need = ctypes.c_size_t()
     _check(fn(*args, ctypes.byref(need)), fn.__name__)
+    if need.value == 0:
+        return None, 0
     return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
 
 
@@ -310,12 +312,14 @@ class _Ffn(torch.autograd.Function):
         rows, d = x.shape
         f = w_down.shape[1]
         code = _DTYPE[x.dtype]
+        ws, n = _workspace(tlf.load().tlf_ffn_ws_bytes, code, rows, d, f, device=x.device)
         # what the backward pass keeps, then a (a multiple of 16 bytes), in one buffer
         size = tlf.ffn_kept_bytes(code, rows, f) if grad else 0
         kept = torch.empty(size + rows * f * x.element_size(), dtype=torch.uint8, device=x.device)
         y = torch.empty((rows, d), dtype=x.dtype, device=x.device)
         at = kept.data_ptr()
-        _run(tlf.load().tlf_ffn, x.device, x, w_gate_up, w_down, code, rows, d, f, at if grad else None, at + size, y)
+        _run(tlf.load().tlf_ffn, x.device, x, w_gate_up, w_down, code, rows, d, f, at if grad else None, at + size, y,
+             ws, n)
         if grad:
             ctx.save_for_backward(x, w_gate_up, w_down, kept)
         return y

@@ -210,6 +210,20 @@ def test_ffn_many_rows(t, n, d, f):
     _check_ffn(n, d, f, t)
 
 
+@pytest.mark.parametrize("t,n,d,f", [
+    ("bf16", 6000, 512, 1856),   # the fused products on 256 x 256 tiles, a ragged last row of them
+    ("bf16", 5300, 2048, 128),   # y and dx on 256 x 256 tiles, weight gradients of few tiles split by rows
+    ("bf16", 40, 2048, 2560),    # the weight gradient on 256 x 256 tiles
+    ("bf16", 2500, 2048, 64),    # y and dx on 128 x 128 tiles
+    ("bf16", 3001, 640, 128),    # y and dx on 64 x 64 tiles, by four waves
+    ("bf16", 20, 128, 4224),     # y and dx split over the compute units
+    ("f32", 20, 128, 2304),      # the same in float32
+    ("f32", 530, 64, 64),        # fewer steps than workgroups they are split over
+])
+def test_ffn_tile_shapes(t, n, d, f):
+    _check_ffn(n, d, f, t)
+
+
 @pytest.mark.parametrize("t", ["bf16", "f32"])
 def test_ffn_without_rows(t):
     train = _train()
@@ -553,7 +567,7 @@ def test_operators_replayed_from_a_graph():
     def calls():
         s = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
         return [lib.tlf_rms_norm(P(x), B, P(gamma), P(group), G, n, d, EPS, P(y), B, P(rstd), s),
-                lib.tlf_ffn(P(y), P(wgu), P(wd), B, n, d, f, P(gu), P(a), P(z), s),
+                lib.tlf_ffn(P(y), P(wgu), P(wd), B, n, d, f, P(gu), P(a), P(z), P(ws), ws.numel(), s),
                 lib.tlf_ffn_grad(P(dy), P(y), P(wgu), P(wd), P(gu), P(a), B, n, d, f, P(dyn), P(dwgu), P(dwd), P(ws),
                                  ws.numel(), s),
                 lib.tlf_rms_norm_grad(P(dyn), B, P(x), B, P(gamma), P(group), G, P(rstd), n, d, P(dx), P(dgamma), P(ws2),
@@ -608,7 +622,7 @@ def test_rows_behind_the_last_stay_as_they_were():
     assert lib.tlf_ffn_grad_ws_bytes(B, n, d, f, ctypes.byref(size)) == tlf.OK
     ws = torch.full((size.value + 64,), 7, dtype=torch.uint8, device="cuda")
     assert lib.tlf_rms_norm(P(x), B, None, None, 0, n, d, EPS, P(h), B, P(rstd), s) == tlf.OK
-    assert lib.tlf_ffn(P(x), P(wgu), P(wd), B, n, d, f, P(gu), P(a), P(y), s) == tlf.OK
+    assert lib.tlf_ffn(P(x), P(wgu), P(wd), B, n, d, f, P(gu), P(a), P(y), P(ws), size.value, s) == tlf.OK
     assert lib.tlf_ffn_grad(P(dy), P(x), P(wgu), P(wd), P(gu), P(a), B, n, d, f, P(dx), P(dwgu), P(dwd), P(ws),
                             size.value, s) == tlf.OK
     for t in (a, y, dx, dwgu, dwd, h):

@@ -61,9 +61,10 @@ def test_rms_norm_grad_of_nothing(lib):
 
 
 def _ffn(lib, **kw):
-    a = dict(x=P, wgu=P, wd=P, t=BF16, rows=5, d=64, f=128, gu=P, a=P, y=P)
+    a = dict(x=P, wgu=P, wd=P, t=BF16, rows=5, d=64, f=128, gu=P, a=P, y=P, ws=P, n=1 << 30)
     a.update(kw)
-    return lib.tlf_ffn(a["x"], a["wgu"], a["wd"], a["t"], a["rows"], a["d"], a["f"], a["gu"], a["a"], a["y"], None)
+    return lib.tlf_ffn(a["x"], a["wgu"], a["wd"], a["t"], a["rows"], a["d"], a["f"], a["gu"], a["a"], a["y"], a["ws"],
+                       a["n"], None)
 
 
 WIDTHS = [(dict(d=0), BAD), (dict(f=-64), BAD), (dict(rows=-1), BAD), (dict(t=2), BAD), (dict(d=96), UNS),
@@ -73,7 +74,7 @@ WIDTHS = [(dict(d=0), BAD), (dict(f=-64), BAD), (dict(rows=-1), BAD), (dict(t=2)
 @pytest.mark.parametrize("kw,status", WIDTHS + [
     (dict(x=None), BAD), (dict(wgu=None), BAD), (dict(wd=None), BAD), (dict(a=None), BAD), (dict(y=None), BAD),
     (dict(x=ODD), BAD), (dict(wgu=ODD), BAD), (dict(wd=ODD), BAD), (dict(gu=ODD), BAD), (dict(a=ODD), BAD),
-    (dict(y=ODD), BAD),
+    (dict(y=ODD), BAD), (dict(ws=ODD), BAD),
 ])
 def test_ffn_refusals(lib, kw, status):
     assert _ffn(lib, **kw) == status
