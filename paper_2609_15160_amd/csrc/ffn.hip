@@ -64,7 +64,8 @@ struct FArgs {
   int M, N, K;    // E_SWIGLU: N = F
   void* out;
   void* kept;     // E_SWIGLU: written unless NULL; E_DSWIGLU: read
-  float* part;    // split tiles (SPLIT): their parts
+  float* part;    // sums over `splits` ranges of k, [range][tile], each as its accumulators lie
+  int splits;
 };
 
 // q and p between the passes.  float32: as they are.  bf16: 16 bits, of which 6
@@ -239,26 +240,6 @@ struct Tiles {
   }
 };
 
-// Split of a product's tiles over G workgroups: workgroup b computes
-// `whole` tiles, then the steps [first(b), first(b + 1)) of the remaining ones
-// taken one after the other, KT steps each.  A tile that falls to several
-// workgroups is left in parts, which k_ffn_join adds in order: the part that
-// begins inside its tile in place 0 of the workgroup, the other one in place 1.
-struct Split {
-  int64_t steps;  // of the remaining tiles
-  int G, KT, whole;
-  __host__ __device__ Split(int64_t tiles, int G_, int KT_) : G(G_), KT(KT_), whole((int)(tiles / G_)) {
-    steps = (tiles - (int64_t)whole * G) * KT;
-  }
-  __host__ __device__ int64_t first(int b) const { return steps * b / G; }
-  __host__ __device__ int owner(int64_t step) const {  // the workgroup of a step
-    int b = (int)(step * G / steps);
-    while (first(b + 1) <= step) ++b;
-    while (first(b) > step) --b;
-    return b;
-  }
-};
-
 template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct Tile {
   static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::GTH, KB = SH::KB, RING = SH::RING, WK = SH::WK;
   static constexpr int MT = BM / SH::WM / 16, NT = BN / SH::WN / 16;
@@ -275,7 +256,7 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
   static_assert((WK - 1) * BM * BN * 4 <= LDS && LDS <= 160 * 1024, "LDS");
 
   // Steps [first, last) of the tile at (m0, n0); the sums go to the epilogue, or
-  // (SPLIT, part) to a part.
+  // (SPLIT) to `part` as they are.
   static __device__ __forceinline__ void run(const FArgs& g, int m0, int n0, int first, int last, float* part, char* lds0) {
     const int grp = WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NTH);
     const int tid = threadIdx.x - grp * NTH, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
@@ -500,13 +481,11 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
 
     // lane: row m0 + .. + lane % 16, columns .. + 4 (lane / 16) + 0..3
     if constexpr (SPLIT) {
-      if (part) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j) Vec4<float>::store(part + (((wave * MT + i) * NT + j) * kWave + lane) * 4, acc[i][j]);
-        return;
-      }
+      return;
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -567,52 +546,37 @@ template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch
   TL::run(g, row * SH::BM, col * TL::TN, 0, (g.K + TL::BK - 1) / TL::BK, nullptr, lds);
 }
 
-// Products with few tiles and a long sum (weight gradients: over the rows),
-// dealt evenly to the compute units (Split).
+// Products with few tiles and a long sum, in `splits` ranges of k.  The tiles of
+// one range follow each other, so that an XCD's workgroups read the same k at a
+// time (with ranges that begin at any k, every tile's share of the same length,
+// dW_gate_up of 16384 x 1024 x 2816 took 243 us, without reuse in L2; LATER).
 template <typename T, bool TA, bool TB, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn_split(FArgs g) {
   using TL = Tile<T, TA, TB, E_STORE, SH, true>;
   __shared__ __align__(16) char lds[TL::LDS];
   const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + SH::BN - 1) / SH::BN};
-  const Split sp((int64_t)ts.tm * ts.tn, gridDim.x, (g.K + TL::BK - 1) / TL::BK);
-  const int b = xcd_run(blockIdx.x, gridDim.x);
+  const int u = xcd_run(blockIdx.x, gridDim.x), n = ts.tm * ts.tn, s = u / n, KT = (g.K + TL::BK - 1) / TL::BK;
   int row, col;
-  for (int w = 0; w < sp.whole; ++w) {
-    ts.at(w * sp.G + b, row, col);
-    TL::run(g, row * SH::BM, col * SH::BN, 0, sp.KT, nullptr, lds);
-    __syncthreads();
-  }
-  const int64_t end = sp.first(b + 1);
-  for (int64_t at = sp.first(b); at < end;) {
-    const int t = (int)(at / sp.KT), ka = (int)(at - (int64_t)t * sp.KT), kb = (int)min((int64_t)sp.KT, ka + (end - at));
-    ts.at(sp.whole * sp.G + t, row, col);
-    float* part = ka == 0 && kb == sp.KT ? nullptr : g.part + ((int64_t)b * 2 + (ka == 0)) * (SH::BM * SH::BN);
-    TL::run(g, row * SH::BM, col * SH::BN, ka, kb, part, lds);
-    __syncthreads();
-    at += kb - ka;
-  }
+  ts.at(u - s * n, row, col);
+  TL::run(g, row * SH::BM, col * SH::BN, (int)((int64_t)KT * s / g.splits), (int)((int64_t)KT * (s + 1) / g.splits),
+          g.part + (int64_t)u * (SH::BM * SH::BN), lds);
 }
 
-// The parts of the remaining tiles added in order and rounded once; a
-// workgroup per 1024 elements of a tile, in the accumulators' order.
-template <typename T, typename SH> __global__ __launch_bounds__(256) void k_ffn_join(FArgs g, int G, int KT) {
+// The ranges' sums added in order and rounded once; a workgroup per 1024
+// elements of a tile, in the accumulators' order.
+template <typename T, typename SH> __global__ __launch_bounds__(256) void k_ffn_join(FArgs g) {
   constexpr int MT = SH::BM / SH::WM / 16, NT = SH::BN / SH::WN / 16;
   const Tiles ts{(g.M + SH::BM - 1) / SH::BM, (g.N + SH::BN - 1) / SH::BN};
-  const Split sp((int64_t)ts.tm * ts.tn, G, KT);
-  const int t = blockIdx.y;
-  const int64_t s0 = (int64_t)t * KT, s1 = s0 + KT;
-  const int b0 = sp.owner(s0), b1 = sp.owner(s1 - 1);
-  if (b0 == b1) return;  // one workgroup's, stored whole
   int row, col;
-  ts.at(sp.whole * G + t, row, col);
+  ts.at(blockIdx.y, row, col);
   const int v = blockIdx.x * 256 + threadIdx.x, lane = v & 63, f = v >> 6;  // fragment of the tile
   const int j = f % NT, i = f / NT % MT, wave = f / (NT * MT);
   const int m = row * SH::BM + wave / SH::WN * (SH::BM / SH::WM) + i * 16 + (lane & 15);
   const int n = col * SH::BN + wave % SH::WN * (SH::BN / SH::WN) + j * 16 + (lane >> 4) * 4;
-  f32x4 c = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int b = b0; b <= b1; ++b) {
-    if (sp.first(b) == sp.first(b + 1)) continue;
-    c += Vec4<float>::load(g.part + ((int64_t)b * 2 + (sp.first(b) <= s0)) * (SH::BM * SH::BN) + (int64_t)v * 4);
-  }
+  const float* p = g.part + (int64_t)blockIdx.y * (SH::BM * SH::BN) + (int64_t)v * 4;
+  const int64_t step = (int64_t)gridDim.y * (SH::BM * SH::BN);
+  f32x4 c = Vec4<float>::load(p);
+#pragma unroll 4
+  for (int s = 1; s < g.splits; ++s) c += Vec4<float>::load(p + s * step);
   if (m < g.M && n < g.N) Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + n, c);
 }
 
@@ -669,64 +633,88 @@ int check(int32_t dtype, int32_t rows, int32_t d, int32_t f) {
 enum { P_SMALL = 0, P_MID = 1, P_BIG = 2, P_DEEP = 3 };
 struct Plan {
   int shape;
-  int G;  // workgroups that the tiles are split over, or 0
+  int splits;      // ranges of k that are summed apart, 1: none
+  size_t part;     // bytes of their sums
 };
 
 int tile_of(int shape) { return shape == P_BIG ? 256 : shape == P_MID ? 128 : 64; }
 
+Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
+  const int64_t b = tile_of(shape);
+  return {shape, (int)splits, splits > 1 ? (size_t)(splits * tiles_of(m, n, b) * b * b) * sizeof(float) : 0};
+}
+
 // y and dx, m rows, n columns, `stages` of 128 bytes of k.  Large tiles where
 // they fill the device; 64 x 64 by four waves from 400 tiles on, by 16 waves,
-// which share the sum, below; and where 64 of them or fewer have a long sum, the
-// tiles split over all compute units.  us of the forward pass with Small, Deep
-// and Small split over 256: 1 x 2048 x 5504 43, 32, 25; 333 x 768 x 2048 22, 20,
-// 24; 1000 x 768 x 2048 30, 26, 33; 2000 x 1024 x 2816 60, 64, 60.
+// which share the sum, below; and where 64 of them or fewer have a long sum, that
+// is split until every compute unit has a share.  us of the forward pass with
+// Small, Deep and Small split: 1 x 2048 x 5504 43, 32, 25; 333 x 768 x 2048 22,
+// 20, 24; 1000 x 768 x 2048 30, 26, 33; 2000 x 1024 x 2816 60, 64, 60.
 Plan store_plan(bool half, int64_t m, int64_t n, int64_t stages) {
-  if (half && big_fits(tiles_of(m, n, 256))) return {P_BIG, 0};
-  if (half && tiles_of(m, n, 128) >= 300) return {P_MID, 0};
+  if (half && big_fits(tiles_of(m, n, 256))) return plan_of(P_BIG, m, n, 1);
+  if (half && tiles_of(m, n, 128) >= 300) return plan_of(P_MID, m, n, 1);
   const int64_t tiles = tiles_of(m, n, 64);
-  if (tiles >= 400) return {P_SMALL, 0};
-  if (tiles <= 64 && stages > 64) return {P_SMALL, (int)kCus};
-  return {P_DEEP, 0};
+  if (tiles >= 400) return plan_of(P_SMALL, m, n, 1);
+  if (tiles > 0 && tiles <= 64 && stages > 64) return plan_of(P_SMALL, m, n, kCus / tiles < 16 ? kCus / tiles : 16);
+  return plan_of(P_DEEP, m, n, 1);
 }
 
-// A weight gradient [m][n], a sum over `rows` rows.  bf16: large tiles where
-// they fill the device; split over the compute units where those left without a
-// tile would wait longer than the parts cost (100 steps of 32 rows: 2 x 64 MB
-// written and read); else 128 x 128 from 300 tiles on, or 64 x 64.  us of dW_down with
-// Small, Mid, Big and Big split: 1000 x 768 x 2048 12, 16, 29, 34; 3001 x 1024 x
-// 2816 37, 44, 73, 49; 6000 x 768 x 2048 54, 72, 129, 50; 8191 x 2048 x 5504 339,
-// 238, 183, 266.  float32: 64 x 64, split where there are fewer than 256 tiles
-// and 512 rows or more (3001 x 256 x 512: 71 -> 21 us).
+// Estimated ns of a weight gradient with tiles of b x b, `slots` of which the
+// device holds: per round, the stages (64 rows) and a start and an end.
+int64_t rounds_time(int64_t tiles, int64_t slots, int64_t stages, int64_t stage_ns, int64_t base_ns) {
+  return (tiles + slots - 1) / slots * (stages * stage_ns + base_ns);
+}
+
+// A weight gradient [m][n], a sum over `rows` rows.  bf16: the shape of the least
+// estimated time, tiles of 256 x 256 also in ranges of rows, whose sums are
+// written and read again at 4.5 TB/s.  The times per stage are fitted to
+// dW_down, measured us with Small, Mid and Big whole: 1000 x 768 x 2048 12, 16, 29;
+// 3001 x 1024 x 2816 37, 44, 73; 6000 x 768 x 2048 54, 72, 129; 1000 x 2048 x 5504
+// 48, 41, 33; 8191 x 2048 x 5504 339, 238, 183.  float32: 64 x 64, split where there are
+// fewer than 256 tiles and 512 rows or more (3001 x 256 x 512: 71 -> 21 us).
 Plan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
-  if (!half) return {P_SMALL, tiles_of(m, n, 64) < kCus && rows >= 512 ? (int)kCus : 0};
-  const int64_t big = tiles_of(m, n, 256);
-  if (big_fits(big)) return {P_BIG, 0};
-  const int64_t over = big % kCus;
-  if (over != 0 && rows / 32 * (kCus - over) > 100 * kCus) return {P_BIG, (int)kCus};
-  return {tiles_of(m, n, 128) >= 300 ? P_MID : P_SMALL, 0};
+  const int64_t stages = (rows + 63) / 64, small = tiles_of(m, n, 64), mid = tiles_of(m, n, 128), big = tiles_of(m, n, 256);
+  if (!half) {
+    const int64_t most = rows / 128, want = (kCus + small - 1) / small;
+    return plan_of(P_SMALL, m, n, small >= kCus || rows < 512 ? 1 : want < most ? want : most);
+  }
+  Plan best = plan_of(P_SMALL, m, n, 1);
+  int64_t t = rounds_time(small, 3 * kCus, stages, small <= kCus ? 400 : small <= 2 * kCus ? 500 : 680, 3500);
+  const int64_t tm = rounds_time(mid, 2 * kCus, stages, mid <= kCus ? 850 : 930, 5000);
+  if (tm < t) {
+    t = tm;
+    best = plan_of(P_MID, m, n, 1);
+  }
+  for (int64_t s = 1; s <= 12 && (s == 1 || stages >= 4 * s); ++s) {
+    const int64_t parts = s > 1 ? s * big * 117 + 5000 : 0;  // 2 x 256 KB each
+    const int64_t tb = rounds_time(big * s, kCus, (stages + s - 1) / s, 1400, 6000) + parts;
+    if (tb < t) {
+      t = tb;
+      best = plan_of(P_BIG, m, n, s);
+    }
+  }
+  return best;
 }
-
-size_t part_bytes(const Plan& p) { return (size_t)p.G * 2 * tile_of(p.shape) * tile_of(p.shape) * sizeof(float); }
 
 size_t dgu_bytes(int32_t dtype, int64_t rows, int64_t f) {
   return (size_t)(rows * 2 * f) * (dtype == TLF_DTYPE_BF16 ? 2 : 4);
 }
 
-template <typename T, bool TA, bool TB, typename SH> hipError_t launch_split(const FArgs& p, int G, hipStream_t s) {
-  if (G == 0) return launch_shape<T, TA, TB, E_STORE, SH>(p, s);
-  const int64_t tiles = (int64_t)((p.M + SH::BM - 1) / SH::BM) * ((p.N + SH::BN - 1) / SH::BN);
-  const int KT = (p.K + SH::KB / (int)sizeof(T) - 1) / (SH::KB / (int)sizeof(T));
-  hipLaunchKernelGGL((k_ffn_split<T, TA, TB, SH>), dim3(G), dim3(SH::NTH), 0, s, p);
-  const int rest = (int)(tiles % G);
-  if (rest > 0)
-    hipLaunchKernelGGL((k_ffn_join<T, SH>), dim3(SH::BM * SH::BN / 1024, rest), dim3(256), 0, s, p, G, KT);
+template <typename T, bool TA, bool TB, typename SH> hipError_t launch_split(const FArgs& p, hipStream_t s) {
+  if (p.splits == 1) return launch_shape<T, TA, TB, E_STORE, SH>(p, s);
+  const int64_t tiles = tiles_of(p.M, p.N, SH::BM);
+  hipLaunchKernelGGL((k_ffn_split<T, TA, TB, SH>), dim3((unsigned)(tiles * p.splits)), dim3(SH::NTH), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_ffn_join<T, SH>), dim3(SH::BM * SH::BN / 1024, (unsigned)tiles), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
-template <typename T, bool TA, bool TB> hipError_t launch_store(const FArgs& p, const Plan& plan, hipStream_t s) {
+template <typename T, bool TA, bool TB> hipError_t launch_store(FArgs p, const Plan& plan, hipStream_t s) {
+  p.splits = plan.splits;
   if constexpr (sizeof(T) == 2) {
     if (plan.shape == P_BIG) {
-      if constexpr (TA) return launch_split<T, TA, TB, Big>(p, plan.G, s);
+      if constexpr (TA) return launch_split<T, TA, TB, Big>(p, s);
       else return launch_shape<T, TA, TB, E_STORE, Big>(p, s);
     }
     if (plan.shape == P_MID) return launch_shape<T, TA, TB, E_STORE, Mid>(p, s);
@@ -735,7 +723,7 @@ template <typename T, bool TA, bool TB> hipError_t launch_store(const FArgs& p, 
   if constexpr (!TA) {
     if (plan.shape == P_DEEP) return launch_shape<T, TA, TB, E_STORE, Deep>(p, s);
   }
-  return launch_split<T, TA, TB, Small>(p, plan.G, s);
+  return launch_split<T, TA, TB, Small>(p, s);
 }
 
 template <typename T>
@@ -793,7 +781,7 @@ int tlf_ffn_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* 
   const int st = tlf::check(dtype, rows, d, f);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
   const bool half = dtype == TLF_DTYPE_BF16;
-  *ws_bytes = tlf::part_bytes(tlf::store_plan(half, rows, d, (int64_t)f * (half ? 2 : 4) / 128));
+  *ws_bytes = tlf::store_plan(half, rows, d, (int64_t)f * (half ? 2 : 4) / 128).part;
   return TLF_OK;
 }
 
@@ -822,7 +810,7 @@ int tlf_ffn_grad_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, siz
   size_t part = 0;  // of the three products that may be split, one after the other
   for (const tlf::Plan& p : {tlf::store_plan(half, rows, d, 2 * (int64_t)f * (half ? 2 : 4) / 128),
                              tlf::grad_plan(half, 2 * (int64_t)f, d, rows), tlf::grad_plan(half, d, f, rows)})
-    part = tlf::part_bytes(p) > part ? tlf::part_bytes(p) : part;
+    part = p.part > part ? p.part : part;
   *ws_bytes = tlf::dgu_bytes(dtype, rows, f) + part;
   return TLF_OK;
 }
