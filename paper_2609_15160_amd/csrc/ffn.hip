@@ -135,7 +135,7 @@ template <typename T> __device__ __forceinline__ float sigmoid(float g);
 template <> __device__ __forceinline__ float sigmoid<bf16>(float g) { return __builtin_amdgcn_rcpf(1.f + __expf(-g)); }
 template <> __device__ __forceinline__ float sigmoid<float>(float g) { return 1.f / (1.f + expf(-g)); }
 
-// One operand of a step: ROWS rows of m (or n) times KB = 64 or 128 bytes of k,
+// One operand of a stage: ROWS rows of m (or n) times 128 bytes of k, a whole line,
 // in 16-byte chunks that the 64 lanes of a load put into consecutive places.
 //
 // k contiguous: LDS row = one row's chunks, chunk c at place c ^ key(row), so
@@ -144,18 +144,19 @@ template <> __device__ __forceinline__ float sigmoid<float>(float g) { return 1.
 // m contiguous: LDS row = one k with ROWS elements; the piece c of 16 elements
 // lies at place c ^ key(k), so that the k of a transposed read do.
 // (No bank conflicts counted for either.)
-template <typename T, bool TR, int ROWS, int KB> struct Operand {
+template <typename T, bool TR, int ROWS> struct Operand {
+  static constexpr int KB = 128;
   static constexpr int EPC = 16 / (int)sizeof(T);        // elements of a chunk
-  static constexpr int BK = KB / (int)sizeof(T);         // k of a step
+  static constexpr int BK = KB / (int)sizeof(T);         // k of a stage
   static constexpr int BYTES = ROWS * KB;
   static constexpr int CPP = 16 / EPC;                   // chunks of a 16-element piece
   static constexpr int CPR = TR ? ROWS / EPC : KB / 16;  // chunks of an LDS row
   static __device__ __forceinline__ int key(int line) {
-    if constexpr (!TR) return KB == 64 ? (line >> 1) & 3 : line & 7;
+    if constexpr (!TR) return line & 7;
     const int x = sizeof(T) == 2 ? (line & 3) | ((line >> 3) & 3) << 2 : (line >> 2) & 3;
     return x & (ROWS / 16 - 1);
   }
-  // source of chunk q: row (relative to the tile) or k of the step, and the element of it
+  // source of chunk q: row (relative to the tile) or k of the stage, and the element of it
   static __device__ __forceinline__ void place(int q, int& line, int& elem) {
     line = q / CPR;
     const int c = q % CPR;
@@ -164,16 +165,16 @@ template <typename T, bool TR, int ROWS, int KB> struct Operand {
   }
 };
 
-// Fragment of 16 rows (m) from row r0 and 64 bytes of k, the h-th of the step.
-template <typename T, bool TR, int ROWS, int KB> struct Frag;
-template <bool TR, int ROWS, int KB> struct Frag<bf16, TR, ROWS, KB> {
+// Fragment of 16 rows (m) from row r0 and 64 bytes of k, the h-th half of the stage.
+template <typename T, bool TR, int ROWS> struct Frag;
+template <bool TR, int ROWS> struct Frag<bf16, TR, ROWS> {
   bf16x8 v;  // k = 32 h + 8 (lane / 16) + 0..7
   static __device__ __forceinline__ Frag load(const char* s, int r0, int h, int lane) {
-    using O = Operand<bf16, TR, ROWS, KB>;
+    using O = Operand<bf16, TR, ROWS>;
     Frag f;
     const int g = lane >> 4, i = lane & 15;
     if constexpr (!TR) {
-      f.v = *reinterpret_cast<const bf16x8*>(s + (r0 + i) * KB + (((h * 4 + g) ^ O::key(i)) << 4));
+      f.v = *reinterpret_cast<const bf16x8*>(s + (r0 + i) * O::KB + (((h * 4 + g) ^ O::key(i)) << 4));
     } else {
       // a group of 16 lanes reads 4 k x 16 m, lane i receives the 4 k of m = i
       const int k = g * 8 + (i >> 2);
@@ -186,14 +187,14 @@ template <bool TR, int ROWS, int KB> struct Frag<bf16, TR, ROWS, KB> {
     return f;
   }
 };
-template <bool TR, int ROWS, int KB> struct Frag<float, TR, ROWS, KB> {
+template <bool TR, int ROWS> struct Frag<float, TR, ROWS> {
   float v[4];  // k = 16 h + 4 (lane / 16) + j for the j-th instruction
   static __device__ __forceinline__ Frag load(const char* s, int r0, int h, int lane) {
-    using O = Operand<float, TR, ROWS, KB>;
+    using O = Operand<float, TR, ROWS>;
     Frag f;
     const int g = lane >> 4, i = lane & 15;
     if constexpr (!TR) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(s + (r0 + i) * KB + (((h * 4 + g) ^ O::key(i)) << 4));
+      const f32x4 x = *reinterpret_cast<const f32x4*>(s + (r0 + i) * O::KB + (((h * 4 + g) ^ O::key(i)) << 4));
 #pragma unroll
       for (int j = 0; j < 4; ++j) f.v[j] = x[j];
     } else {
@@ -204,8 +205,8 @@ template <bool TR, int ROWS, int KB> struct Frag<float, TR, ROWS, KB> {
     return f;
   }
 };
-template <typename T, bool TA, int RA, bool TB, int RB, int KB>
-__device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA, KB>& a, const Frag<T, TB, RB, KB>& b, f32x4 c) {
+template <typename T, bool TA, int RA, bool TB, int RB>
+__device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA>& a, const Frag<T, TB, RB>& b, f32x4 c) {
   if constexpr (sizeof(T) == 2) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
   } else {
@@ -215,11 +216,11 @@ __device__ __forceinline__ f32x4 mma(const Frag<T, TA, RA, KB>& a, const Frag<T,
   }
 }
 
-// Tile of BM x BN by WM x WN waves, KB bytes of k per step, RING steps in LDS;
-// WK groups of such waves share the tile's steps (their sums are added in LDS
-// afterwards, in a fixed order).
-template <int BM_, int BN_, int WM_, int WN_, int KB_, int RING_, int WK_> struct FShape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KB = KB_, RING = RING_, WK = WK_;
+// Tile of BM x BN by WM x WN waves, RA stages of A and RB of B in LDS; WK groups
+// of such waves share the tile's stages (their sums are added in LDS afterwards,
+// in a fixed order).
+template <int BM_, int BN_, int WM_, int WN_, int RA_, int RB_, int WK_> struct FShape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, RA = RA_, RB = RB_, WK = WK_;
   static constexpr int GTH = WM * WN * kWave, NTH = GTH * WK;
 };
 
@@ -241,31 +242,31 @@ struct Tiles {
 };
 
 template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct Tile {
-  static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::GTH, KB = SH::KB, RING = SH::RING, WK = SH::WK;
+  static constexpr int BM = SH::BM, BN = SH::BN, NTH = SH::GTH, RA = SH::RA, RB = SH::RB, WK = SH::WK;
   static constexpr int MT = BM / SH::WM / 16, NT = BN / SH::WN / 16;
-  using OA = Operand<T, TA, BM, KB>;
-  using OB = Operand<T, TB, BN, KB>;
-  using FA = Frag<T, TA, BM, KB>;
-  using FB = Frag<T, TB, BN, KB>;
-  static constexpr int BK = OA::BK, STEP = OA::BYTES + OB::BYTES;
-  static constexpr int ACH = OA::BYTES / 16 / NTH, BCH = OB::BYTES / 16 / NTH, LPT = ACH + BCH;
+  using OA = Operand<T, TA, BM>;
+  using OB = Operand<T, TB, BN>;
+  using FA = Frag<T, TA, BM>;
+  using FB = Frag<T, TB, BN>;
+  static constexpr int BK = OA::BK, ALL = RA * OA::BYTES + RB * OB::BYTES;
+  static constexpr int ACH = OA::BYTES / 16 / NTH, BCH = OB::BYTES / 16 / NTH;
   static constexpr int TN = EK == E_SWIGLU ? BN / 2 : BN;  // columns of N that a tile covers
   static_assert(OA::BYTES % (16 * NTH) == 0 && OB::BYTES % (16 * NTH) == 0, "chunks");
   static_assert(NT % 2 == 0 && (EK != E_SWIGLU || (NT % 4 == 0 && !TB)), "pairs of columns, of gate and of up");
-  static constexpr int LDS = WK * RING * STEP;
+  static constexpr int LDS = WK * ALL;
   static_assert((WK - 1) * BM * BN * 4 <= LDS && LDS <= 160 * 1024, "LDS");
 
-  // Steps [first, last) of the tile at (m0, n0); the sums go to the epilogue, or
+  // Stages [first, last) of the tile at (m0, n0); the sums go to the epilogue, or
   // (SPLIT) to `part` as they are.
   static __device__ __forceinline__ void run(const FArgs& g, int m0, int n0, int first, int last, float* part, char* lds0) {
     const int grp = WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NTH);
     const int tid = threadIdx.x - grp * NTH, lane = tid & 63, wave = tid >> 6, wm = wave / SH::WN, wn = wave % SH::WN;
     const int wbase = __builtin_amdgcn_readfirstlane(tid & ~(kWave - 1));
-    char* lds = lds0 + grp * (RING * STEP);
-    // this group's steps [k0, k1); all groups go through `turns` of them
+    char* lds = lds0 + grp * ALL;  // RA places of A, then RB of B
+    // this group's stages [k0, k1); all groups go through `turns` of them
     const int turns_n = (last - first + WK - 1) / WK, k0 = min(first + grp * turns_n, last), k1 = min(k0 + turns_n, last);
 
-    // byte offsets of this thread's chunks from the step's first element; rows
+    // byte offsets of this thread's chunks from the stage's first element; rows
     // and columns past the matrix read the last one (their results are not stored)
     unsigned ao[ACH], bo[BCH];
 #pragma unroll
@@ -290,42 +291,50 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
     }
     const char* ab = reinterpret_cast<const char*>(g.A) + (TA ? 0 : m0 * g.lda * (int64_t)sizeof(T));
     const char* bb = reinterpret_cast<const char*>(g.B) + (TB ? 0 : n0 * g.ldb * (int64_t)sizeof(T));
-    const int64_t astep = TA ? BK * g.lda * (int64_t)sizeof(T) : KB, bstep = TB ? BK * g.ldb * (int64_t)sizeof(T) : KB;
+    const int64_t astep = TA ? BK * g.lda * (int64_t)sizeof(T) : OA::KB, bstep = TB ? BK * g.ldb * (int64_t)sizeof(T) : OB::KB;
     const unsigned lbase = lds_offset(lds);
 
-    // chunks [c0, c1) of A's and B's of step kt into place `slot` of the ring
-    auto issue = [&](int kt, int slot, int c0, int c1) __attribute__((always_inline)) {
-      const char* as = ab + kt * astep;
-      const char* bs = bb + kt * bstep;
-      const unsigned s = lbase + slot * STEP;
-#pragma unroll
-      for (int c = 0; c < LPT; ++c) {
-        if (c < c0 || c >= c1) continue;
-        if (c < ACH) stage16(as, ao[c], s + (c * NTH + wbase) * 16);
-        else stage16(bs, bo[c - ACH], s + OA::BYTES + ((c - ACH) * NTH + wbase) * 16);
-      }
+    // chunk c of A's of stage kt into place `slot`, and of B's
+    auto load_a = [&](int kt, int slot, int c) __attribute__((always_inline)) {
+      stage16(ab + kt * astep, ao[c], lbase + slot * OA::BYTES + (c * NTH + wbase) * 16);
     };
-    // any step, the short last one of a sum over rows too (k past the end are zeros)
+    auto load_b = [&](int kt, int slot, int c) __attribute__((always_inline)) {
+      stage16(bb + kt * bstep, bo[c], lbase + RA * OA::BYTES + slot * OB::BYTES + (c * NTH + wbase) * 16);
+    };
+    // any stage, the short last one of a sum over rows too: k past the end are
+    // zeros, and none of its loads is left (the waits below count loads)
     const int kfull = TA && TB ? min(k1, g.K / BK) : k1;
-    auto issue_any = [&](int kt, int slot) __attribute__((always_inline)) {
-      if ((TA && TB) && kt >= kfull) {
+    auto any_a = [&](int kt, int slot) __attribute__((always_inline)) {
 #pragma unroll
-        for (int c = 0; c < LPT; ++c) {
-          const bool isa = c < ACH;
-          const int q = tid + (isa ? c : c - ACH) * NTH;
+      for (int c = 0; c < ACH; ++c) {
+        if ((TA && TB) && kt >= kfull) {
+          const int q = tid + c * NTH;
           int line, e;
-          if (isa) OA::place(q, line, e);
-          else OB::place(q, line, e);
+          OA::place(q, line, e);
           uint4 v = make_uint4(0, 0, 0, 0);
-          if (kt * BK + line < g.K)
-            v = *reinterpret_cast<const uint4*>(isa ? ab + kt * astep + ao[c] : bb + kt * bstep + bo[c - ACH]);
-          *reinterpret_cast<uint4*>(lds + slot * STEP + (isa ? 0 : OA::BYTES) + q * 16) = v;
+          if (kt * BK + line < g.K) v = *reinterpret_cast<const uint4*>(ab + kt * astep + ao[c]);
+          *reinterpret_cast<uint4*>(lds + slot * OA::BYTES + q * 16) = v;
+        } else {
+          load_a(kt, slot, c);
         }
-        // the waits below count loads: of this step there are none left
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      } else {
-        issue(kt, slot, 0, LPT);
       }
+      if ((TA && TB) && kt >= kfull) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    auto any_b = [&](int kt, int slot) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < BCH; ++c) {
+        if ((TA && TB) && kt >= kfull) {
+          const int q = tid + c * NTH;
+          int line, e;
+          OB::place(q, line, e);
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (kt * BK + line < g.K) v = *reinterpret_cast<const uint4*>(bb + kt * bstep + bo[c]);
+          *reinterpret_cast<uint4*>(lds + RA * OA::BYTES + slot * OB::BYTES + q * 16) = v;
+        } else {
+          load_b(kt, slot, c);
+        }
+      }
+      if ((TA && TB) && kt >= kfull) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
 
     f32x4 acc[MT][NT];
@@ -338,12 +347,11 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
       if constexpr (EK == E_SWIGLU) return (j < NT / 2 ? 0 : TN) + wn * (TN / SH::WN) + (j % (NT / 2)) * 16;
       else return wn * (BN / SH::WN) + j * 16;
     };
-    auto fetch = [&](FA (&a)[MT], FB (&b)[NT], int slot, int h) __attribute__((always_inline)) {
-      const char* s = lds + slot * STEP;
+    auto fetch = [&](FA (&a)[MT], FB (&b)[NT], int sa, int sb, int h) __attribute__((always_inline)) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) b[j] = FB::load(s + OA::BYTES, bcol(j), h, lane);
+      for (int j = 0; j < NT; ++j) b[j] = FB::load(lds + RA * OA::BYTES + sb * OB::BYTES, bcol(j), h, lane);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[i] = FA::load(s, wm * (BM / SH::WM) + i * 16, h, lane);
+      for (int i = 0; i < MT; ++i) a[i] = FA::load(lds + sa * OA::BYTES, wm * (BM / SH::WM) + i * 16, h, lane);
     };
     // B is the instruction's first operand, so that a lane holds four consecutive columns of one row
     auto multiply = [&](FA (&a)[MT], FB (&b)[NT], int i) __attribute__((always_inline)) {
@@ -352,103 +360,134 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
     };
 
     if (first < last) {
-      if constexpr (KB == 64) {
-        // A ring of five steps, loaded two at a time: a row's 128-byte line is then
-        // fetched by neighbouring loads.  Two waves on each SIMD take turns: while
-        // one multiplies a step, the other reads the fragments of its next one, then
-        // they change places at a barrier (waves 4 to 7 start one barrier later).
-        // When either multiplies step k, both have read k - 1, so every other step
-        // loads k + 3 and k + 4 between its products.  When the early waves have
-        // multiplied step k and the late ones have read it, everyone waits for its
-        // own loads of k + 1.
-        static_assert(NTH == 512 && WK == 1 && RING == 5 && MT == 2 * LPT, "loads between the products");
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k0 + k < k1) issue_any(k0 + k, k);
-        if (k0 + 3 < k1) wait_barrier<2 * LPT>();
-        else wait_barrier<0>();
-        auto slot_of = [](int s) __attribute__((always_inline)) { return s >= 5 ? s - 5 : s; };
+      if constexpr (NTH == 512) {
+        // Three stages of A in LDS and two of B.  Two waves on each SIMD take turns:
+        // while one multiplies half a stage, the other reads the fragments of its
+        // next half, then they change places at a barrier (waves 4 to 7 start one
+        // barrier later).  When the late waves have read the last half of stage k,
+        // its places are free for B of k + 2 and A of k + 3: the late waves load them
+        // between the products of that half, the early ones, whose turn it is to
+        // read, between those of their next.  A stage's loads of B have three to four
+        // turns to arrive, those of A seven to eight: the weights are in L2, the rows
+        // come from memory.  At the last turn before stage k + 1 everyone waits for
+        // its own loads of it, which leaves those of A of k + 2.
+        static_assert(WK == 1 && RA == 3 && RB == 2 && MT == ACH + BCH, "loads between the products");
+        const bool is_late = wbase >= 256;
+        any_a(k0, 0);
+        any_b(k0, 0);
+        if (k0 + 1 < k1) any_a(k0 + 1, 1);
+        if (is_late && k0 + 1 < k1) any_b(k0 + 1, 1);
+        if (is_late && k0 + 2 < k1) any_a(k0 + 2, 2);
+        if (k0 + 2 >= kfull) wait_barrier<0>();
+        else if (is_late) wait_barrier<2 * ACH + BCH>();
+        else wait_barrier<ACH>();
         auto turns = [&](auto late_) __attribute__((always_inline)) {
           constexpr bool late = decltype(late_)::value;
           FA a[MT];
           FB b[NT];
           if (late) wait_reads();
-          int kt = k0, s = 0;
-          for (; kt + 5 < kfull; kt += 2) {
-            fetch(a, b, s, 0);
-            if (late) wait_barrier<2 * LPT>();
-            else wait_reads();
+          int kt = k0, sa = 0, sb = 0;
+          auto next3 = [](int s) __attribute__((always_inline)) { return s == 2 ? 0 : s + 1; };
+          // one stage; its loads are of B of kb and A of kb + 1, both whole
+          for (; kt + (late ? 3 : 2) < kfull; ++kt) {
+            const int sp = sa == 0 ? 2 : sa - 1;  // A of kt - 1, and of kt + 2
+            fetch(a, b, sa, sb, 0);
+            wait_reads();
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int i = 0; i < MT; ++i) multiply(a, b, i);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (late) wait_reads();
-            else wait_barrier<2 * LPT>();
-            __builtin_amdgcn_sched_barrier(0);
-            fetch(a, b, slot_of(s + 1), 0);
-            if (late) wait_barrier<0>();
-            else wait_reads();
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            const int s4 = slot_of(s + 4);
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
               multiply(a, b, i);
-              issue(kt + 4 + (i & 1), i & 1 ? s : s4, i / 2, i / 2 + 1);
+              if (!late && i < BCH) load_b(kt + 1, sb ^ 1, i);
+              else if (!late) load_a(kt + 2, sp, i - BCH);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(a, b, sa, sb, 1);
+            if (late) wait_barrier<ACH>();
+            else wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              multiply(a, b, i);
+              if (late && i < BCH) load_b(kt + 2, sb, i);
+              else if (late) load_a(kt + 3, sa, i - BCH);
             }
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
             if (late) wait_reads();
-            else wait_barrier<2 * LPT>();
+            else wait_barrier<ACH>();
             __builtin_amdgcn_sched_barrier(0);
-            s = slot_of(s + 2);
+            sa = next3(sa);
+            sb ^= 1;
           }
           for (; kt < k1; ++kt) {
-            fetch(a, b, s, 0);
+            const int sp = sa == 0 ? 2 : sa - 1;
+            fetch(a, b, sa, sb, 0);
+            wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (!late && kt + 1 < k1) any_b(kt + 1, sb ^ 1);
+            if (!late && kt + 2 < k1) any_a(kt + 2, sp);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) multiply(a, b, i);
+            __builtin_amdgcn_sched_barrier(0);
+            wait_reads();
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(a, b, sa, sb, 1);
             if (late) wait_barrier<0>();
             else wait_reads();
             __builtin_amdgcn_sched_barrier(0);
-            if (kt + 4 < k1) issue_any(kt + 4, slot_of(s + 4));
+            if (late && kt + 2 < k1) any_b(kt + 2, sb);
+            if (late && kt + 3 < k1) any_a(kt + 3, sa);
 #pragma unroll
             for (int i = 0; i < MT; ++i) multiply(a, b, i);
             __builtin_amdgcn_sched_barrier(0);
             if (late) wait_reads();
             else wait_barrier<0>();
             __builtin_amdgcn_sched_barrier(0);
-            s = slot_of(s + 1);
+            sa = next3(sa);
+            sb ^= 1;
           }
           if (!late) wait_reads();
         };
-        if (wbase >= 256) turns(std::true_type{});
+        if (is_late) turns(std::true_type{});
         else turns(std::false_type{});
       } else {
-        // Two sets of fragments: while half a step is multiplied, the next half's
+        // Two sets of fragments: while half a stage is multiplied, the next half's
         // fragments are read.  The barrier in the middle ends every wave's reads of
-        // step kt and every wave's loads of kt + 1; kt + RING then goes where kt was.
-        static_assert(KB == 128, "two halves");
+        // stage kt and every wave's loads of kt + 1; kt + RA then goes where kt was.
+        static_assert(RA == RB, "one ring");
+        constexpr int LPT = ACH + BCH;
         FA a0[MT], a1[MT];
         FB b0[NT], b1[NT];
 #pragma unroll
-        for (int k = 0; k < RING; ++k)
-          if (k0 + k < k1) issue_any(k0 + k, k);
-        if (k0 + RING - 1 < kfull) wait_barrier<(RING - 1) * LPT>();
+        for (int k = 0; k < RA; ++k)
+          if (k0 + k < k1) {
+            any_a(k0 + k, k);
+            any_b(k0 + k, k);
+          }
+        if (k0 + RA - 1 < kfull) wait_barrier<(RA - 1) * LPT>();
         else wait_barrier<0>();
-        if (WK == 1 || k0 < k1) fetch(a0, b0, 0, 0);
+        if (WK == 1 || k0 < k1) fetch(a0, b0, 0, 0, 0);
         int st = 0;
         for (int it = 0; it < turns_n; ++it) {
-          const int kt = k0 + it, sn = st + 1 == RING ? 0 : st + 1;
+          const int kt = k0 + it, sn = st + 1 == RA ? 0 : st + 1;
           const bool on = WK == 1 || kt < k1;
           if (on) {
-            fetch(a1, b1, st, 1);
+            fetch(a1, b1, st, st, 1);
 #pragma unroll
             for (int i = 0; i < MT; ++i) multiply(a0, b0, i);
           }
-          if (RING > 2 && kt + RING - 1 < kfull) wait_barrier<(RING - 2) * LPT>();
+          if (RA > 2 && kt + RA - 1 < kfull) wait_barrier<(RA - 2) * LPT>();
           else wait_barrier<0>();
-          if (kt + RING < k1) issue_any(kt + RING, st);
-          if (kt + 1 < k1) fetch(a0, b0, sn, 0);
+          if (kt + RA < k1) {
+            any_a(kt + RA, st);
+            any_b(kt + RA, st);
+          }
+          if (kt + 1 < k1) fetch(a0, b0, sn, sn, 0);
           if (on) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) multiply(a1, b1, i);
@@ -580,10 +619,10 @@ template <typename T, typename SH> __global__ __launch_bounds__(256) void k_ffn_
   if (m < g.M && n < g.N) Vec4<T>::store(reinterpret_cast<T*>(g.out) + m * g.ldo + n, c);
 }
 
-using Big = FShape<256, 256, 2, 4, 64, 5, 1>;
-using Mid = FShape<128, 128, 2, 2, 128, 2, 1>;
-using Small = FShape<64, 64, 4, 1, 128, 3, 1>;
-using Deep = FShape<64, 64, 4, 1, 128, 2, 4>;
+using Big = FShape<256, 256, 2, 4, 3, 2, 1>;
+using Mid = FShape<128, 128, 2, 2, 2, 2, 1>;
+using Small = FShape<64, 64, 4, 1, 3, 3, 1>;
+using Deep = FShape<64, 64, 4, 1, 2, 2, 4>;
 
 template <typename T, bool TA, bool TB, int EK, typename SH> hipError_t launch_shape(const FArgs& g, hipStream_t s) {
   constexpr int TN = EK == E_SWIGLU ? SH::BN / 2 : SH::BN;
