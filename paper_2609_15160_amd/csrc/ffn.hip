@@ -26,6 +26,7 @@ namespace tlf {
 
 namespace {
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -88,7 +89,8 @@ __device__ __forceinline__ float unkept16(unsigned c) {
 }
 // They lie as the lanes of a 16 x 16 accumulator hold them, [row / 16][f / 16]
 // [lane][4 q, 4 p], so that a wave reads and writes whole lines (row by row it
-// moved 8 bytes per lane in 32-byte pieces).
+// moved 8 bytes per lane in 32-byte pieces), past the caches, which keep a and
+// the weights instead (16384 x 1024 x 2816: gate/up 224 -> 217 us, down 88 -> 83).
 template <typename T> struct Kept;
 template <> struct Kept<float> {
   static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
@@ -104,13 +106,14 @@ template <> struct Kept<float> {
 };
 template <> struct Kept<bf16> {
   static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
-    const uint4 c = reinterpret_cast<const uint4*>(base)[at];
+    const u32x4 c = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + at);
     q = f32x4{unkept16(c.x), unkept16(c.x >> 16), unkept16(c.y), unkept16(c.y >> 16)};
     p = f32x4{unkept16(c.z), unkept16(c.z >> 16), unkept16(c.w), unkept16(c.w >> 16)};
   }
   static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
-    reinterpret_cast<uint4*>(base)[at] = make_uint4(kept16(q[0]) | kept16(q[1]) << 16, kept16(q[2]) | kept16(q[3]) << 16,
-                                                    kept16(p[0]) | kept16(p[1]) << 16, kept16(p[2]) | kept16(p[3]) << 16);
+    __builtin_nontemporal_store((u32x4){kept16(q[0]) | kept16(q[1]) << 16, kept16(q[2]) | kept16(q[3]) << 16,
+                                        kept16(p[0]) | kept16(p[1]) << 16, kept16(p[2]) | kept16(p[3]) << 16},
+                                reinterpret_cast<u32x4*>(base) + at);
   }
 };
 
