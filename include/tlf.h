@@ -502,11 +502,12 @@ typedef struct tlf_adamw_tensor {
 /* One AdamW step of `count` tensors (Appendix A's recipe), few launches for all:
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
  *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
- * Moments of zeros (codes and scales too) are a fresh state.  With 8 bits the
- * step uses the new moments before they are rounded; a block's scale is its
- * largest |m| / 448 or v / 57344, and a v > 0 keeps at least the smallest code
- * above zero.  A gradient that is not finite spoils the moments of its element
- * (8 bits: of its block).
+ * with eps at least FLT_MIN.  Moments of zeros (codes and scales too) are a
+ * fresh state.  With 8 bits the step uses the new moments before they are
+ * rounded; a block's scale is its largest |m| / 448 or v / 57344, and a v > 0
+ * keeps at least the smallest code above zero.  A gradient that is not finite,
+ * or whose square is none in float32, spoils the moments of its element (8 bits:
+ * of its block).
  *   h_tensors: host array, read during the call; no tensor appears twice.
  * The step counts and rates are values of the call: a captured call replays them. */
 int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,

@@ -125,7 +125,7 @@ def _adamw(lib, count=1, lr=1e-3, b1=0.9, b2=0.95, eps=1e-8, table=True, **kw):
 
 @pytest.mark.parametrize("kw", [
     dict(count=-1), dict(table=False), dict(lr=-1.0), dict(lr=math.nan), dict(lr=math.inf), dict(b1=1.0), dict(b1=-0.1),
-    dict(b2=1.0), dict(b2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=math.inf), dict(d_param=None),
+    dict(b2=1.0), dict(b2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-40), dict(eps=math.inf), dict(d_param=None),
     dict(d_grad=None), dict(d_m=None), dict(d_v=None), dict(n=-1), dict(step=0), dict(weight_decay=-0.1),
     dict(weight_decay=math.nan), dict(grad_dtype=7), dict(state_bits=16), dict(state_bits=8, d_m_scale=None),
     dict(state_bits=8, d_v_scale=None), dict(d_param=P + 2), dict(d_grad=P + 1), dict(d_m=P + 2), dict(d_copy=P + 1),
