@@ -12,6 +12,7 @@ torch stream.  The shared block between gather and scatter is the caller's.
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 import torch
@@ -242,6 +243,16 @@ def _workspace(fn, *args, device):
     return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
 
 
+def _first_order(backward):
+    """once_differentiable, without its cost (5 us) where no graph of the gradients is built."""
+    checked = torch.autograd.function.once_differentiable(backward)
+
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        return checked(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+    return run
+
+
 class _RmsNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gamma, group, eps, dtype, grad):
@@ -256,7 +267,7 @@ class _RmsNorm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x, gamma, group, rstd = ctx.saved_tensors
         rows, d = x.shape
@@ -325,7 +336,7 @@ class _Ffn(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x, w_gate_up, w_down, kept = ctx.saved_tensors
         rows, d = x.shape
