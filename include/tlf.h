@@ -427,8 +427,10 @@ int tlf_ste(const int32_t* d_depth, const float* d_score, const float* d_grad_va
  *   d_y      [rows][d] (y_dtype);
  *   d_rstd   [rows] float32, receives r (tlf_rms_norm_grad reads it), or NULL;
  *            4-byte aligned, as d_group.
- * d a multiple of 4, at most TLF_NORM_MAX_D; groups at most TLF_NORM_MAX_GROUPS. */
+ * d a multiple of 4, at most TLF_NORM_MAX_D; groups at most TLF_NORM_MAX_GROUPS,
+ * rows at most TLF_NORM_MAX_ROWS. */
 #define TLF_NORM_MAX_D 4096
+#define TLF_NORM_MAX_ROWS (1 << 30)
 #define TLF_NORM_MAX_GROUPS 16
 int tlf_rms_norm(const void* d_x, int32_t x_dtype, const float* d_gamma, const int32_t* d_group, int32_t groups,
                  int32_t rows, int32_t d, float eps, void* d_y, int32_t y_dtype, float* d_rstd, void* stream);
@@ -459,7 +461,8 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
  *   d_a           [rows][f], receives a (read by the second product);
  *   d_y           [rows][d];
  *   d_workspace   tlf_ffn_ws_bytes bytes (may be 0), used during the call only.
- * d and f multiples of 64, at most TLF_FFN_MAX_WIDTH. */
+ * d and f multiples of 64, at most TLF_FFN_MAX_WIDTH; rows times the larger of
+ * them less than 2^35. */
 #define TLF_FFN_MAX_WIDTH 16384
 static inline size_t tlf_ffn_kept_bytes(int32_t dtype, int32_t rows, int32_t f) {
   return rows <= 0 || f <= 0 ? 0
@@ -492,7 +495,7 @@ typedef struct tlf_adamw_tensor {
   void* d_v;            /* [n] second moment: float32, or e5m2 codes */
   float* d_m_scale;     /* 8 bits: [ceil(n / TLF_ADAMW_BLOCK)]; element e stands for code e times scale e / BLOCK */
   float* d_v_scale;     /* likewise */
-  int64_t n;
+  int64_t n;            /* at most 2^35 */
   int64_t step;         /* t >= 1: how many steps this tensor has had, this one included */
   double weight_decay;
   int32_t grad_dtype;   /* TLF_DTYPE_F32 or TLF_DTYPE_BF16 */

@@ -31,6 +31,7 @@ constexpr int kAdamThreads = 256;
 constexpr int kAdamUnroll = 4;
 constexpr int kAdamPer = kAdamThreads * 4 * kAdamUnroll;  // elements of a workgroup
 constexpr int kAdamTensors = 40;                          // tensors of a launch: its arguments stay below 4 KiB
+constexpr int kAdamBlocks = (1 << 24) - 1;                // of a launch, which has fewer than 2^32 threads
 constexpr int kBlock = TLF_ADAMW_BLOCK;
 static_assert(kBlock == 4 * kWave, "one wave per block of 8-bit moments");
 
@@ -264,7 +265,7 @@ int check(const tlf_adamw_tensor& t) {
   if (!aligned(t.d_param, 4) || !aligned(t.d_copy, 2) || !aligned(t.d_grad, g16 ? 2 : 4) || !aligned(t.d_m_scale, 4) ||
       !aligned(t.d_v_scale, 4) || (t.state_bits == 32 && (!aligned(t.d_m, 4) || !aligned(t.d_v, 4))))
     return TLF_E_INVALID_ARG;
-  return t.n > ((int64_t)1 << 40) ? TLF_E_UNSUPPORTED : TLF_OK;
+  return t.n > ((int64_t)1 << 35) ? TLF_E_UNSUPPORTED : TLF_OK;
 }
 
 }  // namespace
@@ -291,7 +292,7 @@ extern "C" int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, doubl
       const bool take = t && t->state_bits == bits && t->n > 0;
       const int64_t blocks = take ? (t->n + kAdamPer - 1) / kAdamPer : 0;
       // full, or done
-      if (a.count > 0 && (!t || (take && (a.count == kAdamTensors || a.first[a.count] + blocks > INT32_MAX)))) {
+      if (a.count > 0 && (!t || (take && (a.count == kAdamTensors || a.first[a.count] + blocks > kAdamBlocks)))) {
         if (bits == 32) hipLaunchKernelGGL(k_adamw, dim3(a.first[a.count]), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
         else hipLaunchKernelGGL(k_adamw8, dim3(a.first[a.count]), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
         if (hipGetLastError() != hipSuccess) return TLF_E_HIP;

@@ -671,6 +671,9 @@ int check(int32_t dtype, int32_t rows, int32_t d, int32_t f) {
   return TLF_OK;
 }
 
+// Up to this many elements every launch has fewer than 2^32 threads.
+bool launchable(int32_t rows, int32_t d, int32_t f) { return rows * (int64_t)(d > f ? d : f) < (int64_t)1 << 35; }
+
 // How a product that is only stored is computed.
 enum { P_SMALL = 0, P_MID = 1, P_BIG = 2, P_DEEP = 3 };
 struct Plan {
@@ -833,6 +836,7 @@ int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int3
   const int st = tlf_ffn_ws_bytes(dtype, rows, d, f, &need);
   if (st != TLF_OK) return st;
   if (rows == 0) return TLF_OK;
+  if (!tlf::launchable(rows, d, f)) return TLF_E_UNSUPPORTED;
   if (!d_x || !d_w_gate_up || !d_w_down || !d_a || !d_y) return TLF_E_INVALID_ARG;
   if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
   for (const void* p : {d_x, d_w_gate_up, d_w_down, (const void*)d_kept, (const void*)d_a, (const void*)d_y,
@@ -865,6 +869,7 @@ int tlf_ffn_grad(const void* d_dy, const void* d_x, const void* d_w_gate_up, con
   if (st != TLF_OK) return st;
   if (!d_dx && !d_dw_gate_up && !d_dw_down) return TLF_OK;
   if (rows > 0) {
+    if (!tlf::launchable(rows, d, f)) return TLF_E_UNSUPPORTED;
     if (!d_dy || !d_x || !d_w_gate_up || !d_w_down || !d_kept || !d_a) return TLF_E_INVALID_ARG;
     if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
   }

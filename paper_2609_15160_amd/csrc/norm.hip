@@ -264,10 +264,26 @@ bool is_dtype(int32_t t) { return t == TLF_DTYPE_F32 || t == TLF_DTYPE_BF16; }
 
 int check(int32_t x_dtype, int32_t y_dtype, int32_t groups, int32_t rows, int32_t d) {
   if (!is_dtype(x_dtype) || !is_dtype(y_dtype) || groups < 0 || rows < 0 || d <= 0 || d % 4 != 0) return TLF_E_INVALID_ARG;
-  return d > TLF_NORM_MAX_D || groups > TLF_NORM_MAX_GROUPS ? TLF_E_UNSUPPORTED : TLF_OK;
+  return d > TLF_NORM_MAX_D || groups > TLF_NORM_MAX_GROUPS || rows > TLF_NORM_MAX_ROWS ? TLF_E_UNSUPPORTED : TLF_OK;
 }
 
-template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
+constexpr int kLaunchRows = 1 << 24;  // a launch has fewer than 2^32 threads
+
+template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(NormArgs a, hipStream_t s) {
+  if (a.rows > kLaunchRows) {
+    NormArgs head = a;
+    head.rows = kLaunchRows;
+    const hipError_t e = launch_rows<TX, TY, GRAD>(head, s);
+    if (e != hipSuccess) return e;
+    const int64_t n = (int64_t)kLaunchRows * a.d;
+    a.x = reinterpret_cast<const TX*>(a.x) + n;
+    if (GRAD) a.dy = reinterpret_cast<const TY*>(a.dy) + n;
+    a.out = reinterpret_cast<char*>(a.out) + n * (GRAD ? sizeof(TX) : sizeof(TY));
+    if (a.group) a.group += kLaunchRows;
+    if (a.rstd) a.rstd += kLaunchRows;
+    a.rows -= kLaunchRows;
+    return launch_rows<TX, TY, GRAD>(a, s);
+  }
   const dim3 grid((a.rows + kNormWaves - 1) / kNormWaves), block(kNormWaves * kWave);
 #define TLF_NORM(NV)                                                                   \
   if (GRAD) hipLaunchKernelGGL((k_norm_dx<TX, TY, NV>), grid, block, 0, s, a);         \

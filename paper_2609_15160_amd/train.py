@@ -208,6 +208,10 @@ def ste(score: torch.Tensor, depth: torch.Tensor) -> torch.Tensor:
 
 # ---------------------------------------------------------------------------
 # The block's FFN half: RMSNorm, the gated FFN, and the optimizer's step
+#
+# rms_norm and ffn may be captured into a graph, their backward pass with them if
+# no graph from before the capture holds the same leaves: autograd runs a leaf's
+# gradient on the stream where the leaf was first used.
 # ---------------------------------------------------------------------------
 
 _DTYPE = {torch.float32: tlf.DTYPE_F32, torch.bfloat16: tlf.DTYPE_BF16}
@@ -229,6 +233,11 @@ def _same_device(t, *others):
     for o in others:
         if o is not None and o.device != t.device:
             raise ValueError(f"tensors on {t.device} and {o.device}: one device expected")
+
+
+def _int32(name, *tensors):
+    if any(n >= 1 << 31 for t in tensors if t is not None for n in t.shape):
+        raise ValueError(f"{name}: a dimension of 2^31 or more")
 
 
 def _wants_grad(*tensors) -> bool:
@@ -296,7 +305,7 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor = None, group: torch.Tensor = 
 
     gamma is None, one [d] or [1, d] scale, or [groups, d] scales of which row r takes number group[r] (int32 [rows];
     a row whose number is none of them takes no scale): the AdaLN modulation of each token's depth.  The result has
-    `dtype` (x's by default)."""
+    `dtype` (x's by default).  d is a multiple of 4 up to 4096, and there are 16 groups at most."""
     if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
         raise ValueError("rms_norm: expected a float32 or bfloat16 [rows, d] CUDA tensor")
     dtype = dtype or x.dtype
@@ -312,6 +321,7 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor = None, group: torch.Tensor = 
         if gamma is None or group.dtype != torch.int32 or group.shape != (x.shape[0],):
             raise ValueError("rms_norm: group is int32 [rows] and goes with gamma")
         group = group.contiguous()
+    _int32("rms_norm", x, gamma)
     _same_device(x, gamma, group)
     return _RmsNorm.apply(_aligned(x), None if gamma is None else _aligned(gamma), group, float(eps), dtype,
                           _wants_grad(x, gamma))
@@ -365,6 +375,7 @@ def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch
                          "expected [rows, d], [2f, d], [d, f]")
     if w_gate_up.dtype != x.dtype or w_down.dtype != x.dtype:
         raise ValueError("ffn: x and the weights are of one dtype")
+    _int32("ffn", x, w_gate_up)
     _same_device(x, w_gate_up, w_down)
     return _Ffn.apply(_aligned(x), _aligned(w_gate_up), _aligned(w_down), _wants_grad(x, w_gate_up, w_down))
 
@@ -403,7 +414,7 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
     if n == 0:
         return
     table = (tlf.AdamwTensor * n)()
-    dev = params[0].device
+    dev, updated = params[0].device, set()
     for k, (p, g, c) in enumerate(zip(params, grads, copies)):
         if p.dtype != torch.float32 or not p.is_cuda or not p.is_contiguous():
             raise ValueError("adamw_: parameters are contiguous float32 CUDA tensors")
@@ -419,10 +430,13 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
         for t in (p, g, c, m, v, ms, vs):
             if t is not None and t.device != dev:
                 raise ValueError("adamw_: tensors on one device expected")
-        table[k] = tlf.AdamwTensor(p.data_ptr(), c.data_ptr() if c is not None else None, g.data_ptr(), m.data_ptr(),
-                                   v.data_ptr(), ms.data_ptr() if ms is not None else None,
+        at = p.data_ptr(), m.data_ptr(), v.data_ptr()
+        updated.update(at if p.numel() else ())
+        table[k] = tlf.AdamwTensor(at[0], c.data_ptr() if c is not None else None, g.data_ptr(), at[1], at[2], ms.data_ptr() if ms is not None else None,
                                    vs.data_ptr() if vs is not None else None, p.numel(), steps[k], decays[k],
                                    _DTYPE[g.dtype], 32 if ms is None else 8)
+    if len(updated) != sum(3 for p in params if p.numel()):
+        raise ValueError("adamw_: a parameter or moment appears twice")
     with torch.cuda.device(dev):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("adamw_: the step number and rates are values and cannot be captured into a graph")

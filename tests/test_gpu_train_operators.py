@@ -645,3 +645,91 @@ def test_adamw_eight_bit_ties():
         codes, scales = O.encode(new, which)
         assert np.array_equal(got[1].cpu().numpy(), scales), which
         assert torch.equal(got[0].cpu().view(torch.uint8), codes.view(torch.uint8)), which
+
+
+@pytest.mark.parametrize("scaled", [False, True])
+def test_norm_of_more_rows_than_a_launch(scaled):
+    """2^26 + 5 rows of 4, past the rows of one launch.  The expected values are float64 of the same bfloat16 inputs,
+    rounded to bfloat16 by the comparison: half a step, 2^-8, and 2^-16 for the kernel's float32 arithmetic (a chain of
+    about ten roundings of 2^-24, amplified at most tenfold where dx's two terms cancel, held against the row's largest
+    |h| r)."""
+    train = _train()
+    n, d = 2 ** 26 + 5, 4
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randn(n, d, generator=gen, device="cuda", dtype=torch.bfloat16).requires_grad_()
+    dy = torch.randn(n, d, generator=gen, device="cuda", dtype=torch.bfloat16)
+    gamma = torch.tensor([[0.5, -0.25, 0.0, 1.0], [-0.5, 0.75, 0.125, 2.0]], device="cuda").requires_grad_() if scaled else None
+    group = torch.randint(0, 3, (n,), generator=gen, device="cuda", dtype=torch.int32) if scaled else None  # 2: none
+    _say("norm", n, d, scaled)
+    y = train.rms_norm(x, gamma, group)
+    got = torch.autograd.grad(y, [x] + ([gamma] if scaled else []), dy)
+    at = torch.cat([torch.arange(0, n, 1009, device="cuda")] +
+                   [torch.arange(k * 2 ** 24 - 3, k * 2 ** 24 + 3, device="cuda") for k in (1, 2, 3, 4)] +
+                   [torch.arange(n - 9, n, device="cuda")]).clamp(max=n - 1)
+    xs, gs = x.detach()[at].double(), dy[at].double()
+    gain = 1.0
+    if scaled:
+        gain = torch.cat([1.0 + gamma.detach().double(), torch.ones(1, d, device="cuda", dtype=torch.float64)])[group[at].long()]
+    r = (xs.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    h = gs * gain
+    want = xs * r * gain
+    dx = r * (h - xs * r * r * (h * xs).mean(1, keepdim=True))
+    assert ((y.detach()[at].double() - want).abs() <= want.abs() * (2 ** -8 + 2 ** -16)).all()
+    assert ((got[0][at].double() - dx).abs() <= dx.abs() * (2 ** -8 + 2 ** -16) +
+            2 ** -16 * (r * h.abs().amax(1, keepdim=True))).all()
+    if scaled:
+        # float32 sums of n products: each workgroup's run of rows adds one rounding per row to the sum of |terms| at
+        # worst, of which 2^14 rows make 2^14 2^-24; rounding errors' signs are mixed, so this is a wide bound
+        xr = x.detach().double()
+        xr *= (xr.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+        xr *= dy
+        for k in (0, 1):
+            one = xr * (group == k)[:, None]
+            bound = one.abs().sum(0) * (2 ** 14 + 512) * 2 ** -24
+            assert ((got[1][k].double() - one.sum(0)).abs() <= bound).all()
+
+
+def test_adamw_refuses_a_tensor_given_twice():
+    train = _train()
+    p, q, g, m, v, m2 = (torch.zeros(64, device="cuda") for _ in range(6))
+    with pytest.raises(ValueError, match="twice"):
+        train.adamw_([p, p], [g, g], [m, m2], [v, q], 1, lr=1e-3)
+    with pytest.raises(ValueError, match="twice"):
+        train.adamw_([p, q], [g, g], [m, m], [v, m2], 1, lr=1e-3)
+    assert not any(t.any() for t in (p, q, m, v, m2))
+    empty = torch.zeros(0, device="cuda")
+    train.adamw_([empty, empty], [empty, empty], [empty, empty], [empty, empty], 1, lr=1e-3)
+
+
+def test_forward_and_backward_captured_together():
+    """The operators and their gradients recorded into a graph by leaves that no other graph holds, replayed with new
+    contents between eager calls on tensors of their own: the same to the bit."""
+    train = _train()
+    n, d, f = 200, 256, 320
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    new = lambda *s, scale=1.0, t=torch.float32: (torch.randn(*s, generator=gen, device="cuda") * scale).to(t)  # noqa: E731
+    make = lambda: [new(n, d), new(4, d, scale=0.3), new(2 * f, d, scale=0.1, t=torch.bfloat16),  # noqa: E731
+                    new(d, f, scale=0.1, t=torch.bfloat16), new(n, d, t=torch.bfloat16)]
+    group = torch.randint(0, 4, (n,), generator=gen, device="cuda", dtype=torch.int32)
+
+    def step(x, gamma, wgu, wd, dy):
+        y = train.ffn(train.rms_norm(x, gamma, group, dtype=torch.bfloat16), wgu, wd)
+        return [y.detach(), *torch.autograd.grad(y, (x, gamma, wgu, wd), dy)]
+
+    leaves = lambda ts: [t.clone().requires_grad_() for t in ts[:4]] + [ts[4].clone()]  # noqa: E731
+    sets = [make() for _ in range(4)]
+    want = [[t.clone() for t in step(*leaves(s))] for s in sets]
+    held = leaves(sets[0])
+    _say("capture", n, d, f)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(*held)
+    for k in (1, 2, 3, 0):
+        with torch.no_grad():
+            for t, s in zip(held, sets[k]):
+                t.copy_(s)
+        graph.replay()
+        step(*leaves(sets[(k + 1) % 4]))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[k])), k

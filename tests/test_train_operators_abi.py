@@ -165,3 +165,27 @@ def test_wrappers_refuse_host_tensors_and_wrong_shapes():
     with pytest.raises(ValueError):
         train.AdamW([x.requires_grad_()], lr=1e-3)
     train.adamw_([], [], [], [], 1, lr=1e-3)
+
+
+@pytest.mark.parametrize("rows", [2 ** 30 + 1, 2 ** 31 - 1])
+def test_rms_norm_refuses_more_rows_than_it_counts(lib, rows):
+    n = ctypes.c_size_t()
+    assert _norm(lib, rows=rows) == UNS
+    assert _norm_grad(lib, rows=rows) == UNS
+    assert lib.tlf_rms_norm_grad_ws_bytes(2, rows, 8, ctypes.byref(n)) == UNS
+
+
+@pytest.mark.parametrize("rows,d,f", [(2 ** 31 - 1, 64, 64), (2 ** 29, 64, 64), (2 ** 21, 64, 16384), (2 ** 21, 16384, 64)])
+def test_ffn_refuses_more_elements_than_a_launch_covers(lib, rows, d, f):
+    assert _ffn(lib, rows=rows, d=d, f=f) == UNS
+    assert _ffn_grad(lib, rows=rows, d=d, f=f, n=1 << 60) == UNS
+
+
+def test_adamw_refuses_more_elements_than_a_launch_covers(lib):
+    assert _adamw(lib, n=2 ** 35 + 1) == UNS
+
+
+def test_wrappers_refuse_dimensions_past_32_bits():
+    x = torch.empty(2 ** 31, 4, device="meta")
+    with pytest.raises(ValueError, match="2\\^31"):
+        train._int32("rms_norm", None, x)
