@@ -591,7 +591,8 @@ template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch
 // Products with few tiles and a long sum, in `splits` ranges of k.  The tiles of
 // one range follow each other, so that an XCD's workgroups read the same k at a
 // time (with ranges that begin at any k, every tile's share of the same length,
-// dW_gate_up of 16384 x 1024 x 2816 took 243 us, without reuse in L2; LATER).
+// dW_gate_up of 16384 x 1024 x 2816 took 243 us where these took 205, and take 191
+// with stages of whole lines: without reuse in L2).
 template <typename T, bool TA, bool TB, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn_split(FArgs g) {
   using TL = Tile<T, TA, TB, E_STORE, SH, true>;
   __shared__ __align__(16) char lds[TL::LDS];
@@ -648,10 +649,11 @@ bool big_fits(int64_t tiles) {
 
 // The fused products: Big where it fits, Mid from 300 tiles of its size, else
 // Small.  bf16, us with Small, Mid and Big, gate/up with the product down
-// behind it and da with dx: 1000 x 768 x 2048 29, 29, 42 and 36, 43, 56; 1000 x
-// 2048 x 5504 113, 102, 97 and 144, 127, 138; 8191 x 2048 x 5504 874, 751, 684
-// and 1020, 947, 909.  float32 is bound by its matrix instructions and takes
-// Small (1000 x 256 x 512: 24 and 36, Mid 36 and 51).
+// behind it and da with dx: 333 x 768 x 2048 19, 25, 37 and 29, 38, 53; 1000 x
+// 768 x 2048 27, 27, 38 and 31, 39, 54; 4096 x 1024 x 2816 109, 101, 102 and 131,
+// 131, 125; 8191 x 2048 x 5504 624, 555, 468 and 606, 539, 490.  float32 is bound
+// by its matrix instructions and takes Small (1000 x 256 x 512: 24 and 36, Mid 36
+// and 51).
 template <typename T, bool TA, bool TB, int EK> hipError_t launch_fused(const FArgs& g, hipStream_t s) {
   if constexpr (sizeof(T) == 2) {
     const int64_t n = EK == E_SWIGLU ? 2 * (int64_t)g.N : g.N;
@@ -690,14 +692,18 @@ Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
 }
 
 // y and dx, m rows, n columns, `stages` of 128 bytes of k.  Large tiles where
-// they fill the device; 64 x 64 by four waves from 400 tiles on, by 16 waves,
-// which share the sum, below; and where 64 of them or fewer have a long sum, that
-// is split until every compute unit has a share.  us of the forward pass with
-// Small, Deep and Small split: 1 x 2048 x 5504 43, 32, 25; 333 x 768 x 2048 22,
-// 20, 24; 1000 x 768 x 2048 30, 26, 33; 2000 x 1024 x 2816 60, 64, 60.
+// they fill the device: us of da with dx with Small, Mid and Big 3001 x 1024 x
+// 2816 (192 tiles of 128 x 128) 106, 111, 160; 3580 x 1024 x 2816 (224) 128, 112,
+// 160; 4400 x 1024 x 2816 (280) 135, 133, 158; 2000 x 2048 x 5504 (256) 225, 191,
+// 278; 8191 x 2048 x 5504 890, 597, 486.  Below, 64 x 64 by four waves from 400
+// tiles on and by 16 waves, which share the sum, under that; and where 64 of them
+// or fewer have a long sum, that is split until every compute unit has a share.
+// us of the forward pass with Small, Deep and Small split: 1 x 2048 x 5504 42, 32,
+// 22; 333 x 768 x 2048 22, 19, 21; 1000 x 768 x 2048 29, 26, 33; 2000 x 1024 x 2816
+// 53, 59, 60.
 Plan store_plan(bool half, int64_t m, int64_t n, int64_t stages) {
   if (half && big_fits(tiles_of(m, n, 256))) return plan_of(P_BIG, m, n, 1);
-  if (half && tiles_of(m, n, 128) >= 300) return plan_of(P_MID, m, n, 1);
+  if (half && tiles_of(m, n, 128) >= 208) return plan_of(P_MID, m, n, 1);
   const int64_t tiles = tiles_of(m, n, 64);
   if (tiles >= 400) return plan_of(P_SMALL, m, n, 1);
   if (tiles > 0 && tiles <= 64 && stages > 64) return plan_of(P_SMALL, m, n, kCus / tiles < 16 ? kCus / tiles : 16);
@@ -713,9 +719,10 @@ int64_t rounds_time(int64_t tiles, int64_t slots, int64_t stages, int64_t stage_
 // A weight gradient [m][n], a sum over `rows` rows.  bf16: the shape of the least
 // estimated time, tiles of 256 x 256 also in ranges of rows, whose sums are
 // written and read again at 4.5 TB/s.  The times per stage are fitted to
-// dW_down, measured us with Small, Mid and Big whole: 1000 x 768 x 2048 12, 16, 29;
-// 3001 x 1024 x 2816 37, 44, 73; 6000 x 768 x 2048 54, 72, 129; 1000 x 2048 x 5504
-// 48, 41, 33; 8191 x 2048 x 5504 339, 238, 183.  float32: 64 x 64, split where there are
+// dW_down, measured us with Small, Mid, Big whole and Big in ranges: 1000 x 768 x
+// 2048 13, 20, 30, 25 (2); 3001 x 1024 x 2816 36, 51, 69, 40 (5); 6000 x 768 x 2048
+// 57, 92, 123, 40 (8); 1000 x 2048 x 5504 50, 42, 33, 66 (2); 8191 x 2048 x 5504
+// 331, 268, 171, 214 (2); 16384 x 1024 x 2816 176, 242, 310, 91 (5).  float32: 64 x 64, split where there are
 // fewer than 256 tiles and 512 rows or more (3001 x 256 x 512: 71 -> 21 us).
 Plan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
   const int64_t stages = (rows + 63) / 64, small = tiles_of(m, n, 64), mid = tiles_of(m, n, 128), big = tiles_of(m, n, 256);
