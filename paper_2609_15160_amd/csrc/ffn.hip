@@ -692,10 +692,13 @@ Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
 }
 
 // y and dx, m rows, n columns, `stages` of 128 bytes of k.  Large tiles where
-// they fill the device: us of da with dx with Small, Mid and Big 3001 x 1024 x
-// 2816 (192 tiles of 128 x 128) 106, 111, 160; 3580 x 1024 x 2816 (224) 128, 112,
-// 160; 4400 x 1024 x 2816 (280) 135, 133, 158; 2000 x 2048 x 5504 (256) 225, 191,
-// 278; 8191 x 2048 x 5504 890, 597, 486.  Below, 64 x 64 by four waves from 400
+// they fill the device, those of 128 x 128 with one on most compute units or with
+// so many that few of them having two does not matter: us of the forward pass and
+// of da with dx with Small, Mid and Big 3001 x 1024 x 2816 (192 tiles of 128 x 128)
+// 82, 88, 112 and 106, 111, 160; 3580 x 1024 x 2816 (224) 92, 88, 113 and 128, 112,
+// 160; 2000 x 2048 x 5504 (256) 180, 171, 214 and 225, 191, 278; 4400 x 1024 x 2816
+// (280) 106, 109, 123 and 135, 133, 158; 8191 x 2048 x 5504 (1024) 589, 515, 456 and
+// 890, 597, 486.  Below, 64 x 64 by four waves from 400
 // tiles on and by 16 waves, which share the sum, under that; and where 64 of them
 // or fewer have a long sum, that is split until every compute unit has a share.
 // us of the forward pass with Small, Deep and Small split: 1 x 2048 x 5504 42, 32,
@@ -703,7 +706,8 @@ Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
 // 53, 59, 60.
 Plan store_plan(bool half, int64_t m, int64_t n, int64_t stages) {
   if (half && big_fits(tiles_of(m, n, 256))) return plan_of(P_BIG, m, n, 1);
-  if (half && tiles_of(m, n, 128) >= 208) return plan_of(P_MID, m, n, 1);
+  const int64_t mid = tiles_of(m, n, 128);
+  if (half && ((mid >= 208 && mid <= kCus) || mid >= 300)) return plan_of(P_MID, m, n, 1);
   const int64_t tiles = tiles_of(m, n, 64);
   if (tiles >= 400) return plan_of(P_SMALL, m, n, 1);
   if (tiles > 0 && tiles <= 64 && stages > 64) return plan_of(P_SMALL, m, n, kCus / tiles < 16 ? kCus / tiles : 16);
