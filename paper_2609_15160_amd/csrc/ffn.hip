@@ -93,11 +93,13 @@ __device__ __forceinline__ float unkept16(unsigned c) {
 // the weights instead (16384 x 1024 x 2816: gate/up 224 -> 217 us, down 88 -> 83).
 template <typename T> struct Kept;
 template <> struct Kept<float> {
-  static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
+  struct Raw { f32x4 q, p; };
+  static __device__ __forceinline__ void load(const void* base, int64_t at, Raw& o) {
     const float* s = reinterpret_cast<const float*>(base) + at * 8;
-    q = Vec4<float>::load(s);
-    p = Vec4<float>::load(s + 4);
+    o.q = Vec4<float>::load(s);
+    o.p = Vec4<float>::load(s + 4);
   }
+  static __device__ __forceinline__ void get(const Raw& o, f32x4& q, f32x4& p) { q = o.q, p = o.p; }
   static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
     float* s = reinterpret_cast<float*>(base) + at * 8;
     Vec4<float>::store(s, q);
@@ -105,8 +107,11 @@ template <> struct Kept<float> {
   }
 };
 template <> struct Kept<bf16> {
-  static __device__ __forceinline__ void load(const void* base, int64_t at, f32x4& q, f32x4& p) {
-    const u32x4 c = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + at);
+  using Raw = u32x4;
+  static __device__ __forceinline__ void load(const void* base, int64_t at, Raw& o) {
+    o = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + at);
+  }
+  static __device__ __forceinline__ void get(const Raw& c, f32x4& q, f32x4& p) {
     q = f32x4{unkept16(c.x), unkept16(c.x >> 16), unkept16(c.y), unkept16(c.y >> 16)};
     p = f32x4{unkept16(c.z), unkept16(c.z >> 16), unkept16(c.w), unkept16(c.w >> 16)};
   }
@@ -529,10 +534,29 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
           for (int j = 0; j < NT; ++j) Vec4<float>::store(part + (((wave * MT + i) * NT + j) * kWave + lane) * 4, acc[i][j]);
       return;
     }
+    // q and p are on their way kAhead rows of accumulators early, since the compiler
+    // moves no load past a store (da of 16384 x 1024 x 2816 148 -> 146 us, of 2000 x
+    // 1024 x 2816 30 -> 28; all 8 rows early spill: 173)
+    constexpr int kAhead = MT < 4 ? MT : 4;
+    typename Kept<T>::Raw raw[MT][NT];
+    auto early = [&](int i) __attribute__((always_inline)) {
+      const int mb = m0 + wm * (BM / SH::WM) + i * 16, n = n0 + wn * (BN / SH::WN);
+      if (mb >= g.M) return;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        if (n + j * 16 < g.N) Kept<T>::load(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (n >> 4) + j) * kWave + lane, raw[i][j]);
+    };
+    if constexpr (EK == E_DSWIGLU) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) early(i);
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int mb = m0 + wm * (BM / SH::WM) + i * 16, m = mb + (lane & 15);
       if (mb >= g.M) break;
+      if constexpr (EK == E_DSWIGLU) {
+        if (i + kAhead < MT) early(i + kAhead);
+      }
       const bool in = m < g.M;
       if constexpr (EK == E_SWIGLU) {
 #pragma unroll
@@ -565,8 +589,7 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
           } else {
             f32x4 q[2], p[2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-              Kept<T>::load(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (n >> 4) + x) * kWave + lane, q[x], p[x]);
+            for (int x = 0; x < 2; ++x) Kept<T>::get(raw[i][j + x], q[x], p[x]);
             T* o = reinterpret_cast<T*>(g.out) + m * g.ldo + n;
             if (in) {
               store_pair<T>(o, acc[i][j] * q[0], acc[i][j + 1] * q[1], lane);
