@@ -714,26 +714,32 @@ Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
   return {shape, (int)splits, splits > 1 ? (size_t)(splits * tiles_of(m, n, b) * b * b) * sizeof(float) : 0};
 }
 
-// y and dx, m rows, n columns, `stages` of 128 bytes of k.  Large tiles where
-// they fill the device, those of 128 x 128 with one on most compute units or with
-// so many that few of them having two does not matter: us of the forward pass and
-// of da with dx with Small, Mid and Big 3001 x 1024 x 2816 (192 tiles of 128 x 128)
-// 82, 88, 112 and 106, 111, 160; 3580 x 1024 x 2816 (224) 92, 88, 113 and 128, 112,
-// 160; 2000 x 2048 x 5504 (256) 180, 171, 214 and 225, 191, 278; 4400 x 1024 x 2816
-// (280) 106, 109, 123 and 135, 133, 158; 8191 x 2048 x 5504 (1024) 589, 515, 456 and
-// 890, 597, 486.  Below, 64 x 64 by four waves from 400
-// tiles on and by 16 waves, which share the sum, under that; and where 64 of them
-// or fewer have a long sum, that is split until every compute unit has a share.
-// us of the forward pass with Small, Deep and Small split: 1 x 2048 x 5504 42, 32,
-// 22; 333 x 768 x 2048 22, 19, 21; 1000 x 768 x 2048 29, 26, 33; 2000 x 1024 x 2816
-// 53, 59, 60.
+// y and dx, m rows, n columns, `stages` of 128 bytes of k.
+//
+// bf16, large tiles where they fill the device, those of 128 x 128 with one on
+// most compute units or with so many that few of them having two does not matter:
+// us of the forward pass and of da with dx with Small, Mid and Big 3001 x 1024 x
+// 2816 (192 tiles of 128 x 128) 82, 88, 112 and 106, 111, 160; 3580 x 1024 x 2816
+// (224) 92, 88, 113 and 128, 112, 160; 2000 x 2048 x 5504 (256) 180, 171, 214 and 225,
+// 191, 278; 4400 x 1024 x 2816 (280) 106, 109, 123 and 135, 133, 158; 8191 x 2048 x
+// 5504 (1024) 589, 515, 456 and 890, 597, 486.
+//
+// Else tiles of 64 x 64, by four waves where there are more than compute units,
+// by 16, which share the sum, below (1300 x 768 x 2048, 252 tiles, 33 and 31, 37 and
+// 35; 1500 x 768 x 2048, 288 tiles, 35 and 41, 44 and 51), and by four with the sum in
+// ranges where few tiles have a long one (16 waves and ranges: 1 x 2048 x 5504 32, 22
+// and 57, 28; 10 x 768 x 2048 16, 14 and 23, 16; 333 x 768 x 2048 19, 19 and 29, 23; 256
+// x 2048 x 5504 45, 38 and 67, 47; not 1000 x 768 x 2048 26, 27 and 31, 33).  float32,
+// whose products take more of the time, the same with other limits (300 x 256 x
+// 512 21, 17 and 31, 20; 1000 x 256 x 512 23, 19 and 33, 23; 3001 x 256 x 512 32, 36 and
+// 36, 39).
 Plan store_plan(bool half, int64_t m, int64_t n, int64_t stages) {
   if (half && big_fits(tiles_of(m, n, 256))) return plan_of(P_BIG, m, n, 1);
-  const int64_t mid = tiles_of(m, n, 128);
+  const int64_t mid = tiles_of(m, n, 128), tiles = tiles_of(m, n, 64);
   if (half && ((mid >= 208 && mid <= kCus) || mid >= 300)) return plan_of(P_MID, m, n, 1);
-  const int64_t tiles = tiles_of(m, n, 64);
-  if (tiles >= 400) return plan_of(P_SMALL, m, n, 1);
-  if (tiles > 0 && tiles <= 64 && stages > 64) return plan_of(P_SMALL, m, n, kCus / tiles < 16 ? kCus / tiles : 16);
+  if (tiles == 0 || tiles > kCus) return plan_of(P_SMALL, m, n, 1);
+  const int64_t wide = (half ? 2 : 1) * kCus / tiles, deep = stages / (half ? 6 : 3), s = wide < deep ? wide : deep;
+  if (s >= 2 && (!half || tiles <= 64 || (tiles <= 176 && stages >= 40))) return plan_of(P_SMALL, m, n, s < 16 ? s : 16);
   return plan_of(P_DEEP, m, n, 1);
 }
 
@@ -749,13 +755,17 @@ int64_t rounds_time(int64_t tiles, int64_t slots, int64_t stages, int64_t stage_
 // dW_down, measured us with Small, Mid, Big whole and Big in ranges: 1000 x 768 x
 // 2048 13, 20, 30, 25 (2); 3001 x 1024 x 2816 36, 51, 69, 40 (5); 6000 x 768 x 2048
 // 57, 92, 123, 40 (8); 1000 x 2048 x 5504 50, 42, 33, 66 (2); 8191 x 2048 x 5504
-// 331, 268, 171, 214 (2); 16384 x 1024 x 2816 176, 242, 310, 91 (5).  float32: 64 x 64, split where there are
-// fewer than 256 tiles and 512 rows or more (3001 x 256 x 512: 71 -> 21 us).
+// 331, 268, 171, 214 (2); 16384 x 1024 x 2816 176, 242, 310, 91 (5).  float32: 64 x 64,
+// the rows in ranges for a workgroup on each compute unit, or two with 375 rows or
+// more (3001 x 256 x 512, ranges for one and for two: dW_down 17, 19, dW_gate_up 42
+// with da, 39; 8000 rows 34, 30 and 89, 76; 1000 rows 11, 13 and 24, 26; whole 3001
+// rows take 80 and 96).
 Plan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
   const int64_t stages = (rows + 63) / 64, small = tiles_of(m, n, 64), mid = tiles_of(m, n, 128), big = tiles_of(m, n, 256);
   if (!half) {
-    const int64_t most = rows / 128, want = (kCus + small - 1) / small;
-    return plan_of(P_SMALL, m, n, small >= kCus || rows < 512 ? 1 : want < most ? want : most);
+    const int64_t one = (kCus + small - 1) / small, few = rows / 64, two = 2 * kCus / small, long_ = rows / 375;
+    const int64_t a = one < few ? one : few, b = two < long_ ? two : long_, s = a > b ? a : b;
+    return plan_of(P_SMALL, m, n, rows < 256 || s < 1 ? 1 : s < 64 ? s : 64);
   }
   Plan best = plan_of(P_SMALL, m, n, 1);
   int64_t t = rounds_time(small, 3 * kCus, stages, small <= kCus ? 400 : small <= 2 * kCus ? 500 : 680, 3500);

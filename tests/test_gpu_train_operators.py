@@ -733,3 +733,18 @@ def test_forward_and_backward_captured_together():
         step(*leaves(sets[(k + 1) % 4]))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want[k])), k
+
+
+@pytest.mark.parametrize("t,n,d,f", [
+    ("bf16", 1000, 768, 512),    # y and dx by 16 waves that share the sum
+    ("bf16", 700, 1024, 64),     # the same, fewer steps than waves share
+    ("bf16", 12, 768, 1024),     # y and dx in ranges, an uneven number of steps in each
+    ("bf16", 600, 1024, 2624),   # the same with more tiles
+    ("bf16", 1700, 768, 256),    # more tiles than compute units, by four waves
+    ("f32", 3001, 256, 192),     # float32 by 16 waves
+    ("f32", 300, 256, 512),      # float32 in ranges
+    ("f32", 5000, 256, 64),      # float32 weight gradients in ranges for two workgroups on each compute unit
+    ("f32", 257, 64, 64),        # and in ranges of 64 rows
+])
+def test_ffn_few_tiles(t, n, d, f):
+    _check_ffn(n, d, f, t)
