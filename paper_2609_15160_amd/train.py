@@ -3,11 +3,16 @@ straight-through estimator (Appendix B) as autograd functions over libtlf.
 
 Argument marshalling only: the active set, the gather, the scatter, their
 gradients and the estimator all run in libtlf's HIP kernels, on the current
-torch stream.  The shared block between gather and scatter is the caller's.
+torch stream.  The attention half of the block is the caller's.
 
     p = plan(depth, batch, seq_len, loop)     # loop i's active rows
     x = gather(h, p)                          # [p.count, d], Eq. 6
     h = scatter(h, block(x), p)               # Eq. 7 (scatter_ writes into h)
+
+Of the block, the FFN half is here: rms_norm (with the AdaLN scale of each row's
+group), ffn, and the optimizer's step, adamw_ and AdamW.
+
+    y = ffn(rms_norm(x, gamma, group, dtype=torch.bfloat16), w_gate_up, w_down)
 """
 from __future__ import annotations
 
