@@ -257,13 +257,27 @@ def _workspace(fn, *args, device):
     return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
 
 
-def _first_order(backward):
-    """once_differentiable, without its cost (5 us) where no graph of the gradients is built."""
-    checked = torch.autograd.function.once_differentiable(backward)
+class _NoSecond(torch.autograd.Function):
+    """The first n tensors, gradients that depend on the rest: their own gradients are refused."""
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tensors[:n]
 
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("rms_norm and ffn have no gradients of gradients")
+
+
+def _first_order(backward):
+    """A backward pass without one of its own: where a graph of it is built (create_graph), differentiating that is
+    refused."""
     @functools.wraps(backward)
     def run(ctx, *grads):
-        return checked(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        return _NoSecond.apply(len(out), *out, *(t for t in (*ctx.saved_tensors, *grads) if t is not None))
     return run
 
 

@@ -748,3 +748,15 @@ def test_forward_and_backward_captured_together():
 ])
 def test_ffn_few_tiles(t, n, d, f):
     _check_ffn(n, d, f, t)
+
+
+def test_gradients_of_gradients_are_refused():
+    train = _train()
+    x, w, v = (torch.randn(64, 64, device="cuda").requires_grad_() for _ in range(3))
+    gu = torch.cat([w, v])
+    for out in (train.rms_norm(x), train.ffn(x, gu, v)):
+        one, = torch.autograd.grad(out, x, torch.ones_like(out), retain_graph=True)
+        dx, = torch.autograd.grad(out, x, torch.ones_like(out), create_graph=True)
+        assert torch.equal(one, dx)
+        with pytest.raises(RuntimeError, match="gradients of gradients"):
+            torch.autograd.grad(dx, x, torch.ones_like(dx))
