@@ -35,28 +35,9 @@ constexpr int kAdamBlocks = (1 << 24) - 1;                // of a launch, which 
 constexpr int kBlock = TLF_ADAMW_BLOCK;
 static_assert(kBlock == 4 * kWave, "one wave per block of 8-bit moments");
 
-// Streams: nothing is read twice, so loads and stores pass the caches by (10^8
-// elements with float32 moments: 510 us through them, 463 past them, 6.0 TB/s;
-// with 8 bits 349 and 340, and 314, 5.1 TB/s, with reciprocals for divisions).
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-template <typename T> struct Stream4;
-template <> struct Stream4<float> {
-  static __device__ __forceinline__ f32x4 load(const float* p) {
-    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
-  }
-  static __device__ __forceinline__ void store(float* p, f32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(p)); }
-};
-template <> struct Stream4<bf16> {
-  static __device__ __forceinline__ f32x4 load(const bf16* p) {
-    const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-    return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
-                 __uint_as_float(v[1] & 0xFFFF0000u)};
-  }
-  static __device__ __forceinline__ void store(bf16* p, f32x4 v) {
-    __builtin_nontemporal_store((u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, reinterpret_cast<u32x2*>(p));
-  }
-};
-
+// Nothing is read twice, so loads and stores pass the caches by (10^8 elements
+// with float32 moments: 510 us through them, 463 past them, 6.0 TB/s; with 8 bits
+// 349 and 340, and 314, 5.1 TB/s, with reciprocals for divisions).
 struct AdamTensor {
   float* p;
   bf16* copy;

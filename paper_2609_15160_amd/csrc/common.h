@@ -163,6 +163,29 @@ template <> struct Vec4<bf16> {
   }
 };
 
+// The same past the caches, for what is not read again soon.
+template <typename T> struct Stream4;
+template <> struct Stream4<float> {
+  static __device__ __forceinline__ f32x4 load(const float* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(p));
+  }
+  static __device__ __forceinline__ void store(float* p, f32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(p)); }
+};
+template <> struct Stream4<bf16> {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ u32x2 raw(const bf16* p) {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  }
+  static __device__ __forceinline__ f32x4 load(const bf16* p) {
+    const u32x2 v = raw(p);
+    return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
+                 __uint_as_float(v[1] & 0xFFFF0000u)};
+  }
+  static __device__ __forceinline__ void store(bf16* p, f32x4 v) {
+    __builtin_nontemporal_store((u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}, reinterpret_cast<u32x2*>(p));
+  }
+};
+
 // Eight consecutive float32 values as the hi and lo fragments of a bf16 MFMA operand.
 __device__ __forceinline__ void split_frag(const float* p, bf16x8& hi, bf16x8& lo) {
   uint2 h0, l0, h1, l1;

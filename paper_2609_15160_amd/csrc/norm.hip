@@ -47,19 +47,38 @@ __device__ __forceinline__ float wave_sum(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Where the call's tensors are more than the memory-side cache holds, the rows are
+// loaded past the caches, which else give up what they could serve (us through and
+// past them, both gradients, 8 groups: 20000 x 1024 42, 50; 24576 63, 57; 32768 84,
+// 71; 65536 154, 140; dx alone 24576 37, 42; 40000 77, 64; forward 40000 38, 45; 65536
+// 73, 68; 131072 139, 118).  What is written is read next and stays in them.
+constexpr int64_t kCacheBytes = 256ll << 20;
+template <bool PAST, typename T> __device__ __forceinline__ f32x4 load4(const T* p) {
+  if constexpr (PAST) return Stream4<T>::load(p);
+  else return Vec4<T>::load(p);
+}
+
 // Four elements as they lie in memory, converted where they are used: a
 // conversion next to the load would wait for it there.
 template <typename T> struct Raw4;
 template <> struct Raw4<float> {
   f32x4 v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) { v = Vec4<float>::load(reinterpret_cast<const float*>(p) + at); }
+  template <bool PAST> __device__ __forceinline__ void load(const void* p, int64_t at) {
+    v = load4<PAST>(reinterpret_cast<const float*>(p) + at);
+  }
   __device__ __forceinline__ void zero() { v = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ f32x4 get() const { return v; }
 };
 template <> struct Raw4<bf16> {
   uint2 v;
-  __device__ __forceinline__ void load(const void* p, int64_t at) {
-    v = *reinterpret_cast<const uint2*>(reinterpret_cast<const bf16*>(p) + at);
+  template <bool PAST> __device__ __forceinline__ void load(const void* p, int64_t at) {
+    const bf16* s = reinterpret_cast<const bf16*>(p) + at;
+    if constexpr (PAST) {
+      const auto r = Stream4<bf16>::raw(s);
+      v = make_uint2(r[0], r[1]);
+    } else {
+      v = *reinterpret_cast<const uint2*>(s);
+    }
   }
   __device__ __forceinline__ void zero() { v = make_uint2(0, 0); }
   __device__ __forceinline__ f32x4 get() const {
@@ -76,7 +95,8 @@ __device__ __forceinline__ const float* gamma_of(const float* gamma, const int32
 
 // One wave per row, the row in registers: 4 NV elements per lane.  Bound by HBM:
 // 32768 x 1024 from float32 to bf16 33 us, 6.1 TB/s.
-template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWaves* kWave) void k_norm(NormArgs a) {
+template <typename TX, typename TY, int NV, bool PAST>
+__global__ __launch_bounds__(kNormWaves* kWave) void k_norm(NormArgs a) {
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * kNormWaves + threadIdx.x / kWave), lane = lane_id();
   if (row >= a.rows) return;
   const TX* x = reinterpret_cast<const TX*>(a.x) + (int64_t)row * a.d;
@@ -86,7 +106,7 @@ template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWa
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = (k * kWave + lane) * 4;
-    v[k] = c < a.d ? Vec4<TX>::load(x + c) : f32x4{0.f, 0.f, 0.f, 0.f};
+    v[k] = c < a.d ? load4<PAST>(x + c) : f32x4{0.f, 0.f, 0.f, 0.f};
   }
 #pragma unroll
   for (int k = 0; k < NV; ++k) ss += (v[k][0] * v[k][0] + v[k][1] * v[k][1]) + (v[k][2] * v[k][2] + v[k][3] * v[k][3]);
@@ -103,7 +123,8 @@ template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWa
   }
 }
 
-template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWaves* kWave) void k_norm_dx(NormArgs a) {
+template <typename TX, typename TY, int NV, bool PAST>
+__global__ __launch_bounds__(kNormWaves* kWave) void k_norm_dx(NormArgs a) {
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * kNormWaves + threadIdx.x / kWave), lane = lane_id();
   if (row >= a.rows) return;
   const TX* x = reinterpret_cast<const TX*>(a.x) + (int64_t)row * a.d;
@@ -117,8 +138,8 @@ template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWa
     const int c = (k * kWave + lane) * 4;
     v[k] = h[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (c < a.d) {
-      v[k] = Vec4<TX>::load(x + c);
-      h[k] = Vec4<TY>::load(dy + c);
+      v[k] = load4<PAST>(x + c);
+      h[k] = load4<PAST>(dy + c);
       if (gm) h[k] *= 1.f + Vec4<float>::load(gm + c);
     }
   }
@@ -138,14 +159,14 @@ template <typename TX, typename TY, int NV> __global__ __launch_bounds__(kNormWa
 // thread four columns of each (a wave per 256 columns), so that a column of
 // gamma's gradient has one owner, which adds its rows in order, each group's in
 // registers of its own (the row's group is uniform, a scalar branch picks them;
-// with the sums in LDS 108 us where these take 90).  The row's mean goes over the
+// with the sums in LDS 108 us where these took 90).  The row's mean goes over the
 // waves through LDS, one barrier for RU rows; the next RU rows are on their way
 // meanwhile, and the groups of those after them.  x and dy are read once, dx is
 // written; the workgroups' sums add 4 groups d bytes each.  32768 x 1024, float32
-// x, bf16 dy, both gradients with their sums joined: 90 us for 8 groups, 77 for
-// one (dx alone 57, 5.9 TB/s); what is left is the loads' latency between two
-// barriers.
-template <typename TX, typename TY, int GMAX, int MAXT, int RU>
+// x, bf16 dy, both gradients with their sums joined: 71 us for 8 groups (5.2 TB/s
+// with the sums), dx alone 54 (6.2 TB/s); what is left is the loads' latency
+// between two barriers.
+template <typename TX, typename TY, int GMAX, int MAXT, int RU, bool PAST>
 __global__ __launch_bounds__(MAXT) void k_norm_grad(NormArgs a, int chunk, float* part) {
   __shared__ __align__(16) float red[2][MAXT / kWave][RU];
   const int tid = threadIdx.x, lane = lane_id(), wave = tid / kWave, nw = blockDim.x / kWave, c = tid * 4;
@@ -173,8 +194,8 @@ __global__ __launch_bounds__(MAXT) void k_norm_grad(NormArgs a, int chunk, float
     o.dy.zero();
     o.gamma = zero;
     if (own && row < r1) {
-      o.x.load(a.x, (int64_t)row * a.d + c);
-      o.dy.load(a.dy, (int64_t)row * a.d + c);
+      o.x.template load<PAST>(a.x, (int64_t)row * a.d + c);
+      o.dy.template load<PAST>(a.dy, (int64_t)row * a.d + c);
       if (GMAX > 1 && k >= 0) o.gamma = Vec4<float>::load(a.gamma + (int64_t)k * a.d + c);
     }
   };
@@ -279,11 +300,11 @@ int check(int32_t x_dtype, int32_t y_dtype, int32_t groups, int32_t rows, int32_
 
 constexpr int kLaunchRows = 1 << 24;  // a launch has fewer than 2^32 threads
 
-template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(NormArgs a, hipStream_t s) {
+template <typename TX, typename TY, bool GRAD, bool PAST> hipError_t launch_rows(NormArgs a, hipStream_t s) {
   if (a.rows > kLaunchRows) {
     NormArgs head = a;
     head.rows = kLaunchRows;
-    const hipError_t e = launch_rows<TX, TY, GRAD>(head, s);
+    const hipError_t e = launch_rows<TX, TY, GRAD, PAST>(head, s);
     if (e != hipSuccess) return e;
     const int64_t n = (int64_t)kLaunchRows * a.d;
     a.x = reinterpret_cast<const TX*>(a.x) + n;
@@ -292,12 +313,12 @@ template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(NormArgs a
     if (a.group) a.group += kLaunchRows;
     if (a.rstd) a.rstd += kLaunchRows;
     a.rows -= kLaunchRows;
-    return launch_rows<TX, TY, GRAD>(a, s);
+    return launch_rows<TX, TY, GRAD, PAST>(a, s);
   }
   const dim3 grid((a.rows + kNormWaves - 1) / kNormWaves), block(kNormWaves * kWave);
 #define TLF_NORM(NV)                                                                   \
-  if (GRAD) hipLaunchKernelGGL((k_norm_dx<TX, TY, NV>), grid, block, 0, s, a);         \
-  else hipLaunchKernelGGL((k_norm<TX, TY, NV>), grid, block, 0, s, a)
+  if (GRAD) hipLaunchKernelGGL((k_norm_dx<TX, TY, NV, PAST>), grid, block, 0, s, a);   \
+  else hipLaunchKernelGGL((k_norm<TX, TY, NV, PAST>), grid, block, 0, s, a)
   if (a.d <= 256) { TLF_NORM(1); }
   else if (a.d <= 512) { TLF_NORM(2); }
   else if (a.d <= 1024) { TLF_NORM(4); }
@@ -307,12 +328,24 @@ template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(NormArgs a
   return hipGetLastError();
 }
 
-template <typename TX, typename TY, int MAXT, int RU>
+template <typename TX, typename TY, bool GRAD> hipError_t launch_rows(const NormArgs& a, hipStream_t s) {
+  const int64_t bytes = (int64_t)a.rows * a.d * (int64_t)(GRAD ? 2 * sizeof(TX) + sizeof(TY) : sizeof(TX) + sizeof(TY));
+  return bytes > kCacheBytes ? launch_rows<TX, TY, GRAD, true>(a, s) : launch_rows<TX, TY, GRAD, false>(a, s);
+}
+
+template <typename TX, typename TY, int MAXT, int RU, bool PAST>
 void launch_sums(const NormArgs& a, int chunk, int chunks, float* part, hipStream_t s) {
   const dim3 grid(chunks), block((a.d + kGammaCols - 1) / kGammaCols * kWave);
-  if (a.groups == 1) hipLaunchKernelGGL((k_norm_grad<TX, TY, 1, MAXT, RU>), grid, block, 0, s, a, chunk, part);
-  else if (a.groups <= 8) hipLaunchKernelGGL((k_norm_grad<TX, TY, 8, MAXT, RU>), grid, block, 0, s, a, chunk, part);
-  else hipLaunchKernelGGL((k_norm_grad<TX, TY, TLF_NORM_MAX_GROUPS, MAXT, RU>), grid, block, 0, s, a, chunk, part);
+  if (a.groups == 1) hipLaunchKernelGGL((k_norm_grad<TX, TY, 1, MAXT, RU, PAST>), grid, block, 0, s, a, chunk, part);
+  else if (a.groups <= 8) hipLaunchKernelGGL((k_norm_grad<TX, TY, 8, MAXT, RU, PAST>), grid, block, 0, s, a, chunk, part);
+  else hipLaunchKernelGGL((k_norm_grad<TX, TY, TLF_NORM_MAX_GROUPS, MAXT, RU, PAST>), grid, block, 0, s, a, chunk, part);
+}
+
+template <typename TX, typename TY, bool PAST>
+void launch_width(const NormArgs& a, int chunk, int chunks, float* part, hipStream_t s) {
+  if (a.d <= 1024) launch_sums<TX, TY, 256, kGradRows, PAST>(a, chunk, chunks, part, s);
+  else if (a.d <= 2048) launch_sums<TX, TY, 512, kGradRows, PAST>(a, chunk, chunks, part, s);
+  else launch_sums<TX, TY, 1024, kGradRows, PAST>(a, chunk, chunks, part, s);
 }
 
 template <typename TX, typename TY> hipError_t launch_grad(const NormArgs& a, void* dx, float* dgamma, float* part, hipStream_t s) {
@@ -321,9 +354,9 @@ template <typename TX, typename TY> hipError_t launch_grad(const NormArgs& a, vo
   if (!dgamma) return a.rows > 0 ? launch_rows<TX, TY, true>(b, s) : hipSuccess;
   const int chunk = grad_chunk(a.rows, a.d), chunks = grad_chunks(a.rows, a.d), n = a.groups * a.d;
   if (chunks > 0) {
-    if (a.d <= 1024) launch_sums<TX, TY, 256, kGradRows>(b, chunk, chunks, part, s);
-    else if (a.d <= 2048) launch_sums<TX, TY, 512, kGradRows>(b, chunk, chunks, part, s);
-    else launch_sums<TX, TY, 1024, kGradRows>(b, chunk, chunks, part, s);
+    const int64_t row = (int64_t)a.d * (int64_t)(2 * sizeof(TX) + sizeof(TY)), sums = (int64_t)chunks * n * 4;
+    if (a.rows * row + sums > kCacheBytes) launch_width<TX, TY, true>(b, chunk, chunks, part, s);
+    else launch_width<TX, TY, false>(b, chunk, chunks, part, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

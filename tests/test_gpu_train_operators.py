@@ -760,3 +760,27 @@ def test_gradients_of_gradients_are_refused():
         assert torch.equal(one, dx)
         with pytest.raises(RuntimeError, match="gradients of gradients"):
             torch.autograd.grad(dx, x, torch.ones_like(dx))
+
+
+@pytest.mark.parametrize("n,d,groups,xt,yt", [(70000, 1024, 8, "f32", "bf16"), (50000, 2048, 0, "bf16", "bf16"),
+                                              (30000, 2052, 3, "f32", "f32")])
+def test_norm_rows_of_a_large_call_as_of_a_small_one(n, d, groups, xt, yt):
+    """Rows do not depend on how many there are: a call of more bytes than the caches hold against one of some of its
+    rows, to the bit."""
+    train = _train()
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x = torch.randn(n, d, generator=gen, device="cuda").to(_dt(xt)).requires_grad_()
+    dy = torch.randn(n, d, generator=gen, device="cuda").to(_dt(yt))
+    gamma = torch.randn(groups, d, generator=gen, device="cuda").requires_grad_() if groups else None
+    group = torch.randint(0, groups, (n,), generator=gen, device="cuda", dtype=torch.int32) if groups else None
+    _say("norm", n, d, groups, xt, yt)
+    at = torch.cat([torch.arange(5, device="cuda"), torch.randint(0, n, (200,), generator=gen, device="cuda"),
+                    torch.arange(n - 5, n, device="cuda")])
+
+    def both(x, dy, group):
+        y = train.rms_norm(x, gamma, group, dtype=_dt(yt))
+        return y.detach(), torch.autograd.grad(y, [x] + ([gamma] if groups else []), dy)[0]
+
+    small = both(x.detach()[at].requires_grad_(), dy[at], None if group is None else group[at])
+    for a, b in zip(both(x, dy, group), small):
+        assert torch.equal(a[at], b)
