@@ -455,9 +455,9 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
  *   d_w_gate_up   [2f][d]: rows gate | up (as tlf_layer_weights);
  *   d_w_down      [d][f];
  *   d_kept        tlf_ffn_kept_bytes bytes, receives what tlf_ffn_grad needs of g
- *                 and u (u silu'(g) and silu(g), in an order of its own; bf16: in 16
- *                 bits with 9 bits of mantissa and magnitudes up to 2^32), or NULL if
- *                 no gradient follows;
+ *                 and u (u silu'(g) and silu(g), in an order of its own; bf16: in 18
+ *                 bits, float32's range with 9 bits of mantissa), or NULL if no
+ *                 gradient follows;
  *   d_a           [rows][f], receives a (read by the second product);
  *   d_y           [rows][d];
  *   d_workspace   tlf_ffn_ws_bytes bytes (may be 0), used during the call only.
@@ -465,8 +465,7 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
  * them less than 2^35. */
 #define TLF_FFN_MAX_WIDTH 16384
 static inline size_t tlf_ffn_kept_bytes(int32_t dtype, int32_t rows, int32_t f) {
-  return rows <= 0 || f <= 0 ? 0
-                             : ((size_t)rows + 15) / 16 * 16 * 2u * (size_t)f * (dtype == TLF_DTYPE_BF16 ? 2u : 4u);
+  return rows <= 0 || f <= 0 ? 0 : ((size_t)rows + 15) / 16 * 8 * (size_t)f * (dtype == TLF_DTYPE_BF16 ? 9u : 16u);
 }
 int tlf_ffn_ws_bytes(int32_t dtype, int32_t rows, int32_t d, int32_t f, size_t* ws_bytes);
 int tlf_ffn(const void* d_x, const void* d_w_gate_up, const void* d_w_down, int32_t dtype, int32_t rows, int32_t d,

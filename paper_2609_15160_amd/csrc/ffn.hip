@@ -69,56 +69,87 @@ struct FArgs {
   int splits;
 };
 
-// q and p between the passes.  float32: as they are.  bf16: 16 bits, of which 6
-// are exponent and 9 mantissa: rounded to bf16 their 2^-8 would be the larger
-// part of the gradients' error (dx and dW_gate_up 0.0030 from 64 bits relative
-// to their norm, 0.0024 with 2^-10), and what the exponent gives up are
-// magnitudes past 2^32 (kept as the largest, 4.29e9) and below 2^-39.
-// Times 2^-96 such a float's two highest exponent bits are zeros, so a code is
-// the float's sign and bits 14 to 28; exponent code 63 is NaN.
-constexpr float kKeptMax = 4290772992.f;  // (2 - 2^-9) 2^31
-__device__ __forceinline__ unsigned kept16(float v) {
-  v = v > kKeptMax ? kKeptMax : v < -kKeptMax ? -kKeptMax : v;
-  unsigned b = __float_as_uint(v * 0x1p-96f);
-  b += 0x1FFFu + ((b >> 14) & 1u);  // nearest, ties to even
-  return ((b >> 14) & 0x7FFFu) | ((b >> 16) & 0x8000u);
+// q and p between the passes.  float32: as they are.  bf16: float32's sign, exponent
+// and 9 bits of mantissa, 18 bits, so that what operands of bf16 give between the
+// ends of their range (infinity and NaN too) comes back as it was up to 2^-10 of
+// it.  Rounded to bf16 their 2^-8 would be the larger part of the gradients' error
+// (dx and dW_gate_up 0.0030 from 64 bits relative to their norm, 0.0024 with 2^-10);
+// 9 bits of mantissa within 16 would leave 6 for the exponent, which loses gates
+// and products past 2^32 and below 2^-30.
+__device__ __forceinline__ unsigned kept18(float v) {  // in the upper 18 bits, the others are not zeros
+  const unsigned b = v == v ? __float_as_uint(v) : 0x7FC00000u;
+  return b + 0x1FFFu + ((b >> 14) & 1u);  // nearest, ties to even
 }
-__device__ __forceinline__ float unkept16(unsigned c) {
-  const float v = __uint_as_float(((c & 0x8000u) << 16) | ((c & 0x7FFFu) << 14)) * 0x1p96f;
-  return fabsf(v) < 0x1p32f ? v : __uint_as_float(0x7FC00000u);
-}
-// They lie as the lanes of a 16 x 16 accumulator hold them, [row / 16][f / 16]
-// [lane][4 q, 4 p], so that a wave reads and writes whole lines (row by row it
-// moved 8 bytes per lane in 32-byte pieces), past the caches, which keep a and
-// the weights instead (16384 x 1024 x 2816: gate/up 224 -> 217 us, down 88 -> 83).
+// They lie as the lanes of two neighbouring 16 x 16 accumulators hold them: first
+// the upper 16 bits, [row / 16][f / 16][lane][4 q, 4 p], behind those of all rows the
+// other two, [row / 16][f / 32][lane][16 of them], so that a wave reads and writes
+// whole lines (row by row it moved 8 bytes per lane in 32-byte pieces), past the
+// caches, which keep a and the weights instead (16384 x 1024 x 2816, measured when
+// q and p were 16 bits: gate/up 224 -> 217 us, down 88 -> 83).  `pair` counts the
+// pairs of accumulators times lanes, `pairs` is their number.
 template <typename T> struct Kept;
 template <> struct Kept<float> {
-  struct Raw { f32x4 q, p; };
-  static __device__ __forceinline__ void load(const void* base, int64_t at, Raw& o) {
-    const float* s = reinterpret_cast<const float*>(base) + at * 8;
-    o.q = Vec4<float>::load(s);
-    o.p = Vec4<float>::load(s + 4);
+  struct Raw { f32x4 q[2], p[2]; };
+  static __device__ __forceinline__ void load(const void* base, int64_t, int64_t pair, int lane, Raw& o) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float* s = reinterpret_cast<const float*>(base) + ((2 * pair + x) * kWave + lane) * 8;
+      o.q[x] = Vec4<float>::load(s);
+      o.p[x] = Vec4<float>::load(s + 4);
+    }
   }
-  static __device__ __forceinline__ void get(const Raw& o, f32x4& q, f32x4& p) { q = o.q, p = o.p; }
-  static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
-    float* s = reinterpret_cast<float*>(base) + at * 8;
-    Vec4<float>::store(s, q);
-    Vec4<float>::store(s + 4, p);
+  static __device__ __forceinline__ void get(const Raw& o, int x, f32x4& q, f32x4& p) { q = o.q[x], p = o.p[x]; }
+  static __device__ __forceinline__ void store(void* base, int64_t, int64_t pair, int lane, const f32x4 (&q)[2],
+                                               const f32x4 (&p)[2]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      float* s = reinterpret_cast<float*>(base) + ((2 * pair + x) * kWave + lane) * 8;
+      Vec4<float>::store(s, q[x]);
+      Vec4<float>::store(s + 4, p[x]);
+    }
   }
 };
 template <> struct Kept<bf16> {
-  using Raw = u32x4;
-  static __device__ __forceinline__ void load(const void* base, int64_t at, Raw& o) {
-    o = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base) + at);
+  struct Raw {
+    u32x4 high[2];
+    unsigned low;  // element r of q and of p of accumulator x: bits 8 x + 2 r and 16 + 8 x + 2 r
+  };
+  static __device__ __forceinline__ void load(const void* base, int64_t pairs, int64_t pair, int lane, Raw& o) {
+    const u32x4* high = reinterpret_cast<const u32x4*>(base);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) o.high[x] = __builtin_nontemporal_load(high + (2 * pair + x) * kWave + lane);
+    o.low = __builtin_nontemporal_load(reinterpret_cast<const unsigned*>(high + 2 * pairs * kWave) + pair * kWave + lane);
   }
-  static __device__ __forceinline__ void get(const Raw& c, f32x4& q, f32x4& p) {
-    q = f32x4{unkept16(c.x), unkept16(c.x >> 16), unkept16(c.y), unkept16(c.y >> 16)};
-    p = f32x4{unkept16(c.z), unkept16(c.z >> 16), unkept16(c.w), unkept16(c.w >> 16)};
+  static __device__ __forceinline__ float value(unsigned two, int r, unsigned low, int at) {
+    const unsigned l = at < 14 ? low << (14 - at) : low >> (at - 14);
+    return __uint_as_float((r & 1 ? two & 0xFFFF0000u : two << 16) | (l & 0xC000u));
   }
-  static __device__ __forceinline__ void store(void* base, int64_t at, f32x4 q, f32x4 p) {
-    __builtin_nontemporal_store((u32x4){kept16(q[0]) | kept16(q[1]) << 16, kept16(q[2]) | kept16(q[3]) << 16,
-                                        kept16(p[0]) | kept16(p[1]) << 16, kept16(p[2]) | kept16(p[3]) << 16},
-                                reinterpret_cast<u32x4*>(base) + at);
+  static __device__ __forceinline__ void get(const Raw& c, int x, f32x4& q, f32x4& p) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      q[r] = value(c.high[x][r >> 1], r, c.low, 8 * x + 2 * r);
+      p[r] = value(c.high[x][2 + (r >> 1)], r, c.low, 16 + 8 * x + 2 * r);
+    }
+  }
+  static __device__ __forceinline__ void store(void* base, int64_t pairs, int64_t pair, int lane, const f32x4 (&q)[2],
+                                               const f32x4 (&p)[2]) {
+    u32x4* high = reinterpret_cast<u32x4*>(base);
+    unsigned low = 0;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      unsigned b[8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        b[r] = kept18(q[x][r]);
+        b[4 + r] = kept18(p[x][r]);
+        low |= (b[r] >> 14 & 3u) << (8 * x + 2 * r) | (b[4 + r] >> 14 & 3u) << (16 + 8 * x + 2 * r);
+      }
+      u32x4 h;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) h[k] = b[2 * k] >> 16 | (b[2 * k + 1] & 0xFFFF0000u);
+      __builtin_nontemporal_store(h, high + (2 * pair + x) * kWave + lane);
+    }
+    __builtin_nontemporal_store(low, reinterpret_cast<unsigned*>(high + 2 * pairs * kWave) + pair * kWave + lane);
   }
 };
 
@@ -538,13 +569,15 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
     // moves no load past a store (da of 16384 x 1024 x 2816 148 -> 146 us, of 2000 x
     // 1024 x 2816 30 -> 28; all 8 rows early spill: 173)
     constexpr int kAhead = MT < 4 ? MT : 4;
-    typename Kept<T>::Raw raw[MT][NT];
+    const int64_t pairs = (int64_t)((g.M + 15) >> 4) * (g.N >> 5);
+    typename Kept<T>::Raw raw[MT][NT / 2];
     auto early = [&](int i) __attribute__((always_inline)) {
       const int mb = m0 + wm * (BM / SH::WM) + i * 16, n = n0 + wn * (BN / SH::WN);
       if (mb >= g.M) return;
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        if (n + j * 16 < g.N) Kept<T>::load(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (n >> 4) + j) * kWave + lane, raw[i][j]);
+      for (int j = 0; j < NT / 2; ++j)
+        if (n + j * 32 < g.N)
+          Kept<T>::load(g.kept, pairs, (int64_t)(mb >> 4) * (g.N >> 5) + (n >> 5) + j, lane, raw[i][j]);
     };
     if constexpr (EK == E_DSWIGLU) {
 #pragma unroll
@@ -563,20 +596,19 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
         for (int j = 0; j < NT / 2; j += 2) {
           const int f = n0 + wn * (TN / SH::WN) + j * 16;
           if (f >= g.N) break;
-          f32x4 h[2];
+          f32x4 h[2], q[2], p[2];
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const f32x4 gt = acc[i][j + x], up = acc[i][j + x + NT / 2];
-            f32x4 q, p;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const float s = sigmoid<T>(gt[r]);
-              p[r] = gt[r] * s;
-              q[r] = up[r] * (s * (1.f + gt[r] * (1.f - s)));
-              h[x][r] = p[r] * up[r];
+              p[x][r] = gt[r] * s;
+              q[x][r] = up[r] * (s * (1.f + gt[r] * (1.f - s)));
+              h[x][r] = p[x][r] * up[r];
             }
-            if (g.kept) Kept<T>::store(g.kept, ((int64_t)(mb >> 4) * (g.N >> 4) + (f >> 4) + x) * kWave + lane, q, p);
           }
+          if (g.kept) Kept<T>::store(g.kept, pairs, (int64_t)(mb >> 4) * (g.N >> 5) + (f >> 5), lane, q, p);
           if (in) store_pair<T>(reinterpret_cast<T*>(g.out) + m * g.ldo + f, h[0], h[1], lane);
         }
       } else {
@@ -589,7 +621,7 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
           } else {
             f32x4 q[2], p[2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) Kept<T>::get(raw[i][j + x], q[x], p[x]);
+            for (int x = 0; x < 2; ++x) Kept<T>::get(raw[i][j / 2], x, q[x], p[x]);
             T* o = reinterpret_cast<T*>(g.out) + m * g.ldo + n;
             if (in) {
               store_pair<T>(o, acc[i][j] * q[0], acc[i][j + 1] * q[1], lane);
@@ -607,7 +639,7 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
 // (1210), 214 (860), 277 (1330).  The loads into LDS bound the products: without
 // them 135, 50, 139 and 91 us of the first four (then 231, 91, 153, 155), alone 131 of
 // gate/up, 73 of down, 126 of dx, of which 37 of down's where all of it is in L2.
-// Gate/up writes 277 MB in its epilogue and da reads and writes 370: one workgroup
+// Gate/up writes 300 MB in its epilogue and da reads and writes 392: one workgroup
 // fills a compute unit, so nothing else runs on it meanwhile.
 template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn(FArgs g) {
   using TL = Tile<T, TA, TB, EK, SH, false>;

@@ -113,7 +113,7 @@ ADAMW_BLOCK = 256
 
 def ffn_kept_bytes(dtype: int, rows: int, f: int) -> int:
     """Bytes that tlf_ffn keeps for tlf_ffn_grad (tlf_ffn_kept_bytes in tlf.h)."""
-    return (rows + 15) // 16 * 16 * 2 * f * (2 if dtype == DTYPE_BF16 else 4)
+    return (rows + 15) // 16 * 8 * f * (9 if dtype == DTYPE_BF16 else 16)
 
 
 class AdamwTensor(ctypes.Structure):

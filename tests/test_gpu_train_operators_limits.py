@@ -1,0 +1,113 @@
+"""GPU tests of the training operators of the block's FFN half where their
+arguments end: gates and products across float32's range, moments whose codes
+are at the ends of the 8-bit formats, states that do not fit, tensors that
+overlap, every tile shape against the formula with its roundings.
+
+Bars as in test_gpu_train_operators.py: e = 2^-24 relative to the value for a
+float32 rounding, 2^-8 for one to bf16, 2^-10 for what the gated FFN keeps
+between its passes; (n + 2) e times the sum of magnitudes for a sum."""
+import numpy as np
+import pytest
+
+from oracle import train_operators as O
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+E32, E16, EKEPT = 2.0 ** -24, 2.0 ** -8, 2.0 ** -10
+
+
+def _train():
+    from paper_2609_15160_amd import train
+    return train
+
+
+def _say(*what):
+    print("[train-op]", *what, flush=True)
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _bf16(v):
+    """The values as bf16, and what those stand for."""
+    t = torch.tensor(v, dtype=torch.float64).to(torch.bfloat16)
+    return t, t.double().numpy()
+
+
+def _close(got, want, bound, what):
+    got = _np(got)
+    over = np.abs(got - want) - bound
+    assert got.shape == want.shape and np.all(over <= 0), (what, np.unravel_index(np.argmax(over), over.shape),
+                                                           got.ravel()[np.argmax(over)], want.ravel()[np.argmax(over)])
+
+
+# ---------------------------------------------------------------------------
+# Gated FFN: the range of what it keeps
+# ---------------------------------------------------------------------------
+
+# gates and ups of bf16 operands: ordinary, past 2^32, near the top, below 2^-30 and far below
+GATES = [0.5, -2.0, 3.0, -9.0, 1e10, 1e20, 1e33, 1.0, 2.0, 5.0, 1e-13, 2.0 ** -28, 2.0 ** -34, 2.0 ** -42, 1e-30, -1e-12]
+UPS = [1.5, 0.25, -4.0, 8.0, 1.0, 1.0, 1.0, 1e10, -1e20, 3e33, 1e-13, 2.0 ** -29, 2.0 ** -33, 1.0, 1e-7, 1e-12]
+
+
+@pytest.mark.parametrize("n,f", [
+    (1, 64), (17, 64), (333, 192),
+    (2000, 2688),  # gate/up and da on 128 x 128 tiles
+    (4096, 2816),  # on 256 x 256 tiles
+])
+def test_ffn_gradients_over_the_range_of_bf16(n, f):
+    """Column c's gate and up are x's first element times one weight each, W_down passes every 64th column on, dy is a
+    power of two: the gradients are sums of dg and du themselves, whatever the column's magnitude.
+
+    An element of dg or du is off by its own rounding, that of what was kept, and 2^-18 for the float32 arithmetic of
+    the activation (1 - s next to 1 times a gate of 10: 10 2^-24, and exp and reciprocal in their last bits)."""
+    train = _train()
+    d = 64
+    _say("ffn range", n, d, f)
+    gate, up = _bf16(np.resize(GATES, f))[0], _bf16(np.resize(UPS, f))[0]
+    x = torch.zeros(n, d, dtype=torch.bfloat16)
+    x[:, 0] = 1.0
+    x[1::2, 0] = -1.0  # the negative gates too
+    wgu = torch.zeros(2 * f, d, dtype=torch.bfloat16)
+    wgu[:f, 0], wgu[f:, 0] = gate, up
+    wd = torch.eye(64, dtype=torch.bfloat16).repeat(1, f // 64).contiguous()
+    dy = torch.full((n, d), 2.0 ** -6, dtype=torch.bfloat16)
+    leaves = [t.cuda().requires_grad_() for t in (x, wgu, wd)]
+    y = train.ffn(*leaves)
+    got = torch.autograd.grad(y, leaves, dy.cuda())
+    X, W, D, G = (t.double().numpy() for t in (x, wgu, wd, dy))
+    A = np.abs
+    with np.errstate(over="ignore"):
+        g, u = X @ W[:f].T, X @ W[f:].T
+        s = O.sigmoid(g)
+        a = g * s * u
+        da = G @ D
+        dgu = np.concatenate([da * u * s * (1 + g * (1 - s)), da * g * s], 1)
+        want = [dgu @ W, dgu.T @ X, G.T @ a]
+    assert all(np.isfinite(w).all() for w in want)
+    ea, ed = A(a) * (E16 + 2.0 ** -18), A(dgu) * (E16 + EKEPT + 2.0 ** -18)
+    bounds = [ed @ A(W) + (2 * f + 2) * E32 * (A(dgu) @ A(W)), ed.T @ A(X) + (n + 2) * E32 * (A(dgu).T @ A(X)),
+              A(G).T @ ea + (n + 2) * E32 * (A(G).T @ A(a))]
+    _close(y, a @ D.T, 1.01 * (ea @ A(D).T + (f + 2) * E32 * (A(a) @ A(D).T) + E16 * A(a @ D.T)) + 1e-37, "y")
+    for name, t, w, b in zip(("dx", "dw_gate_up", "dw_down"), got, want, bounds):
+        _close(t, w, 1.01 * (b + E16 * A(w)) + 1e-37, name)
+
+
+def test_ffn_infinities_reach_the_gradients():
+    """An infinite up value gives infinite gradients, a NaN gives NaN, and neither leaves its columns."""
+    train = _train()
+    n, d, f = 3, 64, 64
+    x = torch.zeros(n, d, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = 1.0
+    wgu = torch.zeros(2 * f, d, dtype=torch.bfloat16, device="cuda")
+    wgu[:, 0] = 0.5
+    wgu[f + 1, 0], wgu[f + 2, 0], wgu[f + 3, 0] = float("inf"), float("-inf"), float("nan")
+    wd = torch.eye(64, dtype=torch.bfloat16, device="cuda")
+    leaves = [t.requires_grad_() for t in (wgu, wd)]
+    y = train.ffn(x, *leaves)
+    dwgu, = torch.autograd.grad(y, leaves[:1], torch.ones_like(y))
+    assert dwgu[1, 0] == float("inf") and dwgu[2, 0] == float("-inf") and torch.isnan(dwgu[3, 0])
+    rest = [k for k in range(f) if k not in (1, 2, 3)]
+    assert torch.isfinite(dwgu[:f][rest]).all() and torch.isfinite(dwgu[f:]).all()
