@@ -269,15 +269,17 @@ class _NoSecond(torch.autograd.Function):
 
 
 def _first_order(backward):
-    """A backward pass without one of its own: where a graph of it is built (create_graph), differentiating that is
-    refused."""
+    """A backward pass without one of its own, backward(ctx, saved tensors, *grads): where a graph of it is built
+    (create_graph), differentiating that is refused.  The saved tensors are unpacked here, once: a recomputed one
+    (checkpointing) is there for one taking only."""
     @functools.wraps(backward)
     def run(ctx, *grads):
+        saved = ctx.saved_tensors
         if not torch.is_grad_enabled():
-            return backward(ctx, *grads)
+            return backward(ctx, saved, *grads)
         with torch.no_grad():
-            out = backward(ctx, *grads)
-        return _NoSecond.apply(len(out), *out, *(t for t in (*ctx.saved_tensors, *grads) if t is not None))
+            out = backward(ctx, saved, *grads)
+        return _NoSecond.apply(len(out), *out, *(t for t in (*saved, *grads) if t is not None))
     return run
 
 
@@ -296,8 +298,8 @@ class _RmsNorm(torch.autograd.Function):
 
     @staticmethod
     @_first_order
-    def backward(ctx, dy):
-        x, gamma, group, rstd = ctx.saved_tensors
+    def backward(ctx, saved, dy):
+        x, gamma, group, rstd = saved
         rows, d = x.shape
         groups = 0 if gamma is None else gamma.numel() // d
         dy = _aligned(dy)
@@ -366,8 +368,8 @@ class _Ffn(torch.autograd.Function):
 
     @staticmethod
     @_first_order
-    def backward(ctx, dy):
-        x, w_gate_up, w_down, kept = ctx.saved_tensors
+    def backward(ctx, saved, dy):
+        x, w_gate_up, w_down, kept = saved
         rows, d = x.shape
         f = w_down.shape[1]
         dy = _aligned(dy)

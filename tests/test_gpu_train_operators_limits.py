@@ -111,3 +111,23 @@ def test_ffn_infinities_reach_the_gradients():
     assert dwgu[1, 0] == float("inf") and dwgu[2, 0] == float("-inf") and torch.isnan(dwgu[3, 0])
     rest = [k for k in range(f) if k not in (1, 2, 3)]
     assert torch.isfinite(dwgu[:f][rest]).all() and torch.isfinite(dwgu[f:]).all()
+
+
+def test_gradients_under_checkpointing():
+    """Recomputed in the backward pass, with and without a graph of it: the gradients of a plain pass, to the bit."""
+    from torch.utils.checkpoint import checkpoint
+    train = _train()
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    new = lambda *s, scale=1.0: (torch.randn(*s, generator=gen, device="cuda") * scale).requires_grad_()  # noqa: E731
+    leaves = [new(70, 128), new(1, 128, scale=0.2), new(2 * 192, 128, scale=0.1), new(128, 192, scale=0.1)]
+
+    def block(x, gamma, wgu, wd):
+        return train.ffn(train.rms_norm(x, gamma), wgu, wd)
+
+    y = block(*leaves)
+    dy = torch.randn(y.shape, generator=gen, device="cuda")
+    want = torch.autograd.grad(y, leaves, dy)
+    for graph in (False, True):
+        y = checkpoint(block, *leaves, use_reentrant=False)
+        for a, b in zip(torch.autograd.grad(y, leaves, dy, create_graph=graph), want):
+            assert torch.equal(a, b)

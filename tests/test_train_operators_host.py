@@ -3,7 +3,11 @@ wrappers do around the kernels."""
 import os
 import subprocess
 
-from paper_2609_15160_amd import tlf
+import pytest
+import torch
+import torch.utils.checkpoint
+
+from paper_2609_15160_amd import tlf, train
 
 INC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
 
@@ -20,3 +24,46 @@ def test_kept_bytes_match_the_header(tmp_path):
     for n, (t, rows, f) in zip(got, cases):
         bits = (rows + 15) // 16 * 16 * f * 2 * (18 if t == tlf.DTYPE_BF16 else 32)
         assert n == tlf.ffn_kept_bytes(t, rows, f) == bits // 8 and n % 16 == 0
+
+
+@pytest.fixture
+def no_kernels(monkeypatch):
+    """The autograd functions without their kernels: what they compute is left as it is allocated."""
+    monkeypatch.setattr(train, "_run", lambda *a: None)
+    monkeypatch.setattr(train, "_workspace", lambda *a, **k: (None, 0))
+
+
+def _operators():
+    x = torch.ones(3, 64, requires_grad=True)
+    gamma, wgu, wd = torch.ones(1, 64), torch.ones(128, 64), torch.ones(64, 64)
+    yield x, lambda t: train._RmsNorm.apply(t, gamma, None, 1e-5, torch.float32, True)
+    yield x, lambda t: train._Ffn.apply(t, wgu, wd, True)
+
+
+def test_gradients_with_a_graph_under_checkpointing(no_kernels):
+    """A recomputed activation can be taken once: a first gradient that keeps a graph takes it no second time."""
+    for x, op in _operators():
+        y = torch.utils.checkpoint.checkpoint(op, x, use_reentrant=False)
+        dx, = torch.autograd.grad(y, x, torch.ones_like(y), create_graph=True)
+        assert dx.shape == x.shape and dx.requires_grad
+        with pytest.raises(RuntimeError, match="gradients of gradients"):
+            torch.autograd.grad(dx, x, torch.ones_like(dx))
+
+
+@pytest.mark.parametrize("create_graph", [False, True])
+def test_saved_tensors_are_unpacked_once(no_kernels, create_graph):
+    for x, op in _operators():
+        packed, unpacked = [], []
+
+        def pack(t):
+            packed.append(t)
+            return t
+
+        def unpack(t):
+            unpacked.append(t)
+            return t
+
+        with torch.autograd.graph.saved_tensors_hooks(pack, unpack):
+            y = op(x)
+        torch.autograd.grad(y, x, torch.ones_like(y), create_graph=create_graph)
+        assert len(packed) == len(unpacked) >= 3
