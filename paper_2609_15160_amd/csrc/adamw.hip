@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
     for (int r = 0; r < 4; ++r) {
       mt[r] = scaled(m1[r], mi, 448.f);
       vt[r] = scaled(v1[r], vi, 57344.f);
-      if (vt[r] > 0.f && vt[r] < 0x1p-16f) vt[r] = 0x1p-16f;
+      if (v1[r] > 0.0 && vi > 0.0 && vt[r] < 0x1p-16f) vt[r] = 0x1p-16f;  // by v1: vt may have become zero in float32
     }
     mc = __builtin_amdgcn_cvt_pk_fp8_f32(mt[0], mt[1], 0, false);
     mc = __builtin_amdgcn_cvt_pk_fp8_f32(mt[2], mt[3], mc, true);

@@ -131,3 +131,34 @@ def test_gradients_under_checkpointing():
         y = checkpoint(block, *leaves, use_reentrant=False)
         for a, b in zip(torch.autograd.grad(y, leaves, dy, create_graph=graph), want):
             assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------------------
+# AdamW
+# ---------------------------------------------------------------------------
+
+def _fresh8(n):
+    """Fresh 8-bit moments of n elements."""
+    codes = lambda t: torch.zeros(n, dtype=torch.uint8, device="cuda").view(t)  # noqa: E731
+    scales = lambda: torch.zeros(-(-n // O.BLOCK), device="cuda")  # noqa: E731
+    return (codes(torch.float8_e4m3fn), scales()), (codes(torch.float8_e5m2), scales())
+
+
+def test_adamw_smallest_second_moments():
+    """Gradients so far below their block's largest that v over the scale is none in float32 keep the smallest code."""
+    train = _train()
+    n = 3 * 256 + 5
+    g = np.zeros(n, np.float32)
+    g[0], g[1:200] = 1.0, 1e-26
+    g[256], g[257:400] = 1e15, 1e-30
+    g[512], g[513:600] = 1e-3, 1e-45
+    g[768], g[769:] = 1.0, 1e-38  # the last, short block
+    p, (m, v) = torch.zeros(n, device="cuda"), _fresh8(n)
+    _say("adamw tiny", n)
+    train.adamw_([p], [torch.from_numpy(g).cuda()], [m], [v], 1, lr=1e-3)
+    _, m1, v1 = O.adamw(np.zeros(n), g, np.zeros(n), np.zeros(n), 1, 1e-3, (0.9, 0.95), 1e-8, 0.0)
+    for got, new, which in ((m, m1, "m"), (v, v1, "v")):
+        codes, scales = O.encode(new, which)
+        assert np.array_equal(got[1].cpu().numpy(), scales), which
+        assert torch.equal(got[0].cpu().view(torch.uint8), codes.view(torch.uint8)), which
+    assert torch.equal(v[0].float() > 0, torch.from_numpy(g > 0).cuda())
