@@ -120,10 +120,12 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
   }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
+// Magnitudes are compared as their bits: NaN is above infinity and is not lost.
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ float wave_max(unsigned v) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, shfl_xor(v, o));
-  return v;
+  for (int o = 32; o > 0; o >>= 1) v = max(v, shfl_xor(v, o));
+  return __uint_as_float(v);
 }
 
 // v / s, at most `most` in magnitude (s may have lost bits where it is subnormal)
@@ -185,19 +187,19 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
     const f32x2 v01 = __builtin_amdgcn_cvt_pk_f32_bf8(vc, false), v23 = __builtin_amdgcn_cvt_pk_f32_bf8(vc, true);
     const float mo[4] = {m01[0], m01[1], m23[0], m23[1]}, vo[4] = {v01[0], v01[1], v23[0], v23[1]};
     double m1[4], v1[4];
-    float mm = 0.f, vm = 0.f;
+    unsigned mtop = 0, vtop = 0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const double g = g4[r];
       m1[r] = moment(a.b1, (double)mo[r] * ms, c1, g);
       v1[r] = moment(a.b2, (double)vo[r] * vs, c2, g * g);
-      mm = fmaxf(mm, fabsf((float)m1[r]));
-      vm = fmaxf(vm, (float)v1[r]);
+      mtop = max(mtop, magnitude((float)m1[r]));
+      vtop = max(vtop, magnitude((float)v1[r]));
       p4[r] = update(p4[r], (float)m1[r], (float)v1[r], t, a.eps);
     }
-    mm = (float)((double)wave_max(mm) / 448.0);
-    vm = (float)((double)wave_max(vm) / 57344.0);
-    const double mi = mm > 0.f ? inverse(mm) : 0.0, vi = vm > 0.f ? inverse(vm) : 0.0;
+    // an infinite or NaN scale spoils its block: every code times it is infinite or NaN
+    const float mm = (float)((double)wave_max(mtop) / 448.0), vm = (float)((double)wave_max(vtop) / 57344.0);
+    const double mi = mm > 0.f && mm < INFINITY ? inverse(mm) : 0.0, vi = vm > 0.f && vm < INFINITY ? inverse(vm) : 0.0;
     float mt[4], vt[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {

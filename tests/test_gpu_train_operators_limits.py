@@ -162,3 +162,32 @@ def test_adamw_smallest_second_moments():
         assert np.array_equal(got[1].cpu().numpy(), scales), which
         assert torch.equal(got[0].cpu().view(torch.uint8), codes.view(torch.uint8)), which
     assert torch.equal(v[0].float() > 0, torch.from_numpy(g > 0).cuda())
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf"), 1e38])
+def test_adamw_spoilt_gradients_spoil_their_block(bad):
+    """8 bits: one gradient that is not finite, or whose square is none in float32, makes the block's scale of the
+    second moments (and, unless finite, of the first) infinite or NaN, as the formula's largest magnitude; the other
+    blocks go on, and the next step shows NaN in the block."""
+    train = _train()
+    n = 3 * 256 + 100
+    rng = np.random.default_rng(41)
+    g = (rng.standard_normal(n) * 1e-3).astype(np.float32)
+    g[256 + 77] = bad
+    g[768 + 99] = bad  # the last, short block
+    p, (m, v) = torch.zeros(n, device="cuda"), _fresh8(n)
+    _say("adamw spoilt", bad)
+    train.adamw_([p], [torch.from_numpy(g).cuda()], [m], [v], 1, lr=1e-3)
+    with np.errstate(all="ignore"):
+        _, m1, v1 = O.adamw(np.zeros(n), g, np.zeros(n), np.zeros(n), 1, 1e-3, (0.9, 0.95), 1e-8, 0.0)
+        for got, new, which in ((m, m1, "m"), (v, v1, "v")):
+            codes, scales = O.encode(new, which)
+            assert np.array_equal(got[1].cpu().numpy(), scales, equal_nan=True), which
+            want = O.decode(codes, scales)
+            have = O.decode(got[0].cpu(), got[1].cpu().numpy())
+            assert np.array_equal(have, want, equal_nan=True), which
+    whole = torch.ones(n, dtype=torch.bool, device="cuda")
+    whole[256:512] = whole[768:] = False
+    assert not torch.isfinite(v[1][1]) and not torch.isfinite(v[1][3])
+    train.adamw_([p], [torch.zeros(n, device="cuda")], [m], [v], 2, lr=1e-3)
+    assert torch.isfinite(p[whole]).all() and torch.isnan(p[~whole]).all()
