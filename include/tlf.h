@@ -510,7 +510,9 @@ typedef struct tlf_adamw_tensor {
  * keeps at least the smallest code above zero.  A gradient that is not finite,
  * or whose square is none in float32, spoils the moments of its element (8 bits:
  * of its block).
- *   h_tensors: host array, read during the call; no tensor appears twice.
+ *   h_tensors: host array, read during the call.  Parameters, copies, moments
+ *   and scales overlap nothing else of the call (TLF_E_INVALID_ARG), gradients
+ *   may overlap each other.
  * The step counts and rates are values of the call: a captured call replays them. */
 int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
               void* stream);

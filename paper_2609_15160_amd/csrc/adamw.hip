@@ -20,6 +20,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 #include "common.h"
 #include "tlf.h"
 
@@ -251,6 +255,41 @@ int check(const tlf_adamw_tensor& t) {
   return t.n > ((int64_t)1 << 35) ? TLF_E_UNSUPPORTED : TLF_OK;
 }
 
+// What the step updates must overlap nothing else of the call, since the
+// workgroups run in no order; gradients may overlap each other.
+int check_overlap(const tlf_adamw_tensor* tensors, int32_t count) {
+  struct Range {
+    uintptr_t begin, end;
+    bool updated;
+  };
+  const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[7 * (size_t)count + 1]);
+  if (!ranges) return TLF_E_HIP;
+  size_t n = 0;
+  for (int i = 0; i < count; ++i) {
+    const tlf_adamw_tensor& t = tensors[i];
+    auto add = [&](const void* p, int64_t bytes, bool updated) {
+      if (p && bytes > 0) ranges[n++] = Range{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, updated};
+    };
+    const int64_t moment = t.state_bits / 8, scales = t.state_bits == 8 ? (t.n + kBlock - 1) / kBlock : 0;
+    add(t.d_param, t.n * 4, true);
+    add(t.d_copy, t.n * 2, true);
+    add(t.d_grad, t.n * (t.grad_dtype == TLF_DTYPE_BF16 ? 2 : 4), false);
+    add(t.d_m, t.n * moment, true);
+    add(t.d_v, t.n * moment, true);
+    add(t.d_m_scale, scales * 4, true);
+    add(t.d_v_scale, scales * 4, true);
+  }
+  std::sort(ranges.get(), ranges.get() + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t any = 0, updated = 0;  // where the ranges so far end, and those that are updated
+  for (size_t k = 0; k < n; ++k) {
+    const Range& r = ranges[k];
+    if (r.begin < (r.updated ? any : updated)) return TLF_E_INVALID_ARG;
+    any = std::max(any, r.end);
+    if (r.updated) updated = std::max(updated, r.end);
+  }
+  return TLF_OK;
+}
+
 }  // namespace
 
 }  // namespace tlf
@@ -265,6 +304,8 @@ extern "C" int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, doubl
     const int st = check(h_tensors[i]);
     if (st != TLF_OK) return st;
   }
+  const int st = check_overlap(h_tensors, count);
+  if (st != TLF_OK) return st;
   for (int bits : {32, 8}) {
     AdamArgs a{};
     a.b1 = beta1;

@@ -413,6 +413,12 @@ def _moment(state, like, dtype8, name):
     return t, s
 
 
+def _given_twice(table) -> bool:
+    """Whether one address is updated twice by the tensors of an adamw_ call."""
+    at = [a for t in table if t.n for a in (t.d_param, t.d_copy, t.d_m, t.d_v, t.d_m_scale, t.d_v_scale) if a]
+    return len(set(at)) < len(at)
+
+
 def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.95), eps: float = 1e-8,
            weight_decay=0.0, copies=None) -> None:
     """One AdamW step over many tensors, in place (tlf_adamw; few launches for all of them).
@@ -425,6 +431,9 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
                  captured into a graph is refused: its replays would repeat the corrections of one step
     weight_decay one value or one for each tensor
     copies       bfloat16 tensors that receive the updated parameters rounded, or None
+
+    What is updated overlaps nothing else of the call; gradients may overlap each other.  eps is at least the smallest
+    normal float32.
     """
     n = len(params)
     steps = [step] * n if isinstance(step, int) else list(step)
@@ -435,7 +444,7 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
     if n == 0:
         return
     table = (tlf.AdamwTensor * n)()
-    dev, updated = params[0].device, set()
+    dev = params[0].device
     for k, (p, g, c) in enumerate(zip(params, grads, copies)):
         if p.dtype != torch.float32 or not p.is_cuda or not p.is_contiguous():
             raise ValueError("adamw_: parameters are contiguous float32 CUDA tensors")
@@ -451,17 +460,19 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
         for t in (p, g, c, m, v, ms, vs):
             if t is not None and t.device != dev:
                 raise ValueError("adamw_: tensors on one device expected")
-        at = p.data_ptr(), m.data_ptr(), v.data_ptr()
-        updated.update(at if p.numel() else ())
-        table[k] = tlf.AdamwTensor(at[0], c.data_ptr() if c is not None else None, g.data_ptr(), at[1], at[2], ms.data_ptr() if ms is not None else None,
+        table[k] = tlf.AdamwTensor(p.data_ptr(), c.data_ptr() if c is not None else None, g.data_ptr(), m.data_ptr(),
+                                   v.data_ptr(), ms.data_ptr() if ms is not None else None,
                                    vs.data_ptr() if vs is not None else None, p.numel(), steps[k], decays[k],
                                    _DTYPE[g.dtype], 32 if ms is None else 8)
-    if len(updated) != sum(3 for p in params if p.numel()):
-        raise ValueError("adamw_: a parameter or moment appears twice")
     with torch.cuda.device(dev):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("adamw_: the step number and rates are values and cannot be captured into a graph")
-    _run(tlf.load().tlf_adamw, dev, table, n, lr, betas[0], betas[1], eps)
+    try:
+        _run(tlf.load().tlf_adamw, dev, table, n, lr, betas[0], betas[1], eps)
+    except tlf.TlfError as e:
+        if e.status == tlf.E_INVALID_ARG and _given_twice(table):
+            raise ValueError("adamw_: a parameter, copy, moment or scale appears twice") from None
+        raise
     # a graph that saved a parameter or copy for its backward pass has to notice the update
     torch.autograd.graph.increment_version([*params, *(c for c in copies if c is not None)])
 

@@ -191,3 +191,35 @@ def test_adamw_spoilt_gradients_spoil_their_block(bad):
     assert not torch.isfinite(v[1][1]) and not torch.isfinite(v[1][3])
     train.adamw_([p], [torch.zeros(n, device="cuda")], [m], [v], 2, lr=1e-3)
     assert torch.isfinite(p[whole]).all() and torch.isnan(p[~whole]).all()
+
+
+def test_adamw_neighbours_in_one_buffer_and_shared_gradients():
+    """Tensors that touch without overlapping and gradients that two tensors share are as good as separate ones."""
+    train = _train()
+    rng = np.random.default_rng(43)
+    new = lambda n: torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda()  # noqa: E731
+    room, g = new(6 * 1000), new(1000)
+    one = [t.abs() for t in room.split(1000)]
+    room.abs_()
+    parts = list(room.split(1000))
+    for p in (one, parts):
+        train.adamw_(p[:2], [g, g], p[2:4], p[4:], 3, lr=1e-2)
+    assert all(torch.equal(a, b) for a, b in zip(one, parts))
+    with pytest.raises((ValueError, RuntimeError)):
+        train.adamw_([room[:1000], room[999:1999]], [g, g], [new(1000), new(1000)], [new(1000), new(1000)], 1, lr=1e-3)
+    assert all(torch.equal(a, b) for a, b in zip(one, parts))
+
+
+def test_adamw_refuses_copies_and_scales_given_twice():
+    train = _train()
+    new = lambda: torch.ones(300, device="cuda")  # noqa: E731
+    copy = torch.ones(300, dtype=torch.bfloat16, device="cuda")
+    p, q = new(), new()
+    with pytest.raises(ValueError, match="twice"):
+        train.adamw_([p, q], [new(), new()], [new(), new()], [new(), new()], 1, lr=1e-3, copies=[copy, copy])
+    (m, v), (m2, v2) = _fresh8(300), _fresh8(300)
+    with pytest.raises(ValueError, match="twice"):
+        train.adamw_([p, q], [new(), new()], [m, (m2[0], m[1])], [v, v2], 1, lr=1e-3)
+    with pytest.raises(ValueError, match="twice"):
+        train.adamw_([p], [new()], [m], [(v[0], m[1])], 1, lr=1e-3)
+    assert all(torch.equal(t.float(), torch.ones(300, device="cuda")) for t in (p, q, copy))

@@ -67,3 +67,43 @@ def test_saved_tensors_are_unpacked_once(no_kernels, create_graph):
             y = op(x)
         torch.autograd.grad(y, x, torch.ones_like(y), create_graph=create_graph)
         assert len(packed) == len(unpacked) >= 3
+
+
+# ---------------------------------------------------------------------------
+# AdamW: overlapping tensors are refused before any device work
+# ---------------------------------------------------------------------------
+
+def _at(tensor, buffer, offset=0):
+    return ((tensor * 8 + buffer + 1) << 16) + offset
+
+
+def _buffers(tensor):
+    """A tensor of 1000 elements, each of its buffers 64 KiB from the next."""
+    names = ("d_param", "d_copy", "d_grad", "d_m", "d_v", "d_m_scale", "d_v_scale")
+    return dict({name: _at(tensor, i) for i, name in enumerate(names)}, n=1000, step=1, weight_decay=0.0,
+                grad_dtype=tlf.DTYPE_F32, state_bits=8)
+
+
+def _step(*tensors):
+    table = (tlf.AdamwTensor * len(tensors))(*(tlf.AdamwTensor(**{**_buffers(k), **a}) for k, a in enumerate(tensors)))
+    return tlf.load().tlf_adamw(table, len(tensors), 1e-3, 0.9, 0.95, 1e-8, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(d_param=_at(0, 0)), dict(d_copy=_at(0, 1)), dict(d_m=_at(0, 3)), dict(d_v=_at(0, 4)), dict(d_m_scale=_at(0, 5)),
+    dict(d_v_scale=_at(0, 6)),                                            # the same buffer in two tensors
+    dict(d_param=_at(0, 0, 3996)), dict(d_copy=_at(0, 1, 1998)), dict(d_m=_at(0, 3, 999)), dict(d_v=_at(0, 4, -999)),
+    dict(d_m_scale=_at(0, 5, 12)),                                        # their last or first element
+    dict(d_m_scale=_at(1, 6)), dict(d_copy=_at(1, 0)), dict(d_m=_at(1, 4, 500)),  # within one tensor
+    dict(d_grad=_at(0, 0)), dict(d_grad=_at(1, 0)), dict(d_grad=_at(0, 1, 1000)),  # a gradient that an update overwrites
+])
+def test_adamw_refuses_overlapping_buffers(kw):
+    assert _step({}, kw) == tlf.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw,twice", [({}, False), (dict(d_copy=_at(0, 1)), True), (dict(d_m_scale=_at(0, 5)), True),
+                                      (dict(d_v_scale=_at(1, 5)), True), (dict(d_grad=_at(0, 2)), False),
+                                      (dict(d_copy=_at(0, 1), n=0), False)])
+def test_adamw_wrapper_names_a_buffer_given_twice(kw, twice):
+    table = (tlf.AdamwTensor * 2)(*(tlf.AdamwTensor(**{**_buffers(k), **a}) for k, a in enumerate(({}, kw))))
+    assert train._given_twice(table) is twice
