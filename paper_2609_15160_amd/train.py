@@ -537,11 +537,13 @@ class AdamW:
     def load_state_dict(self, state: dict) -> None:
         if state["state_bits"] != self.state_bits or len(state["steps"]) != len(self.params):
             raise ValueError("AdamW: the state is of other parameters or another state_bits")
-        self.steps = list(state["steps"])
-        flat = lambda v: [t for s in v for t in (s if isinstance(s, tuple) else (s,)) if t is not None]  # noqa: E731
+        parts = lambda s: () if s is None else tuple(s) if isinstance(s, (tuple, list)) else (s,)  # noqa: E731
+        steps, pairs = [int(k) for k in state["steps"]], []
         for key in ("masters", "exp_avgs", "exp_avg_sqs"):
-            mine, given = flat(getattr(self, key)), flat(state[key])
-            if [(t.shape, t.dtype) for t in mine] != [(t.shape, t.dtype) for t in given]:
+            mine, given = [[parts(s) for s in v] for v in (getattr(self, key), state[key])]
+            if [[(t.shape, t.dtype) for t in s] for s in mine] != [[(t.shape, t.dtype) for t in s] for s in given]:
                 raise ValueError(f"AdamW: {key} do not fit the parameters")
-            for t, s in zip(mine, given):
-                t.copy_(s)
+            pairs += [(t, g) for a, b in zip(mine, given) for t, g in zip(a, b)]
+        for t, g in pairs:  # all of it fits
+            t.copy_(g)
+        self.steps = steps

@@ -107,3 +107,46 @@ def test_adamw_refuses_overlapping_buffers(kw):
 def test_adamw_wrapper_names_a_buffer_given_twice(kw, twice):
     table = (tlf.AdamwTensor * 2)(*(tlf.AdamwTensor(**{**_buffers(k), **a}) for k, a in enumerate(({}, kw))))
     assert train._given_twice(table) is twice
+
+
+# ---------------------------------------------------------------------------
+# AdamW's state
+# ---------------------------------------------------------------------------
+
+class _Cuda(torch.Tensor):
+    """A host tensor that passes for a device one where nothing reaches a device."""
+    is_cuda = True
+
+
+def _optimizer(bits=32):
+    leaves = [torch.ones(300, dtype=torch.bfloat16), torch.ones(7)]
+    return train.AdamW([t.as_subclass(_Cuda).requires_grad_() for t in leaves], lr=1e-3, state_bits=bits)
+
+
+def _flat(opt):
+    pairs = [t for v in (opt.masters, opt.exp_avgs, opt.exp_avg_sqs) for s in v for t in (s if isinstance(s, tuple) else (s,))]
+    return [t for t in pairs if t is not None]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("key", ["steps", "masters", "exp_avgs", "exp_avg_sqs"])
+def test_a_refused_state_is_not_half_loaded(bits, key):
+    opt, other = _optimizer(bits), _optimizer(bits)
+    other.steps = [3, 4]
+    for t in _flat(other):
+        t.view(torch.uint8).fill_(1)
+    state = other.state_dict()
+    if key == "steps":
+        state[key] = [3]
+    elif key == "masters":
+        state[key] = [None, state[key][0]]  # the float32 leaf's place instead of the bfloat16 one's
+    else:
+        state[key] = [state[key][0], (torch.zeros(9) if bits == 32 else (state[key][1][0], torch.zeros(2)))]
+    before = [t.clone() for t in _flat(opt)]
+    with pytest.raises(ValueError):
+        opt.load_state_dict(state)
+    assert opt.steps == [0, 0]
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(_flat(opt), before))
+    opt.load_state_dict(other.state_dict())
+    assert opt.steps == [3, 4]
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(_flat(opt), _flat(other)))
