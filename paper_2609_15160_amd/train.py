@@ -483,7 +483,8 @@ class AdamW:
     params: contiguous float32 or bfloat16 CUDA leaves.  A bfloat16 one is trained through a float32 master that the
     optimizer holds (masters[k]); the leaf receives it rounded.  step() updates every parameter that has a gradient,
     each with its own count of steps.  weight_decay is one value or one for each parameter.  lr may be set between
-    steps.  state_dict and load_state_dict carry the masters, moments and counts."""
+    steps.  state_dict and load_state_dict carry the masters, moments and counts; load_state_dict sets the bfloat16
+    leaves to the masters rounded and leaves float32 ones as they are."""
 
     def __init__(self, params, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0,
                  state_bits: int = 32):
@@ -546,4 +547,7 @@ class AdamW:
             pairs += [(t, g) for a, b in zip(mine, given) for t, g in zip(a, b)]
         for t, g in pairs:  # all of it fits
             t.copy_(g)
+        for p, m in zip(self.params, self.masters):
+            if m is not None:
+                p.copy_(m)
         self.steps = steps

@@ -150,3 +150,13 @@ def test_a_refused_state_is_not_half_loaded(bits, key):
     opt.load_state_dict(other.state_dict())
     assert opt.steps == [3, 4]
     assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(_flat(opt), _flat(other)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_loaded_state_reaches_the_bfloat16_leaves(bits):
+    opt, other = _optimizer(bits), _optimizer(bits)
+    other.masters[0].copy_(torch.linspace(-3, 3, 300))
+    opt.load_state_dict(other.state_dict())
+    assert torch.equal(opt.masters[0], other.masters[0])
+    assert torch.equal(opt.params[0].detach(), opt.masters[0].to(torch.bfloat16))
+    assert torch.equal(opt.params[1].detach(), torch.ones(7))  # a float32 leaf is the caller's to load
