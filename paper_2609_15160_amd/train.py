@@ -477,14 +477,21 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
     torch.autograd.graph.increment_version([*params, *(c for c in copies if c is not None)])
 
 
+def _writes(t: torch.Tensor):
+    """How often t was written, as autograd counts it (inference tensors are not counted)."""
+    return None if t.is_inference() else t._version
+
+
 class AdamW:
     """AdamW over leaf tensors, with moments of 32 or 8 bits.
 
     params: contiguous float32 or bfloat16 CUDA leaves.  A bfloat16 one is trained through a float32 master that the
-    optimizer holds (masters[k]); the leaf receives it rounded.  step() updates every parameter that has a gradient,
-    each with its own count of steps.  weight_decay is one value or one for each parameter.  lr may be set between
-    steps.  state_dict and load_state_dict carry the masters, moments and counts; load_state_dict sets the bfloat16
-    leaves to the masters rounded and leaves float32 ones as they are."""
+    optimizer holds (masters[k]); the leaf receives it rounded.  Elements that are written into such a leaf afterwards
+    go into the master at the next step or state_dict, but for writes through its .data, which autograd does not count
+    and the step overwrites.  step() updates every parameter that has a gradient, each with its own count of steps.
+    weight_decay is one value or one for each parameter.  lr may be set between steps.  state_dict and load_state_dict
+    carry the masters, moments and counts; load_state_dict sets the bfloat16 leaves to the masters rounded and leaves
+    float32 ones as they are."""
 
     def __init__(self, params, lr: float, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay=0.0,
                  state_bits: int = 32):
@@ -504,6 +511,7 @@ class AdamW:
         self.exp_avgs = [self._zeros(p, torch.float8_e4m3fn) for p in self.params]
         self.exp_avg_sqs = [self._zeros(p, torch.float8_e5m2) for p in self.params]
         self.steps = [0] * n
+        self._written = [_writes(p) for p in self.params]  # as far as the masters know the leaves
 
     def _zeros(self, p, dtype8):
         if self.state_bits == 32:
@@ -511,9 +519,17 @@ class AdamW:
         return (torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(dtype8),
                 torch.zeros(-(-p.numel() // tlf.ADAMW_BLOCK), dtype=torch.float32, device=p.device))
 
+    def _take_written(self, have) -> None:
+        for k in have:
+            p, m = self.params[k].detach(), self.masters[k]
+            if m is not None and _writes(p) != self._written[k]:
+                m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))
+                self._written[k] = _writes(p)
+
     @torch.no_grad()
     def step(self) -> None:
         have = [k for k, p in enumerate(self.params) if p.grad is not None]
+        self._take_written(have)
         by = {}
         for k in have:
             by.setdefault(self.params[k].device, []).append(k)
@@ -525,12 +541,15 @@ class AdamW:
                    [self.steps[k] + 1 for k in at], self.lr, self.betas, self.eps, pick(self.weight_decay), copies)
             for k in at:
                 self.steps[k] += 1
+                self._written[k] = _writes(self.params[k])
 
     def zero_grad(self) -> None:
         for p in self.params:
             p.grad = None
 
+    @torch.no_grad()
     def state_dict(self) -> dict:
+        self._take_written(range(len(self.params)))
         return {"steps": list(self.steps), "masters": list(self.masters), "exp_avgs": list(self.exp_avgs),
                 "exp_avg_sqs": list(self.exp_avg_sqs), "state_bits": self.state_bits}
 
@@ -547,7 +566,8 @@ class AdamW:
             pairs += [(t, g) for a, b in zip(mine, given) for t, g in zip(a, b)]
         for t, g in pairs:  # all of it fits
             t.copy_(g)
-        for p, m in zip(self.params, self.masters):
+        for k, (p, m) in enumerate(zip(self.params, self.masters)):
             if m is not None:
                 p.copy_(m)
+                self._written[k] = _writes(p)
         self.steps = steps

@@ -223,3 +223,23 @@ def test_adamw_refuses_copies_and_scales_given_twice():
     with pytest.raises(ValueError, match="twice"):
         train.adamw_([p], [new()], [m], [(v[0], m[1])], 1, lr=1e-3)
     assert all(torch.equal(t.float(), torch.ones(300, device="cuda")) for t in (p, q, copy))
+
+
+def test_adamw_class_goes_on_from_written_leaves():
+    """Weights written into a bfloat16 leaf after the optimizer was made are the ones that the next step updates."""
+    train = _train()
+    rng = np.random.default_rng(47)
+    leaf = torch.zeros(500, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    opt = train.AdamW([leaf], lr=1e-2)
+    with torch.no_grad():
+        leaf.copy_(torch.from_numpy(rng.standard_normal(500)))
+    start = leaf.detach().float()
+    leaf.grad = torch.from_numpy(rng.standard_normal(500)).to(torch.bfloat16).cuda()
+    for _ in range(2):
+        opt.step()
+    p, m, v = _np(start), np.zeros(500), np.zeros(500)
+    for t in (1, 2):
+        p, m, v = O.adamw(p, _np(leaf.grad), m, v, t, 1e-2, (0.9, 0.95), 1e-8, 0.0)
+    # each step moves by about 1e-2, off by some tens of roundings of it and of the parameter (below 4)
+    assert np.max(np.abs(_np(opt.masters[0]) - p)) <= 2 * (2e-2 * 40 * E32 + 4 * 4 * E32)
+    assert torch.equal(leaf.detach(), opt.masters[0].to(torch.bfloat16))

@@ -160,3 +160,44 @@ def test_a_loaded_state_reaches_the_bfloat16_leaves(bits):
     assert torch.equal(opt.masters[0], other.masters[0])
     assert torch.equal(opt.params[0].detach(), opt.masters[0].to(torch.bfloat16))
     assert torch.equal(opt.params[1].detach(), torch.ones(7))  # a float32 leaf is the caller's to load
+
+
+def _stepped(monkeypatch, opt):
+    """opt.step() with a gradient for every leaf and a kernel that adds 2^-12 to each parameter, copies rounded."""
+    def kernel(params, grads, m, v, steps, lr, betas, eps, decay, copies):
+        for p, c in zip(params, copies):
+            p += 2.0 ** -12
+            if c is not None:
+                c.copy_(p)
+
+    monkeypatch.setattr(train, "adamw_", kernel)
+    for p in opt.params:
+        p.grad = torch.zeros_like(p)
+    opt.step()
+
+
+def test_weights_written_into_a_leaf_reach_its_master(monkeypatch):
+    """What a bfloat16 leaf was set to between steps is what the next step goes on from; elements that are as the
+    master rounded keep the master's bits, after a write of the same values too."""
+    opt = _optimizer()
+    for _ in range(3):
+        _stepped(monkeypatch, opt)
+    master, leaf = opt.masters[0], opt.params[0]
+    kept = master.clone()
+    assert torch.equal(kept, torch.full((300,), 1 + 3 * 2.0 ** -12))  # 1 in bfloat16
+    with torch.no_grad():
+        leaf[:100] = 5.0
+        leaf[100:200] = leaf[100:200].clone()
+    _stepped(monkeypatch, opt)
+    assert torch.equal(master[:100], torch.full((100,), 5 + 2.0 ** -12))
+    assert torch.equal(master[100:], kept[100:] + 2.0 ** -12)
+    assert torch.equal(leaf.detach(), master.to(torch.bfloat16))
+    with torch.no_grad():
+        leaf.fill_(-2.0)
+    assert torch.equal(opt.state_dict()["masters"][0], torch.full((300,), -2.0))
+    with torch.no_grad():
+        leaf.fill_(7.0)
+    fresh = _optimizer()
+    opt.load_state_dict(fresh.state_dict())  # a loaded state comes after what was written before it
+    _stepped(monkeypatch, opt)
+    assert torch.equal(master, torch.full((300,), 1 + 2.0 ** -12))
