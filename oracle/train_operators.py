@@ -98,3 +98,31 @@ def adamw(p, g, m, v, step, lr, betas, eps, weight_decay):
     v = b2 * v + (1 - b2) * g ** 2
     mh, vh = m / (1 - b1 ** step), v / (1 - b2 ** step)
     return p * (1 - lr * weight_decay) - lr * mh / (np.sqrt(vh) + eps), m, v
+
+
+# ---------------------------------------------------------------------------
+# The gated FFN of bf16 tensors with the roundings that it documents, in torch
+# (float64 on any device), so that large sizes can be compared
+# ---------------------------------------------------------------------------
+
+def round_bits(v, bits):
+    """float64 values rounded to so many significant bits, ties to even."""
+    drop = 53 - bits
+    b = v.contiguous().view(torch.int64)
+    b = b + ((1 << (drop - 1)) - 1) + ((b >> drop) & 1)
+    return ((b >> drop) << drop).view(torch.float64)
+
+
+def ffn_rounded(dy, x, w_gate_up, w_down, kept_bits=10):
+    """(y, dx, dw_gate_up, dw_down): a, dg, du and the results rounded to bf16, silu(g) and u silu'(g) to `kept_bits`
+    significant bits between the passes, everything else in float64."""
+    half = lambda t: t.to(torch.bfloat16).double()  # noqa: E731
+    dy, x, wgu, wd = (t.double() for t in (dy, x, w_gate_up, w_down))
+    f = wd.shape[1]
+    g, u = x @ wgu[:f].T, x @ wgu[f:].T
+    s = 1.0 / (1.0 + torch.exp(-g))
+    p, q = g * s, u * (s * (1.0 + g * (1.0 - s)))
+    a = half(p * u)
+    da = dy @ wd
+    dgu = half(torch.cat([da * round_bits(q, kept_bits), da * round_bits(p, kept_bits)], 1))
+    return tuple(half(t) for t in (a @ wd.T, dgu @ wgu, dgu.T @ x, dy.T @ a))

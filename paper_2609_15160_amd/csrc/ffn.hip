@@ -846,12 +846,12 @@ template <typename T, bool TA, bool TB> hipError_t launch_store(FArgs p, const P
       else return launch_shape<T, TA, TB, E_STORE, Big>(p, s);
     }
     if (plan.shape == P_MID) return launch_shape<T, TA, TB, E_STORE, Mid>(p, s);
-    if constexpr (TA) return launch_shape<T, TA, TB, E_STORE, Small>(p, s);
   }
   if constexpr (!TA) {
     if (plan.shape == P_DEEP) return launch_shape<T, TA, TB, E_STORE, Deep>(p, s);
   }
-  return launch_split<T, TA, TB, Small>(p, s);
+  if constexpr (TA && sizeof(T) == 2) return launch_shape<T, TA, TB, E_STORE, Small>(p, s);
+  else return launch_split<T, TA, TB, Small>(p, s);
 }
 
 template <typename T>

@@ -243,3 +243,144 @@ def test_adamw_class_goes_on_from_written_leaves():
     # each step moves by about 1e-2, off by some tens of roundings of it and of the parameter (below 4)
     assert np.max(np.abs(_np(opt.masters[0]) - p)) <= 2 * (2e-2 * 40 * E32 + 4 * 4 * E32)
     assert torch.equal(leaf.detach(), opt.masters[0].to(torch.bfloat16))
+
+
+# ---------------------------------------------------------------------------
+# Every kernel of the FFN and of the norm, at sizes that select it
+# ---------------------------------------------------------------------------
+
+FFN_SHAPES = [
+    # bf16: gate/up, da, y, dx and the weights' gradients of 256 x 256 ...
+    (6000, 512, 1856), (5500, 2048, 128), (40, 2048, 2560), (5300, 2048, 128),
+    # ... of 128 x 128, the last for the weights' gradients ...
+    (2600, 768, 2048), (2500, 2048, 64), (1500, 768, 2048), (333, 2048, 2048),
+    # ... and of 64 x 64: by four waves, by 16, in ranges
+    (3001, 640, 128), (1000, 768, 512), (20, 128, 4224), (5003, 256, 320),
+]
+FFN_SHAPES_F32 = [(1, 64, 64), (3001, 256, 192), (3001, 256, 512), (300, 256, 512), (5000, 256, 64), (20, 128, 2304),
+                  (530, 64, 64)]
+
+
+def _ffn_operands(n, d, f, dtype, seed=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed + n + 3 * d + f)
+    new = lambda *s, std=1.0: (torch.randn(*s, generator=gen, device="cuda") * std).to(dtype)  # noqa: E731
+    return new(n, d), new(2 * f, d, std=1.5 / d ** 0.5), new(d, f, std=0.1), new(n, d, std=0.1)
+
+
+def _ffn_and_gradients(x, wgu, wd, dy):
+    leaves = [t.detach().requires_grad_() for t in (x, wgu, wd)]
+    y = _train().ffn(*leaves)
+    return (y.detach(), *torch.autograd.grad(y, leaves, dy))
+
+
+@pytest.mark.parametrize("n,d,f", FFN_SHAPES)
+def test_ffn_is_its_formula_with_its_roundings(n, d, f):
+    """Each result in norm against float64 with the documented roundings at their places.  What is left is where a
+    float32 sum falls to the other side of a rounding: its error is about sqrt(K) 2^-24 of a sum of K terms (K up to
+    6000: 5e-6 relative to the value), so a value of 8 bits, steps of 2^-7 to 2^-8, flips with a probability of at most
+    2 x 5e-6 / 2^-8 = 2.4e-3 by one step: sqrt(2.4e-3) 2^-8 = 2e-4 in norm, 4e-4 with three such roundings in a row and a
+    kept value's; 2^-10 is the bar.  Keeping 8 bits instead of 10, or leaving out a row, moves more than that
+    (test_oracle_train_operators.py)."""
+    _say("ffn formula", n, d, f)
+    x, wgu, wd, dy = _ffn_operands(n, d, f, torch.bfloat16)
+    dy2 = dy.clone()
+    dy2[: n - n % 64] = 0  # the weights' gradients from the rows of the last, short stage alone
+    for dy in [dy] + ([dy2] if n % 64 else []):
+        got = _ffn_and_gradients(x, wgu, wd, dy)
+        for name, a, b in zip(("y", "dx", "dw_gate_up", "dw_down"), got, O.ffn_rounded(dy, x, wgu, wd)):
+            off = float((a.double() - b).norm() / b.norm())
+            _say(name, f"{off:.1e}")
+            assert off <= 2.0 ** -10, (name, off)
+
+
+def _kernels(prefix, calls):
+    """Names of the kernels, of those whose name has the prefix, that the calls launch, and of those in the library."""
+    import re
+    import subprocess
+    from paper_2609_15160_amd import tlf
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
+        for call in calls:
+            call()
+        torch.cuda.synchronize()
+    with open(tlf.LIB_PATH, "rb") as f:
+        built = {m.decode() for m in re.findall(rb"_ZN3tlf12_GLOBAL__N_1\d+" + prefix.encode() + rb"\w*", f.read())}
+    names = sorted(n for n in built if "device_stub" not in n)
+    plain = subprocess.run(["c++filt"], input="\n".join(names), capture_output=True, text=True, check=True).stdout.split("\n")
+    known = dict(zip(names, names)) | dict(zip(plain, names))
+    return {known[e.name] for e in prof.events() if e.name in known}, set(names)
+
+
+def test_every_ffn_kernel_is_reached():
+    """The sizes above, and those of float32, launch every tile shape, transposition, epilogue and split there is."""
+    _say("ffn kernels")
+    calls = [lambda s=s, t=t: _ffn_and_gradients(*_ffn_operands(*s, t)) for t, shapes in
+             ((torch.bfloat16, FFN_SHAPES), (torch.float32, FFN_SHAPES_F32)) for s in shapes]
+    ran, built = _kernels("k_ffn", calls)
+    assert len(built) >= 30 and ran == built, sorted(built - ran)
+
+
+# Widths of 1, 2, 4, 8 and 16 vectors of a lane; one wave to sixteen for the sums of gamma's gradient.
+NORM_TYPES = [(a, b) for a in (torch.float32, torch.bfloat16) for b in (torch.float32, torch.bfloat16)]
+NORM_WIDTHS = [(256, (0,)), (512, (0,)), (1024, (0, 1, 8, 16)), (2048, (0, 1, 8, 16)), (4096, (0, 1, 8, 16))]
+MANY = 300 << 20  # bytes of x and y, above what the rows of a call may have to be read through the caches
+
+
+def _norm_operands(bytes_, d, groups, xt, yt):
+    n = bytes_ // (d * (xt.itemsize + yt.itemsize)) | 1
+    gen = torch.Generator(device="cuda").manual_seed(n + d + groups)
+    new = lambda t, *s: torch.randn(*s, generator=gen, device="cuda").to(t)  # noqa: E731
+    gamma = new(torch.float32, groups, d) * 0.3 if groups else None
+    # with one group too, some rows belong to none
+    group = torch.randint(-1, groups + 1, (n,), generator=gen, device="cuda", dtype=torch.int32) if groups else None
+    return new(xt, n, d), gamma, group, new(yt, n, d)
+
+
+def _norm_and_gradients(x, gamma, group, dy):
+    leaves = [t.detach().requires_grad_() for t in (x, gamma) if t is not None]
+    y = _train().rms_norm(leaves[0], leaves[1] if gamma is not None else None, group, dtype=dy.dtype)
+    return (y.detach(), *torch.autograd.grad(y, leaves, dy))
+
+
+@pytest.mark.parametrize("xt,yt", NORM_TYPES)
+@pytest.mark.parametrize("d,groups", [(d, k) for d, ks in NORM_WIDTHS for k in ks])
+def test_norm_of_many_bytes(xt, yt, d, groups):
+    """A call of more bytes than the caches hold: its rows to the bit as those of a small call, which is held against
+    float64 here; gamma's gradient against float64 over all rows.  The sum of a column goes over at most rows / 256 + 8
+    rows in order, then 128 partial sums; r is off by (d + 12) 2^-24 of it."""
+    _say("norm", d, groups, xt, yt)
+    x, gamma, group, dy = _norm_operands(MANY, d, groups, xt, yt)
+    n = x.shape[0]
+    gen = torch.Generator(device="cuda").manual_seed(d + groups)
+    at = torch.cat([torch.arange(9, device="cuda"), torch.randint(0, n, (100,), generator=gen, device="cuda"),
+                    torch.arange(n - 9, n, device="cuda")])
+    some = (x[at], gamma, None if group is None else group[at], dy[at])
+    large, small = _norm_and_gradients(x, gamma, group, dy), _norm_and_gradients(*some)
+    assert torch.equal(large[0][at], small[0]) and torch.equal(large[1][at], small[1])
+    xs, gs = some[0].double(), some[3].double()
+    gain = torch.ones_like(xs)
+    if groups:
+        known = (some[2] >= 0) & (some[2] < groups)
+        gain[known] += gamma.double()[some[2][known].long()]
+    r = (xs.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+    h, e = gs * gain, (d + 12) * E32
+    want, dx = xs * r * gain, r * (h - xs * r * r * (h * xs).mean(1, keepdim=True))
+    mag = r * (h.abs() + xs.abs() * r * r * (h * xs).abs().mean(1, keepdim=True))
+    half = lambda t: E16 if t == torch.bfloat16 else E32  # noqa: E731
+    assert ((small[0].double() - want).abs() <= want.abs() * (2 * e + half(yt) * 1.001)).all()
+    assert ((small[1].double() - dx).abs() <= 4 * e * mag + dx.abs() * half(xt) * 1.001).all()
+    if groups:
+        xr = x.double()
+        xr *= (xr.square().mean(1, keepdim=True) + 1e-5).rsqrt()
+        xr *= dy
+        for k in range(groups):
+            one = xr[group == k]
+            bound = one.abs().sum(0) * (n / 256 + 8 + 128 + d + 16) * E32
+            assert ((large[2][k].double() - one.sum(0)).abs() <= bound).all(), k
+
+
+def test_every_norm_kernel_is_reached():
+    _say("norm kernels")
+    calls = [lambda a=(b, d, k, xt, yt): _norm_and_gradients(*_norm_operands(*a))
+             for b in (1 << 20, MANY) for d, ks in NORM_WIDTHS for k in ks for xt, yt in NORM_TYPES]
+    ran, built = _kernels("k_norm", calls)
+    assert len(built) >= 100 and ran == built, sorted(built - ran)

@@ -96,3 +96,41 @@ def test_eight_bit_round_trip_is_within_half_a_step(which):
     # half a step of the value or of the subnormal grid (a whole one for a v held above zero), and the
     # scale's own float32 rounding
     assert np.all(np.abs(back - v) <= np.maximum(half * np.abs(v), smallest * top) * (1 + 2.0 ** -20) + np.abs(v) * 2.0 ** -22)
+
+
+def test_round_bits():
+    one = torch.tensor([1.0, 1.0 + 2.0 ** -10, 1.0 + 2.0 ** -9, 1.0 + 3 * 2.0 ** -10, -1.0 - 2.0 ** -10 - 2.0 ** -40, 0.0,
+                        3e-300], dtype=torch.float64)
+    want = [1.0, 1.0, 1.0 + 2.0 ** -9, 1.0 + 2.0 ** -8, -1.0 - 2.0 ** -9, 0.0]
+    got = O.round_bits(one, 10)
+    assert got[:6].tolist() == want and abs(got[6] / 3e-300 - 1) <= 2.0 ** -10
+    r = torch.from_numpy(RNG(8).standard_normal(1000))
+    assert torch.equal(O.round_bits(r.float().double(), 24), r.float().double())
+    assert torch.equal(O.round_bits(r, 8), r.to(torch.bfloat16).double())  # but for a tie of float32, of which there is none
+
+
+def _difference_in_norm(got, want):
+    return float((got - want).norm() / want.norm())
+
+
+def test_rounded_ffn_and_what_a_norm_tells():
+    """The rounded formula is the formula up to its roundings; a fault of the kind that a kernel may have moves some
+    result by more than 2^-10 of its norm."""
+    r = RNG(9)
+    n, d, f = 1003, 64, 128
+    new = lambda *s, std=1.0: torch.from_numpy(r.standard_normal(s) * std).to(torch.bfloat16)  # noqa: E731
+    x, wgu, wd, dy = new(n, d), new(2 * f, d, std=1.5 / 8), new(d, f, std=0.1), new(n, d, std=0.1)
+    args = [t.double().numpy() for t in (x, wgu, wd)]
+    plain = [O.ffn(*args), *O.ffn_backward(dy.double().numpy(), *args)]
+    right = O.ffn_rounded(dy, x, wgu, wd)
+    for a, b in zip(right, plain):
+        # at most three bf16 roundings and one of 2^-10 in a row, each up to 2^-8 of a value
+        assert 1e-4 < _difference_in_norm(a, torch.from_numpy(b)) < 3 * 2.0 ** -8 + 2.0 ** -10
+    worst = lambda other: max(_difference_in_norm(a, b) for a, b in zip(other, right))  # noqa: E731
+    assert worst(O.ffn_rounded(dy, x, wgu, wd, kept_bits=8)) > 2.0 ** -10       # kept as bf16
+    lost = dy.clone()
+    lost[-1] = 0                                                                # one row left out of the sums
+    assert worst(O.ffn_rounded(lost, x, wgu, wd)) > 2.0 ** -10
+    part = dy.clone()
+    part[: n - n % 64] = 0                                                      # the last, short stage alone
+    assert worst(O.ffn_rounded(part * 0, x, wgu, wd)) > 2.0 ** -10
