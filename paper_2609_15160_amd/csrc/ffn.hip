@@ -706,7 +706,7 @@ int64_t tiles_of(int64_t m, int64_t n, int64_t b) { return ((m + b - 1) / b) * (
 // third of the compute units' time unused.
 bool big_fits(int64_t tiles) {
   const int64_t rounds = (tiles + kCus - 1) / kCus;
-  return tiles >= 160 && 3 * tiles >= 2 * kCus * rounds;
+  return 3 * tiles >= 2 * kCus * rounds;
 }
 
 // The fused products: Big where it fits, Mid from 300 tiles of its size, else
