@@ -384,3 +384,25 @@ def test_every_norm_kernel_is_reached():
              for b in (1 << 20, MANY) for d, ks in NORM_WIDTHS for k in ks for xt, yt in NORM_TYPES]
     ran, built = _kernels("k_norm", calls)
     assert len(built) >= 100 and ran == built, sorted(built - ran)
+
+
+def test_ffn_weight_gradients_past_32_bit_offsets():
+    """[dg | du] of 66000 x 32768 passes 2^31 elements, and 2^32 bytes lie before its last rows: the weights' gradients,
+    which read it and `a` with rows as the sum, against float64 products of the formula's dg, du and a (as it rounds
+    them) in columns from both ends of each half; y and dx of the last rows."""
+    n, d, f = 66000, 64, 16384
+    x, wgu, wd, dy = _ffn_operands(n, d, f, torch.bfloat16)
+    _say("ffn", n, d, f)
+    y, dx, dwgu, dwd = _ffn_and_gradients(x, wgu, wd, dy)
+    pick = torch.tensor([0, 1, 77, 4095, 8192, f - 65, f - 2, f - 1], device="cuda")
+    # the formula of these columns alone: their gates and ups, their part of W_down
+    _, _, want_gu, want_d = O.ffn_rounded(dy, x, torch.cat([wgu[pick], wgu[f + pick]]), wd[:, pick].contiguous())
+    for name, a, b in (("dw_gate", dwgu[pick], want_gu[:8]), ("dw_up", dwgu[f + pick], want_gu[8:]),
+                       ("dw_down", dwd[:, pick], want_d)):
+        off = float((a.double() - b).norm() / b.norm())
+        _say(name, f"{off:.1e}")
+        assert off <= 2.0 ** -10, name
+    part = torch.arange(n - 300, n, device="cuda")
+    want_y, want_dx, _, _ = O.ffn_rounded(dy[part], x[part], wgu, wd)
+    for name, a, b in (("y", y[part], want_y), ("dx", dx[part], want_dx)):
+        assert float((a.double() - b).norm() / b.norm()) <= 2.0 ** -10, name
