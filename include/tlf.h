@@ -427,8 +427,9 @@ int tlf_ste(const int32_t* d_depth, const float* d_score, const float* d_grad_va
  *   d_y      [rows][d] (y_dtype);
  *   d_rstd   [rows] float32, receives r (tlf_rms_norm_grad reads it), or NULL;
  *            4-byte aligned, as d_group.
- * d a multiple of 4, at most TLF_NORM_MAX_D; groups at most TLF_NORM_MAX_GROUPS,
- * rows at most TLF_NORM_MAX_ROWS. */
+ * Squares are summed in float32: a row whose sum of squares passes its range
+ * gives r = 0.  d a multiple of 4, at most TLF_NORM_MAX_D; groups at most
+ * TLF_NORM_MAX_GROUPS, rows at most TLF_NORM_MAX_ROWS. */
 #define TLF_NORM_MAX_D 4096
 #define TLF_NORM_MAX_ROWS (1 << 30)
 #define TLF_NORM_MAX_GROUPS 16
@@ -450,7 +451,8 @@ int tlf_rms_norm_grad(const void* d_dy, int32_t y_dtype, const void* d_x, int32_
 /* Gated FFN (Appendix A with SwiGLU): y = a W_down^T with a = silu(g) u and
  * g | u = x [W_gate | W_up]^T.
  *   dtype         of x, the weights and every output; products are summed in
- *                 float32, and a and the results are rounded to dtype;
+ *                 float32, and a and the results are rounded to dtype (a is an
+ *                 operand of the second product);
  *   d_x           [rows][d];
  *   d_w_gate_up   [2f][d]: rows gate | up (as tlf_layer_weights);
  *   d_w_down      [d][f];

@@ -75,6 +75,8 @@ __device__ __forceinline__ int tensor_of(const AdamArgs& a, int block) {
   return lo;
 }
 
+// The hardware's reciprocal is off by one of the float32 roundings that the step's
+// other operations make too.
 __device__ __forceinline__ float update(float p, float m, float v, const AdamTensor& t, float eps) {
   return p * t.decay - t.rate * m * __builtin_amdgcn_rcpf(sqrtf(v) * t.root + eps);  // eps is normal
 }

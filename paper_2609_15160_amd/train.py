@@ -326,7 +326,8 @@ def rms_norm(x: torch.Tensor, gamma: torch.Tensor = None, group: torch.Tensor = 
 
     gamma is None, one [d] or [1, d] scale, or [groups, d] scales of which row r takes number group[r] (int32 [rows];
     a row whose number is none of them takes no scale): the AdaLN modulation of each token's depth.  The result has
-    `dtype` (x's by default).  d is a multiple of 4 up to 4096, and there are 16 groups at most."""
+    `dtype` (x's by default).  d is a multiple of 4 up to 4096, there are 16 groups and 2^30 rows at most.  Squares are
+    summed in float32: a row whose sum of squares passes its range comes out as zeros."""
     if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
         raise ValueError("rms_norm: expected a float32 or bfloat16 [rows, d] CUDA tensor")
     dtype = dtype or x.dtype
@@ -387,7 +388,10 @@ class _Ffn(torch.autograd.Function):
 def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch.Tensor:
     """The block's gated FFN, W_down (silu(W_gate x) * (W_up x)) of the rows of x ([rows, d]), with gradients.
 
-    w_gate_up is [2f, d] (rows gate | up), w_down [d, f]; all three float32 or all bfloat16, d and f multiples of 64."""
+    w_gate_up is [2f, d] (rows gate | up), w_down [d, f]; all three float32 or all bfloat16, d and f multiples of 64 up
+    to 16384.  Sums are float32.  In bfloat16 the hidden activation and its gradient, the operands of the next products,
+    are rounded to bfloat16, and what the backward pass takes of the activation to 10 significant bits, over float32's
+    range: as a bfloat16 model does it, and of float32 tensors none of it."""
     if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
         raise ValueError("ffn: expected a float32 or bfloat16 [rows, d] CUDA tensor")
     d, f = x.shape[1], w_down.shape[-1]
