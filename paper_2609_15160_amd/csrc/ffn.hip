@@ -636,13 +636,16 @@ template <typename T, bool TA, bool TB, int EK, typename SH, bool SPLIT> struct 
   }
 };
 
-// bf16 on 256 x 256 tiles, us and TFLOP/s: 16384 x 1024 x 2816 gate/up 217 (870),
-// down 83 (1140), da 146 (650), dx 143 (1320); 8191 x 2048 x 5504 366 (1010), 153
-// (1210), 214 (860), 277 (1330).  The loads into LDS bound the products: without
-// them 135, 50, 139 and 91 us of the first four (then 231, 91, 153, 155), alone 131 of
-// gate/up, 73 of down, 126 of dx, of which 37 of down's where all of it is in L2.
-// Gate/up writes 300 MB in its epilogue and da reads and writes 392: one workgroup
-// fills a compute unit, so nothing else runs on it meanwhile.
+// bf16 on 256 x 256 tiles, us and TFLOP/s of kernels that run one at a time: 16384 x
+// 1024 x 2816 gate/up 216 (875), down 78 (1215), da 151 (625), dx 145 (1300); 8191 x
+// 2048 x 5504 356 (1040), 142 (1300), 222 (830), 280 (1320); traced right behind each
+// other they take up to a tenth more.  The matrix cores are busy 36, 49, 25 and 56%
+// of the first four, no LDS read meets a bank conflict.  The loads into LDS bound the
+// products: without them 135, 50, 139 and 91 us of the first four (then 231, 91, 153,
+// 155), alone 131 of gate/up, 73 of down, 126 of dx, of which 37 of down's where all
+// of it is in L2.  Gate/up writes 300 MB in its epilogue and da reads and writes 392:
+// one workgroup fills a compute unit, so nothing else runs on it meanwhile, and it
+// does not load its next tile then, though the epilogue needs none of the LDS.
 template <typename T, bool TA, bool TB, int EK, typename SH> __global__ __launch_bounds__(SH::NTH) void k_ffn(FArgs g) {
   using TL = Tile<T, TA, TB, EK, SH, false>;
   __shared__ __align__(16) char lds[TL::LDS];
@@ -763,7 +766,9 @@ Plan plan_of(int shape, int64_t m, int64_t n, int64_t splits) {
 // 2816 (192 tiles of 128 x 128) 82, 88, 112 and 106, 111, 160; 3580 x 1024 x 2816
 // (224) 92, 88, 113 and 128, 112, 160; 2000 x 2048 x 5504 (256) 180, 171, 214 and 225,
 // 191, 278; 4400 x 1024 x 2816 (280) 106, 109, 123 and 135, 133, 158; 8191 x 2048 x
-// 5504 (1024) 589, 515, 456 and 890, 597, 486.
+// 5504 (1024) 589, 515, 456 and 890, 597, 486.  From 257 to 299 tiles of 128 x 128 the
+// sides are level: 280 above, and the y of 6000 x 768 x 2048 (282) 76-78 with Small in
+// the whole pass, 79 with Mid.
 //
 // Else tiles of 64 x 64, by four waves where there are more than compute units,
 // by 16, which share the sum, below (1300 x 768 x 2048, 252 tiles, 33 and 31, 37 and
@@ -800,7 +805,8 @@ int64_t rounds_time(int64_t tiles, int64_t slots, int64_t stages, int64_t stage_
 // the rows in ranges for a workgroup on each compute unit, or two with 375 rows or
 // more (3001 x 256 x 512, ranges for one and for two: dW_down 17, 19, dW_gate_up 42
 // with da, 39; 8000 rows 34, 30 and 89, 76; 1000 rows 11, 13 and 24, 26; whole 3001
-// rows take 80 and 96).
+// rows take 80 and 96; ranges of 375 rows were faster and of 125 slower, those in
+// between are not measured).
 Plan grad_plan(bool half, int64_t m, int64_t n, int64_t rows) {
   const int64_t stages = (rows + 63) / 64, small = tiles_of(m, n, 64), mid = tiles_of(m, n, 128), big = tiles_of(m, n, 256);
   if (!half) {

@@ -94,7 +94,9 @@ __device__ __forceinline__ const float* gamma_of(const float* gamma, const int32
 }
 
 // One wave per row, the row in registers: 4 NV elements per lane.  Bound by HBM:
-// 32768 x 1024 from float32 to bf16 33 us, 6.1 TB/s.
+// 32768 x 1024 from float32 to bf16, 8 groups, 41 us behind the gradient's pass
+// (4.9 TB/s), 33 again and again on the same rows, of which the memory-side cache
+// then holds a part; bf16 rows 28, without gamma 21 (6.3 TB/s).
 template <typename TX, typename TY, int NV, bool PAST>
 __global__ __launch_bounds__(kNormWaves* kWave) void k_norm(NormArgs a) {
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * kNormWaves + threadIdx.x / kWave), lane = lane_id();
@@ -164,8 +166,8 @@ __global__ __launch_bounds__(kNormWaves* kWave) void k_norm_dx(NormArgs a) {
 // meanwhile, and the groups of those after them.  x and dy are read once, dx is
 // written; the workgroups' sums add 4 groups d bytes each.  32768 x 1024, float32
 // x, bf16 dy, both gradients with their sums joined: 71 us for 8 groups (5.2 TB/s
-// with the sums), dx alone 54 (6.2 TB/s); what is left is the loads' latency
-// between two barriers.
+// with the sums), dx alone 54 (6.2 TB/s); bf16 rows the same 71 us for 201 MB, dx
+// alone 32 (6.2 TB/s): what is left is the loads' latency between two barriers.
 template <typename TX, typename TY, int GMAX, int MAXT, int RU, bool PAST>
 __global__ __launch_bounds__(MAXT) void k_norm_grad(NormArgs a, int chunk, float* part) {
   __shared__ __align__(16) float red[2][MAXT / kWave][RU];
