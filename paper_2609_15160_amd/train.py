@@ -527,8 +527,7 @@ class AdamW:
         for k in have:
             p, m = self.params[k].detach(), self.masters[k]
             if m is not None and _writes(p) != self._written[k]:
-                m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))
-                self._written[k] = _writes(p)
+                m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))  # the same again if no step follows
 
     @torch.no_grad()
     def step(self) -> None:

@@ -406,3 +406,22 @@ def test_ffn_weight_gradients_past_32_bit_offsets():
     want_y, want_dx, _, _ = O.ffn_rounded(dy[part], x[part], wgu, wd)
     for name, a, b in (("y", y[part], want_y), ("dx", dx[part], want_dx)):
         assert float((a.double() - b).norm() / b.norm()) <= 2.0 ** -10, name
+
+
+def test_adamw_class_refused_under_capture_loses_no_written_leaf():
+    """A step that is refused because it is captured takes nothing: the next one still goes on from the written leaf."""
+    train = _train()
+    leaf = torch.zeros(256, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    opt = train.AdamW([leaf], lr=0.0)
+    leaf.grad = torch.ones_like(leaf)
+    with torch.no_grad():
+        leaf.fill_(3.0)
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.zeros(8, device="cuda")
+    with torch.cuda.graph(graph):
+        other.add_(1.0)
+        with pytest.raises(RuntimeError, match="captured"):
+            opt.step()
+    opt.step()
+    assert torch.equal(opt.masters[0], torch.full((256,), 3.0, device="cuda")) and opt.steps == [1]
+    assert torch.equal(leaf.detach().float(), opt.masters[0])
