@@ -411,8 +411,8 @@ int tlf_ste(const int32_t* d_depth, const float* d_score, const float* d_grad_va
  * As above: no context, caller-owned device buffers of the current device,
  * work enqueued on `stream` without waiting, TLF_E_INVALID_ARG or
  * TLF_E_UNSUPPORTED before anything is enqueued, TLF_E_HIP for a failed
- * launch.  Nothing is allocated, so every call may be captured into a graph.
- * Tensors are row-major and contiguous, 16-byte aligned unless said otherwise;
+ * launch.  No device memory is allocated, so every call may be captured into a
+ * graph.  Tensors are row-major and contiguous, 16-byte aligned unless said otherwise;
  * outputs overlap nothing else.  Gradients overwrite their buffers.  Results
  * are the same to the bit from call to call.
  * ------------------------------------------------------------------------- */

@@ -86,7 +86,7 @@ __device__ __forceinline__ unsigned kept18(float v) {  // in the upper 18 bits, 
 // whole lines (row by row it moved 8 bytes per lane in 32-byte pieces), past the
 // caches, which keep a and the weights instead (16384 x 1024 x 2816, measured when
 // q and p were 16 bits: gate/up 224 -> 217 us, down 88 -> 83).  `pair` counts the
-// pairs of accumulators times lanes, `pairs` is their number.
+// pairs of accumulators, row bands of 16 first, of which there are `pairs`.
 template <typename T> struct Kept;
 template <> struct Kept<float> {
   struct Raw { f32x4 q[2], p[2]; };

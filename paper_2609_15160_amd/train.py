@@ -389,9 +389,9 @@ def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch
     """The block's gated FFN, W_down (silu(W_gate x) * (W_up x)) of the rows of x ([rows, d]), with gradients.
 
     w_gate_up is [2f, d] (rows gate | up), w_down [d, f]; all three float32 or all bfloat16, d and f multiples of 64 up
-    to 16384.  Sums are float32.  In bfloat16 the hidden activation and its gradient, the operands of the next products,
-    are rounded to bfloat16, and what the backward pass takes of the activation to 10 significant bits, over float32's
-    range: as a bfloat16 model does it, and of float32 tensors none of it."""
+    to 16384.  Sums are float32.  Of bfloat16 tensors the hidden activation and its gradient, operands of the next
+    products, are rounded to bfloat16, and what the backward pass takes of the activation to 10 significant bits with
+    float32's range; of float32 tensors nothing is rounded on the way."""
     if x.dim() != 2 or x.dtype not in _DTYPE or not x.is_cuda:
         raise ValueError("ffn: expected a float32 or bfloat16 [rows, d] CUDA tensor")
     d, f = x.shape[1], w_down.shape[-1]
