@@ -519,6 +519,64 @@ typedef struct tlf_adamw_tensor {
 int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
               void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Training operators around the FFN half: the block's attention, the gated
+ * residual with the norm that follows, and the clipping of gradients.  As above.
+ * ------------------------------------------------------------------------- */
+
+/* Causal attention of ragged rows (Eq. 10 among the gathered tokens of a loop;
+ * offsets as tlf_gs_plan writes them), with a sliding window and sinks.
+ * Sequence b has nq = q_offsets[b + 1] - q_offsets[b] query rows and n keys from
+ * row k_offsets[b]; its last query stands at its last key, query j at position
+ * p = n - nq + j.  The key at position x is visible to it when
+ *   x <= p and (p - x < window or x < sinks)
+ * and o = sum softmax(scale q . k) v over the visible keys.  A query that sees no
+ * key, and a row behind the last sequence, gives zeros (and zero gradients).
+ * What a query does not see takes no part, whatever values it has. */
+#define TLF_ATTN_MAX_SINKS 64
+#define TLF_ATTN_MAX_HEADS 1024
+#define TLF_ATTN_MAX_ROWS (1 << 29)
+#define TLF_ATTN_MAX_UNITS (1 << 29)     /* rows times heads */
+#define TLF_ATTN_MAX_SEQ_HEADS (1 << 22) /* sequences times heads */
+#define TLF_ATTN_MAX_STRIDE (1 << 22)
+typedef struct tlf_attn_shape {
+  int32_t dtype;     /* of q, k, v, o and their gradients: TLF_DTYPE_F32 or TLF_DTYPE_BF16 */
+  int32_t batch;     /* sequences */
+  int32_t heads;     /* of q and o: a multiple of kv_heads; head h reads key head h / (heads / kv_heads) */
+  int32_t kv_heads;
+  int32_t head_dim;  /* 64 or 128 (16 for float32 only) */
+  int32_t rows_q;    /* rows of q and o */
+  int32_t rows_k;    /* rows of k and v */
+  int32_t window;    /* 0: every earlier key is visible (sinks is then without effect) */
+  int32_t sinks;
+  float scale;       /* > 0; 1 / sqrt(head_dim) usually */
+  /* Elements between rows, multiples of 16 bytes; a row's heads lie one behind the
+   * other.  do lies as o. */
+  int64_t q_stride, k_stride, v_stride, o_stride;
+  /* Device arrays.  Offsets ascend from 0; they are clamped to the rows there are. */
+  const int32_t* d_q_offsets; /* [batch + 1] */
+  const int32_t* d_k_offsets; /* [batch + 1]; d_q_offsets itself where the rows are the same */
+  const int32_t* d_k_lengths; /* [batch] keys that sequence b holds of the rows up to k_offsets[b + 1], or NULL: all */
+} tlf_attn_shape;
+
+/*   d_lse  [heads][rows_q] float32, receives log2 of each softmax sum, base
+ *          included (tlf_attn_grad reads it; +inf where nothing is visible), or NULL.
+ *   d_workspace: tlf_attn_ws_bytes bytes (may be 0), used during the call only. */
+int tlf_attn_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes);
+int tlf_attn(const tlf_attn_shape* shape, const void* d_q, const void* d_k, const void* d_v, void* d_o, float* d_lse,
+             void* d_workspace, size_t ws_bytes, void* stream);
+
+/* Gradients of tlf_attn from its inputs, its o and the lse that it wrote:
+ *   P = exp2(log2(e) scale q . k - lse),  dS = P (do . v - do . o),
+ *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T do
+ * with sums over the queries and over the heads that share a key head.  P and dS
+ * are rounded to dtype as operands, the sums are float32.  All three are written,
+ * every row of them; their strides are elements between rows. */
+int tlf_attn_grad_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes);
+int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q, const void* d_k, const void* d_v,
+                  const void* d_o, const float* d_lse, void* d_dq, int64_t dq_stride, void* d_dk, int64_t dk_stride,
+                  void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,263 @@
+// Causal attention of ragged rows with a sliding window and sinks: what its
+// forward and backward kernels share (gfx950 only).
+//
+// Sequence b has query rows [q_off[b], q_off[b + 1]) and n keys from row k_off[b];
+// its last query stands at its last key, query j at position p = n - nq + j.  The
+// key at position x is visible to the query at p when
+//   x <= p and (p - x < window or x < sinks).
+//
+// All products are MFMA of 16 x 16 tiles.  A row-major LDS tile (rows of keys or of
+// queries) gives both operands: rows as they lie (contraction over the head's
+// dimensions), and transposed (contraction over rows).  Scores are computed so that
+// a lane's accumulators are four rows of one column; as operand of the next product
+// they are the rows 4 g .. 4 g + 3 (g = lane / 16) of one or two tiles, and the
+// other operand is read in the same order of rows, so scores never leave registers.
+#pragma once
+
+#include "common.h"
+#include "stage.h"
+
+namespace tlf {
+
+struct WAttnArgs {
+  const void *q, *k, *v, *o, *dout;
+  void *out, *dq, *dk, *dv;
+  float *lse, *delta;               // [heads][rows_q]: log2 of the softmax sums, o . do
+  float* part;
+  const int32_t *q_off, *k_off, *k_len;
+  int64_t qs, ks, vs, os;           // elements between rows; gradients lie as what they belong to
+  int batch, heads, kv_heads, rows_q, rows_k, window, sinks;
+  int slots;                        // tiles of rows, an upper bound
+  int splits;
+  float scale, scale_log2;
+};
+
+struct WSeq {
+  int q0, nq, k0, n, cap;  // first rows, queries, keys, rows that the keys have room in
+};
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
+
+// Tiles of STEP rows: sequence b's begin at slot off[b] / STEP + b, which leaves
+// each at least as many slots as it has tiles and needs no plan on the device.
+// The rows behind the last sequence are one more, without keys.
+template <int STEP> __device__ __forceinline__ int slot_of(const int32_t* off, int rows, int b) {
+  return clampi(off[b], 0, rows) / STEP + b;
+}
+template <int STEP> inline int64_t slots_of(int64_t rows, int64_t batch) { return rows / STEP + batch + 1; }
+
+// The last b in [0, batch] whose slots begin at or before `slot`, 64 at a time.
+template <int STEP> __device__ __forceinline__ int seq_of(const int32_t* off, int rows, int batch, int slot) {
+  int lo = 0, hi = batch;
+  while (hi > lo) {
+    const int step = (hi - lo + kWave - 1) / kWave, b = lo + (lane_id() + 1) * step;
+    const bool before = b <= hi && slot_of<STEP>(off, rows, min(b, hi)) <= slot;
+    lo += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * step;
+    hi = min(hi, lo + step - 1);
+  }
+  return lo;
+}
+
+__device__ __forceinline__ WSeq load_seq(const WAttnArgs& a, int b) {
+  WSeq s;
+  s.q0 = clampi(a.q_off[b], 0, a.rows_q);
+  s.k0 = clampi(a.k_off[b], 0, a.rows_k);
+  if (b < a.batch) {
+    s.nq = clampi(a.q_off[b + 1], s.q0, a.rows_q) - s.q0;
+    s.cap = clampi(a.k_off[b + 1], s.k0, a.rows_k) - s.k0;
+    s.n = a.k_len ? clampi(a.k_len[b], 0, s.cap) : s.cap;
+  } else {
+    s.nq = a.rows_q - s.q0;
+    s.cap = a.rows_k - s.k0;
+    s.n = 0;
+  }
+  return s;
+}
+
+// Whether the key u positions before the query (u < 0: behind it) at position x is visible.
+__device__ __forceinline__ bool sees(int u, int x, int window, int sinks) {
+  return (unsigned)u < (unsigned)window || (u >= 0 && x < sinks);
+}
+
+// Operands of 16 bytes per lane: bf16, eight values of one MFMA over 32; float32,
+// four values of one MFMA over 4 each.
+template <typename T> struct Opnd;
+template <> struct Opnd<bf16> {
+  typedef bf16x8 frag;
+  static constexpr int TILES = 2;  // score tiles of one operand
+  static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ frag pack(const f32x4* s) {  // the rows of two score tiles
+    return __builtin_bit_cast(frag, make_uint4(pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]),
+                                               pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])));
+  }
+};
+template <> struct Opnd<float> {
+  typedef f32x4 frag;
+  static constexpr int TILES = 1;
+  static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ frag pack(const f32x4* s) { return s[0]; }
+};
+
+// LDS rows of one head: D elements in 16-byte chunks, chunk c of row r at place
+// c ^ key(r).  The keys of 16 rows are distinct where 16 rows span the banks
+// twice, those of rows 0..7 differ by pairs of chunks: reads of 16 rows' chunks and
+// transposed reads of 8 rows' chunk pairs both fall into distinct banks.
+template <typename T, int D> struct HeadRows {
+  using O = Opnd<T>;
+  typedef typename O::frag frag;
+  static constexpr int EPC = 16 / (int)sizeof(T);
+  static constexpr int RB = D * (int)sizeof(T);      // bytes of a row
+  static constexpr int CPR = RB / 16;                // its chunks
+  static constexpr int KSTEPS = CPR / 4;             // contraction steps over D
+  static constexpr int DT = D / 16;
+  static constexpr int ROWS = 16 * O::TILES;         // rows of one transposed operand
+  static constexpr int PER = RB >= 256 ? 1 : 256 / RB, KEYS = CPR < 16 ? CPR : 16;
+  static_assert(CPR % 4 == 0 && D % 16 == 0, "head width");
+  static __device__ __forceinline__ int key(int r) {
+    const int x = (r / PER) & (KEYS - 1);
+    return (x & (KEYS / 2 - 1)) << 1 | x / (KEYS / 2);
+  }
+  // this lane's byte offsets: of row i's chunk of step ks, of the transposed reads of dimension tile dt
+  static __device__ __forceinline__ void direct(int lane, int (&at)[KSTEPS]) {
+    const int i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) at[ks] = i * RB + (((ks * 4 + g) ^ key(i)) << 4);
+  }
+  static __device__ __forceinline__ frag load(const char* tile, int row, int at) {  // row: a multiple of 16
+    return *reinterpret_cast<const frag*>(tile + row * RB + at);
+  }
+  static constexpr int TR = sizeof(T) == 2 ? DT : DT * 4;  // offsets of the transposed reads
+  static __device__ __forceinline__ void transposed(int lane, int (&at)[TR]) {
+    const int i = lane & 15, g = lane >> 4;
+    if constexpr (sizeof(T) == 2) {
+      const int r = 4 * g + (i >> 2);  // a group of 16 lanes reads 4 rows x 16 dimensions, lane i gets dimension i
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) at[dt] = r * RB + (((2 * dt + ((i >> 1) & 1)) ^ key(r)) << 4) + (i & 1) * 8;
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 4 * g + j;
+          at[dt * 4 + j] = r * RB + (((4 * dt + (i >> 2)) ^ key(r)) << 4) + (i & 3) * 4;
+        }
+    }
+  }
+  // dimension tile dt of the rows [row, row + ROWS), row a multiple of 16
+  static __device__ __forceinline__ frag load_t(const char* tile, int row, const int (&at)[TR], int dt) {
+    const char* p = tile + row * RB;
+    if constexpr (sizeof(T) == 2) {
+      union { s16x4 h[2]; frag v; } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + at[dt]));
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * RB + at[dt]));
+      return u.v;
+    } else {
+      frag v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(p + at[dt * 4 + j]);
+      return v;
+    }
+  }
+};
+
+// Two tiles of ROWS rows each (A and B, of one head) from global memory into LDS,
+// asynchronously.  Rows past the last one are read from the last one.
+template <typename T, int D, int ROWS, int NTH> struct PairLoader {
+  using H = HeadRows<T, D>;
+  static constexpr int HALF = ROWS * H::CPR;       // chunks of a tile
+  static constexpr int N = 2 * HALF / NTH;         // chunks of a thread
+  static constexpr int BYTES = 2 * ROWS * H::RB;   // A, then B
+  static_assert(2 * HALF % NTH == 0 && HALF % kWave == 0, "chunks");
+  int row[N], chunk[N];  // row of the tile, byte of the chunk
+  int wbase;
+  __device__ __forceinline__ void init() {
+    wbase = __builtin_amdgcn_readfirstlane(threadIdx.x & ~(kWave - 1));
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const int q = (threadIdx.x + c * NTH) % HALF;
+      row[c] = q / H::CPR;
+      chunk[c] = ((q % H::CPR) ^ H::key(row[c])) << 4;
+    }
+  }
+  // a, b: this head's elements of the tile's first row; as, bs: bytes between rows; last: the last row, from the first
+  __device__ __forceinline__ void issue(const void* a, const void* b, int as, int bs, int last, unsigned lds) const {
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      const bool second = wbase + c * NTH >= HALF;
+      const int r = min(row[c], last);
+      stage16(second ? b : a, (unsigned)(r * (second ? bs : as) + chunk[c]), lds + (wbase + c * NTH) * 16);
+    }
+  }
+};
+
+__device__ __forceinline__ float sum_quads(float v) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float max_quads(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_wave(float v) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v += shfl_xor(v, o);
+  return v;
+}
+
+// By the bits: a difference v - v may be fused with the product that v comes from.
+__device__ __forceinline__ bool finite1(float v) { return (__float_as_uint(v) & 0x7FFFFFFFu) < 0x7F800000u; }
+__device__ __forceinline__ bool finite4(f32x4 v) { return finite1(v[0]) && finite1(v[1]) && finite1(v[2]) && finite1(v[3]); }
+
+// One row of a head over the wave: element e of lane l is dimension e * 64 + l.
+template <typename T, int D> struct LaneRow {
+  static constexpr int N = (D + kWave - 1) / kWave;
+  float v[N];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int d = e * kWave + lane_id();
+      v[e] = d < D ? to_f<T>(p[d]) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = 0.f;
+  }
+  __device__ __forceinline__ void store(T* p, float f) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int d = e * kWave + lane_id();
+      if (d < D) p[d] = from_f<T>(v[e] * f);
+    }
+  }
+  __device__ __forceinline__ void add(float f, const LaneRow& o) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e * kWave + lane_id() < D) v[e] = fmaf(f, o.v[e], v[e]);
+  }
+  __device__ __forceinline__ float dot(const LaneRow& o) const {
+    float t = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) t = fmaf(v[e], o.v[e], t);
+    return sum_wave(t);
+  }
+  // every element is NaN: nothing that is added changes it
+  __device__ __forceinline__ bool all_nan() const {
+    bool all = true;
+#pragma unroll
+    for (int e = 0; e < N; ++e) all &= e * kWave + lane_id() >= D || v[e] != v[e];
+    return __builtin_amdgcn_ballot_w64(!all) == 0;
+  }
+};
+
+}  // namespace tlf

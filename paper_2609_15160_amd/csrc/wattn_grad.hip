@@ -1,0 +1,570 @@
+// Gradients of the causal attention of ragged rows with a sliding window and sinks:
+// the C entry points tlf_attn_grad_ws_bytes and tlf_attn_grad and their kernels.
+//
+//   P = exp2(scale log2(e) q . k - lse),  dP = do . v,  delta = do . o
+//   dS = P (dP - delta),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T do
+//
+// Two passes, each with its sums in registers and no atomics, so that results are
+// the same from call to call: k_wattn_dq owns queries (three products, and delta),
+// k_wattn_dkv owns keys (four products).  That the scores and dP are computed twice
+// costs less than dS in memory would.  P and dS are rounded to bf16 as operands of
+// the next products with bf16 tensors; all else is float32.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "tlf.h"
+#include "wattn.h"
+
+namespace tlf {
+
+int wattn_check(const tlf_attn_shape* t);
+WAttnArgs wattn_args(const tlf_attn_shape& t);
+
+namespace {
+
+struct GradArgs : WAttnArgs {
+  int64_t dqs, dks, dvs;
+  int sink_parts;  // ranges of the queries of a sequence's first key tile, where it has sinks
+};
+
+// One query's row again from its visible keys alone (slow_row of the forward pass says why).
+template <typename T, int D>
+__device__ __forceinline__ void slow_dq(const GradArgs& a, const WSeq& s, int h, int row) {
+  const int kvh = h / (a.heads / a.kv_heads), p = row + s.n - s.nq;
+  const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
+  const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
+  LaneRow<T, D> q, d, x, o;
+  q.load(reinterpret_cast<const T*>(a.q) + (int64_t)(s.q0 + row) * a.qs + h * D);
+  d.load(reinterpret_cast<const T*>(a.dout) + (int64_t)(s.q0 + row) * a.os + h * D);
+  x.load(reinterpret_cast<const T*>(a.o) + (int64_t)(s.q0 + row) * a.os + h * D);
+  const float delta = d.dot(x), lse = a.lse[(int64_t)h * a.rows_q + s.q0 + row];
+  o.zero();
+  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
+  for (int i = 0; i < sinks + p + 1 - near; ++i) {
+    const int64_t j = i < sinks ? i : near + i - sinks;
+    x.load(v + j * a.vs);
+    const float dp = d.dot(x);
+    x.load(k + j * a.ks);
+    o.add(__builtin_amdgcn_exp2f(fmaf(q.dot(x), a.scale_log2, -lse)) * (dp - delta), x);
+    if (o.all_nan()) break;
+  }
+  o.store(reinterpret_cast<T*>(a.dq) + (int64_t)(s.q0 + row) * a.dqs + h * D, a.scale);
+}
+
+// One key's rows again from the queries that see it.
+template <typename T, int D>
+__device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int kvh, int key) {
+  const int each = a.heads / a.kv_heads, off = s.n - s.nq;
+  LaneRow<T, D> k, v, q, d, dk, dv;
+  k.load(reinterpret_cast<const T*>(a.k) + (int64_t)(s.k0 + key) * a.ks + kvh * D);
+  v.load(reinterpret_cast<const T*>(a.v) + (int64_t)(s.k0 + key) * a.vs + kvh * D);
+  dk.zero();
+  dv.zero();
+  const int last = key < a.sinks || a.window > s.n - 1 - key ? s.n - 1 : key + a.window - 1;
+  for (int h = kvh * each; h < (kvh + 1) * each; ++h)
+    for (int j = max(0, key - off); j <= last - off && !(dk.all_nan() && dv.all_nan()); ++j) {
+      const int64_t row = s.q0 + j;
+      q.load(reinterpret_cast<const T*>(a.q) + row * a.qs + h * D);
+      d.load(reinterpret_cast<const T*>(a.dout) + row * a.os + h * D);
+      const float w = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.scale_log2, -a.lse[(int64_t)h * a.rows_q + row]));
+      dv.add(w, d);
+      dk.add(w * (d.dot(v) - a.delta[(int64_t)h * a.rows_q + row]), q);
+    }
+  dk.store(reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D, a.scale);
+  dv.store(reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D, 1.f);
+}
+
+// Tiles, waves and LDS as the forward kernel's (k_wattn).  q and do of the wave's 32
+// queries stay in registers; a tile's keys are read as they lie and transposed, its
+// values as they lie.  dP starts from -delta, so dS = P dP takes one product.
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
+  using H = HeadRows<T, D>;
+  using O = Opnd<T>;
+  typedef typename O::frag Frag;
+  constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, PV = BN / H::ROWS, TL = O::TILES;
+  using Loader = PairLoader<T, D, BN, NW * kWave>;
+  __shared__ __align__(16) char lds[2 * Loader::BYTES];
+
+  const int u = xcd_run(blockIdx.x, gridDim.x), h = u / a.slots, slot = u - h * a.slots;
+  const int b = seq_of<BM>(a.q_off, a.rows_q, a.batch, slot);
+  const WSeq s = load_seq(a, b);
+  const int tile = (s.nq + BM - 1) / BM - 1 - (slot - slot_of<BM>(a.q_off, a.rows_q, b));
+  if (tile < 0) return;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
+  const int kvh = h / (a.heads / a.kv_heads), off = s.n - s.nq;
+  const int p0 = tile * BM + off, p1 = min(tile * BM + BM, s.nq) - 1 + off;
+  const int r0 = tile * BM + wave * QW;
+  const bool mine = r0 < s.nq;
+  const int pw0 = min(r0, s.nq - 1) + off, pw1 = min(r0 + QW, s.nq) - 1 + off;
+
+  int p[QN];
+  Frag qf[QN][KSTEPS], df[QN][KSTEPS];
+  float lse[QN], delta[QN];
+#pragma unroll
+  for (int qn = 0; qn < QN; ++qn) {
+    const int row = min(r0 + qn * 16 + c16, s.nq - 1);
+    p[qn] = row + off;
+    const int64_t at = s.q0 + row, wide = (int64_t)h * D + g * H::EPC;
+    const T* q = reinterpret_cast<const T*>(a.q) + at * a.qs + wide;
+    const T* d = reinterpret_cast<const T*>(a.dout) + at * a.os + wide;
+    const T* o = reinterpret_cast<const T*>(a.o) + at * a.os + wide;
+    float t = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+      qf[qn][ks] = *reinterpret_cast<const Frag*>(q + ks * 4 * H::EPC);
+      df[qn][ks] = *reinterpret_cast<const Frag*>(d + ks * 4 * H::EPC);
+      const Frag of = *reinterpret_cast<const Frag*>(o + ks * 4 * H::EPC);
+#pragma unroll
+      for (int e = 0; e < H::EPC; ++e) t = fmaf((float)df[qn][ks][e], (float)of[e], t);
+    }
+    delta[qn] = sum_quads(t);
+    lse[qn] = a.lse[(int64_t)h * a.rows_q + at];
+    if (g == 0 && r0 + qn * 16 + c16 < s.nq) a.delta[(int64_t)h * a.rows_q + at] = delta[qn];
+  }
+  int at[KSTEPS], att[H::TR];
+  H::direct(lane, at);
+  H::transposed(lane, att);
+  f32x4 dq[DT][QN];
+#pragma unroll
+  for (int qn = 0; qn < QN; ++qn)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dq[dt][qn] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  auto use = [&](int kt, const char* kb) __attribute__((always_inline)) {
+    const int k0 = kt * BN, k1 = k0 + BN - 1;
+    if (!mine || k0 > pw1 || (pw0 - k1 >= a.window && k0 >= a.sinks)) return;
+    const bool edge = k1 > pw0 || (pw1 - k0 >= a.window && k1 >= a.sinks);
+    const char* vb = kb + BN * H::RB;
+#pragma unroll
+    for (int t = 0; t < PV; ++t) {
+      f32x4 sc[QN][TL], dp[QN][TL];
+#pragma unroll
+      for (int n = 0; n < TL; ++n) {
+        const int row = t * H::ROWS + n * 16;
+#pragma unroll
+        for (int qn = 0; qn < QN; ++qn) {
+          sc[qn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+          dp[qn][n] = f32x4{-delta[qn], -delta[qn], -delta[qn], -delta[qn]};
+        }
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+          const Frag kf = H::load(kb, row, at[ks]), vf = H::load(vb, row, at[ks]);
+#pragma unroll
+          for (int qn = 0; qn < QN; ++qn) {
+            sc[qn][n] = O::mma(kf, qf[qn][ks], sc[qn][n]);
+            dp[qn][n] = O::mma(vf, df[qn][ks], dp[qn][n]);
+          }
+        }
+#pragma unroll
+        for (int qn = 0; qn < QN; ++qn)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            dp[qn][n][r] *= __builtin_amdgcn_exp2f(fmaf(sc[qn][n][r], a.scale_log2, -lse[qn]));
+        if (edge) {
+#pragma unroll
+          for (int qn = 0; qn < QN; ++qn)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int x = k0 + row + 4 * g + r;
+              if (!sees(p[qn] - x, x, a.window, a.sinks)) dp[qn][n][r] = 0.f;
+            }
+        }
+      }
+      Frag pf[QN];
+#pragma unroll
+      for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(dp[qn]);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const Frag kf = H::load_t(kb, t * H::ROWS, att, dt);
+#pragma unroll
+        for (int qn = 0; qn < QN; ++qn) dq[dt][qn] = O::mma(kf, pf[qn], dq[dt][qn]);
+      }
+    }
+  };
+
+  if (s.n > 0 && p1 >= 0) {
+    Loader ld;
+    ld.init();
+    const int first = max(0, max(p0, 0) - a.window + 1) / BN, last = p1 / BN;
+    const int sinks = min((min(a.sinks, s.n) + BN - 1) / BN, first), count = sinks + last - first + 1;
+    const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
+    const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
+    const unsigned base = lds_offset(lds);
+    auto issue = [&](int i) __attribute__((always_inline)) {
+      const int row = (i < sinks ? i : first + i - sinks) * BN;
+      ld.issue(k + row * a.ks, v + row * a.vs, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), s.n - 1 - row,
+               base + (i & 1) * Loader::BYTES);
+    };
+    issue(0);
+    for (int i = 0; i < count; ++i) {
+      wait_barrier<0>();
+      if (i + 1 < count) issue(i + 1);
+      use(i < sinks ? i : first + i - sinks, lds + (i & 1) * Loader::BYTES);
+    }
+  }
+  if (!mine) return;
+#pragma unroll
+  for (int qn = 0; qn < QN; ++qn) {
+    const int row = r0 + qn * 16 + c16;
+    bool good = true;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      dq[dt][qn] *= a.scale;
+      good &= finite4(dq[dt][qn]);
+    }
+    uint64_t again = __builtin_amdgcn_ballot_w64(!good && row < s.nq);
+    again |= again >> 32;
+    again = (again | again >> 16) & 0xFFFF;
+    if (row < s.nq && !(again >> c16 & 1)) {
+      T* dst = reinterpret_cast<T*>(a.dq) + (int64_t)(s.q0 + row) * a.dqs + h * D;
+      if constexpr (DT >= 2) {
+#pragma unroll
+        for (int dt = 0; dt < DT; dt += 2) store_pair<T>(dst + dt * 16, dq[dt][qn], dq[dt + 1][qn], lane);
+      } else {
+        Vec4<T>::store(dst + g * 4, dq[0][qn]);
+      }
+    }
+    for (; again; again &= again - 1) slow_dq<T, D>(a, s, h, r0 + qn * 16 + __builtin_ctzll(again));
+  }
+}
+
+// One workgroup: a tile of NW * KN * 16 keys of one key head, whose rows stay in
+// registers (each wave KN tiles of 16), over tiles of BQ queries of every head that
+// shares them; q and do, with their lse and delta, come through two places in LDS.
+// A tile's keys are seen by the queries from its first position to the window's end
+// behind its last; sinks by all from there: where a first tile has sinks, its queries
+// go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
+template <typename T, int D, int NW, int KN>
+__global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
+  using H = HeadRows<T, D>;
+  using O = Opnd<T>;
+  typedef typename O::frag Frag;
+  constexpr int KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 ? 64 : 32;
+  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, STEPS = BQ / H::ROWS, TL = O::TILES;
+  using Loader = PairLoader<T, D, BQ, NW * kWave>;
+  __shared__ __align__(16) char lds[2 * Loader::BYTES];
+  __shared__ __align__(16) float stats[2][2][kWave];  // of each place: lse, delta
+
+  const int sink_blocks = a.sink_parts > 1 ? a.batch * a.kv_heads * a.sink_parts : 0;
+  int b, kvh, tile, part = 0, parts = 1;
+  WSeq s;
+  if ((int)blockIdx.x < sink_blocks) {  // the longest first
+    part = blockIdx.x % a.sink_parts;
+    parts = a.sink_parts;
+    kvh = blockIdx.x / a.sink_parts % a.kv_heads;
+    b = blockIdx.x / (a.sink_parts * a.kv_heads);
+    s = load_seq(a, b);
+    tile = 0;
+    if (s.n == 0) return;
+  } else {
+    const int u = xcd_run(blockIdx.x - sink_blocks, gridDim.x - sink_blocks), slot = u % a.slots;
+    kvh = u / a.slots;
+    b = seq_of<KT>(a.k_off, a.rows_k, a.batch, slot);
+    s = load_seq(a, b);
+    tile = slot - slot_of<KT>(a.k_off, a.rows_k, b);
+    if (tile * KT >= s.cap || (tile == 0 && sink_blocks > 0 && s.n > 0)) return;
+  }
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
+  const int each = a.heads / a.kv_heads, off = s.n - s.nq;
+  const int k0 = tile * KT, k1 = min(k0 + KT, s.n) - 1;     // keys of the tile
+  const int w0 = k0 + wave * KW, w1 = min(w0 + KW, s.n) - 1;  // of the wave
+
+  Frag kf[KN][KSTEPS], vf[KN][KSTEPS];
+  int at[KSTEPS], att[H::TR];
+  H::direct(lane, at);
+  H::transposed(lane, att);
+  f32x4 dk[DT][KN], dv[DT][KN];
+#pragma unroll
+  for (int kn = 0; kn < KN; ++kn)
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) dk[dt][kn] = dv[dt][kn] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // queries [j0, j1] see a key of the tile
+  const int last = k0 < a.sinks || a.window > s.n - 1 - k1 ? s.n - 1 : k1 + a.window - 1;
+  const int j0 = max(0, k0 - off), j1 = last - off;
+  if (k0 < s.n && j0 <= j1) {
+#pragma unroll
+    for (int kn = 0; kn < KN; ++kn) {
+      const int64_t row = s.k0 + min(w0 + kn * 16 + c16, s.n - 1);
+      const T* k = reinterpret_cast<const T*>(a.k) + row * a.ks + kvh * D + g * H::EPC;
+      const T* v = reinterpret_cast<const T*>(a.v) + row * a.vs + kvh * D + g * H::EPC;
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        kf[kn][ks] = *reinterpret_cast<const Frag*>(k + ks * 4 * H::EPC);
+        vf[kn][ks] = *reinterpret_cast<const Frag*>(v + ks * 4 * H::EPC);
+      }
+    }
+    Loader ld;
+    ld.init();
+    const int tiles = (j1 - j0 + BQ) / BQ, all = tiles * each;
+    const int begin = (int)((int64_t)all * part / parts), end = (int)((int64_t)all * (part + 1) / parts);
+    const unsigned base = lds_offset(lds), sbase = lds_offset(stats);
+    int ih = begin / tiles, it = begin % tiles;  // head of the group and tile that are issued next
+    auto issue = [&](int place) __attribute__((always_inline)) {
+      const int h = kvh * each + ih, j = j0 + it * BQ, most = s.nq - 1 - j;
+      const int64_t row = s.q0 + j;
+      ld.issue(reinterpret_cast<const T*>(a.q) + row * a.qs + h * D, reinterpret_cast<const T*>(a.dout) + row * a.os + h * D,
+               (int)(a.qs * sizeof(T)), (int)(a.os * sizeof(T)), most, base + place * Loader::BYTES);
+      // 64 values each, of which the tile uses the first BQ
+      const int64_t stat = (int64_t)h * a.rows_q + row;
+      const unsigned to = sbase + place * (unsigned)sizeof(stats[0]), lane4 = (unsigned)min(lane, most) * 4u;
+      if (wave == 0) stage4(a.lse + stat, lane4, to);
+      if (wave == (NW > 1 ? 1 : 0)) stage4(a.delta + stat, lane4, to + (unsigned)sizeof(stats[0][0]));
+      if (++it == tiles) {
+        it = 0;
+        ++ih;
+      }
+    };
+    if (begin < end) issue(0);
+    int ut = begin % tiles;  // tile that is used next
+    for (int i = begin; i < end; ++i) {
+      const int place = (i - begin) & 1;
+      wait_barrier<0>();
+      if (i + 1 < end) issue(place ^ 1);
+      const int j = j0 + ut * BQ, jl = min(j + BQ - 1, j1), pa = j + off, pb = jl + off;
+      if (++ut == tiles) ut = 0;
+      if (w0 > w1 || pb < w0 || (pa - w1 >= a.window && w0 >= a.sinks)) continue;
+      const bool edge = pa < w1 || jl < j + BQ - 1 || (pb - w0 >= a.window && w1 >= a.sinks);
+      const char* qb = lds + place * Loader::BYTES;
+      const char* db = qb + BQ * H::RB;
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t) {
+        f32x4 sc[KN][TL], dp[KN][TL];
+#pragma unroll
+        for (int n = 0; n < TL; ++n) {
+          const int row = t * H::ROWS + n * 16;
+          const f32x4 lse = Vec4<float>::load(&stats[place][0][row + 4 * g]);
+          const f32x4 delta = Vec4<float>::load(&stats[place][1][row + 4 * g]);
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn) {
+            sc[kn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            dp[kn][n] = -delta;
+          }
+#pragma unroll
+          for (int ks = 0; ks < KSTEPS; ++ks) {
+            const Frag qf = H::load(qb, row, at[ks]), df = H::load(db, row, at[ks]);
+#pragma unroll
+            for (int kn = 0; kn < KN; ++kn) {
+              sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
+              dp[kn][n] = O::mma(df, vf[kn][ks], dp[kn][n]);
+            }
+          }
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              sc[kn][n][r] = __builtin_amdgcn_exp2f(fmaf(sc[kn][n][r], a.scale_log2, -lse[r]));
+              dp[kn][n][r] *= sc[kn][n][r];
+            }
+          if (edge) {
+#pragma unroll
+            for (int kn = 0; kn < KN; ++kn)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const int x = w0 + kn * 16 + c16, q = j + row + 4 * g + r;
+                if (q > j1 || !sees(q + off - x, x, a.window, a.sinks)) sc[kn][n][r] = dp[kn][n][r] = 0.f;
+              }
+          }
+        }
+        Frag pf[KN], sf[KN];
+#pragma unroll
+        for (int kn = 0; kn < KN; ++kn) {
+          pf[kn] = O::pack(sc[kn]);
+          sf[kn] = O::pack(dp[kn]);
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const Frag df = H::load_t(db, t * H::ROWS, att, dt), qf = H::load_t(qb, t * H::ROWS, att, dt);
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn) {
+            dv[dt][kn] = O::mma(df, pf[kn], dv[dt][kn]);
+            dk[dt][kn] = O::mma(qf, sf[kn], dk[dt][kn]);
+          }
+        }
+      }
+    }
+  }
+  if (parts > 1) {  // [batch][key head][part][key][dk, dv]
+    float* dst = a.part + ((int64_t)(b * a.kv_heads + kvh) * parts + part) * KT * 2 * D;
+#pragma unroll
+    for (int kn = 0; kn < KN; ++kn) {
+      float* row = dst + (wave * KW + kn * 16 + c16) * 2 * D + 4 * g;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        Vec4<float>::store(row + dt * 16, dk[dt][kn]);
+        Vec4<float>::store(row + D + dt * 16, dv[dt][kn]);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int kn = 0; kn < KN; ++kn) {
+    const int key = w0 + kn * 16 + c16;  // from n to cap: room without keys, zeros
+    bool good = true;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if (key >= s.n) dk[dt][kn] = dv[dt][kn] = f32x4{0.f, 0.f, 0.f, 0.f};
+      dk[dt][kn] *= a.scale;
+      good &= finite4(dk[dt][kn]) && finite4(dv[dt][kn]);
+    }
+    uint64_t again = __builtin_amdgcn_ballot_w64(!good);
+    again |= again >> 32;
+    again = (again | again >> 16) & 0xFFFF;
+    if (key < s.cap && !(again >> c16 & 1)) {
+      T* dkp = reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D;
+      T* dvp = reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D;
+      if constexpr (DT >= 2) {
+#pragma unroll
+        for (int dt = 0; dt < DT; dt += 2) {
+          store_pair<T>(dkp + dt * 16, dk[dt][kn], dk[dt + 1][kn], lane);
+          store_pair<T>(dvp + dt * 16, dv[dt][kn], dv[dt + 1][kn], lane);
+        }
+      } else {
+        Vec4<T>::store(dkp + g * 4, dk[0][kn]);
+        Vec4<T>::store(dvp + g * 4, dv[0][kn]);
+      }
+    }
+    for (; again; again &= again - 1) slow_dkv<T, D>(a, s, kvh, w0 + kn * 16 + __builtin_ctzll(again));
+  }
+}
+
+// The first tiles' sums over the ranges of their queries: a wave per key.
+template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wattn_sinks(GradArgs a) {
+  constexpr int N = (2 * D + kWave - 1) / kWave;
+  const int unit = blockIdx.x / (KT / 4), key = (blockIdx.x % (KT / 4)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int b = unit / a.kv_heads, kvh = unit % a.kv_heads, lane = lane_id();
+  const WSeq s = load_seq(a, b);
+  if (s.n == 0 || key >= s.cap) return;  // without keys the tile's own workgroup has written its zeros
+  T* dk = reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D;
+  T* dv = reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D;
+  const float* src = a.part + (int64_t)unit * a.sink_parts * KT * 2 * D + key * 2 * D;
+  float t[N];
+  bool good = true;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int d = e * kWave + lane;
+    t[e] = 0.f;
+    if (d < 2 * D && key < s.n)
+      for (int k = 0; k < a.sink_parts; ++k) t[e] += src[(int64_t)k * KT * 2 * D + d];
+    if (d < D) t[e] *= a.scale;
+    good &= finite1(t[e]);
+  }
+  if (__builtin_amdgcn_ballot_w64(!good)) {
+    slow_dkv<T, D>(a, s, kvh, key);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const int d = e * kWave + lane;
+    if (d < D) dk[d] = from_f<T>(t[e]);
+    else if (d < 2 * D) dv[d - D] = from_f<T>(t[e]);
+  }
+}
+
+constexpr int kManyWaves = 4;
+template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }  // KN: registers
+
+// Ranges of a first tile's queries, each as long as four other tiles' at least.
+int sink_parts(const tlf_attn_shape& t) {
+  if (t.window <= 0 || t.sinks <= 0 || t.batch <= 0) return 1;
+  const int64_t rows = t.rows_q / t.batch, other = 4 * ((int64_t)t.window + 128);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(16, rows / other));
+}
+
+bool many_keys(const tlf_attn_shape& t) { return slots_of<128>(t.rows_k, t.batch) * t.kv_heads >= 512; }
+
+int64_t delta_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }
+int64_t part_floats(const tlf_attn_shape& t) {
+  const int parts = many_keys(t) ? sink_parts(t) : 1;
+  return parts > 1 ? (int64_t)t.batch * t.kv_heads * parts * 128 * 2 * t.head_dim : 0;
+}
+
+template <typename T, int D, int NW> hipError_t launch_keys(const tlf_attn_shape& t, GradArgs a, hipStream_t s) {
+  constexpr int KN = key_tiles<T, D>(), KT = NW * KN * 16;
+  a.slots = (int)slots_of<KT>(t.rows_k, t.batch);
+  const int64_t sinks = a.sink_parts > 1 ? (int64_t)a.batch * a.kv_heads * a.sink_parts : 0;
+  hipLaunchKernelGGL((k_wattn_dkv<T, D, NW, KN>), dim3((unsigned)(sinks + (int64_t)a.slots * a.kv_heads)), dim3(NW * kWave), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sinks == 0) return e;
+  hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / 4))), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, GradArgs a, hipStream_t s) {
+  if (t.rows_q > 0) {
+    a.slots = (int)slots_of<128>(t.rows_q, t.batch);
+    if ((int64_t)a.slots * t.heads >= 512) {
+      hipLaunchKernelGGL((k_wattn_dq<T, D, 4>), dim3((unsigned)(a.slots * t.heads)), dim3(4 * kWave), 0, s, a);
+    } else {
+      a.slots = (int)slots_of<32>(t.rows_q, t.batch);
+      hipLaunchKernelGGL((k_wattn_dq<T, D, 1>), dim3((unsigned)(a.slots * t.heads)), dim3(kWave), 0, s, a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (t.rows_k == 0) return hipSuccess;
+  a.sink_parts = many_keys(t) ? sink_parts(t) : 1;
+  return many_keys(t) ? launch_keys<T, D, kManyWaves>(t, a, s) : launch_keys<T, D, 1>(t, a, s);
+}
+
+}  // namespace
+
+}  // namespace tlf
+
+extern "C" {
+
+int tlf_attn_grad_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes) {
+  const int st = tlf::wattn_check(shape);
+  if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
+  *ws_bytes = (size_t)(tlf::delta_floats(*shape) + tlf::part_floats(*shape)) * sizeof(float);
+  return TLF_OK;
+}
+
+int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q, const void* d_k, const void* d_v,
+                  const void* d_o, const float* d_lse, void* d_dq, int64_t dq_stride, void* d_dk, int64_t dk_stride,
+                  void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream) {
+  size_t need = 0;
+  const int st = tlf_attn_grad_ws_bytes(shape, &need);
+  if (st != TLF_OK) return st;
+  const int64_t per = shape->dtype == TLF_DTYPE_BF16 ? 8 : 4, wide = (int64_t)shape->heads * shape->head_dim;
+  const int64_t kv_wide = (int64_t)shape->kv_heads * shape->head_dim;
+  if (dq_stride < wide || dk_stride < kv_wide || dv_stride < kv_wide || dq_stride % per || dk_stride % per || dv_stride % per)
+    return TLF_E_INVALID_ARG;
+  if (std::max({dq_stride, dk_stride, dv_stride}) > TLF_ATTN_MAX_STRIDE) return TLF_E_UNSUPPORTED;
+  if (shape->rows_q > 0 && (!d_do || !d_q || !d_o || !d_lse || !d_dq)) return TLF_E_INVALID_ARG;
+  if (shape->rows_k > 0 && (!d_k || !d_v || !d_dk || !d_dv)) return TLF_E_INVALID_ARG;
+  if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
+  for (const void* p : {d_do, d_q, d_k, d_v, d_o, (const void*)d_dq, (const void*)d_dk, (const void*)d_dv, (const void*)d_workspace})
+    if (((uintptr_t)p & 15u) != 0) return TLF_E_INVALID_ARG;
+  for (const void* p : {(const void*)d_lse, (const void*)shape->d_q_offsets, (const void*)shape->d_k_offsets, (const void*)shape->d_k_lengths})
+    if (((uintptr_t)p & 3u) != 0) return TLF_E_INVALID_ARG;
+  tlf::GradArgs a{};
+  static_cast<tlf::WAttnArgs&>(a) = tlf::wattn_args(*shape);
+  a.q = d_q;
+  a.k = d_k;
+  a.v = d_v;
+  a.o = d_o;
+  a.dout = d_do;
+  a.lse = const_cast<float*>(d_lse);
+  a.dq = d_dq;
+  a.dk = d_dk;
+  a.dv = d_dv;
+  a.dqs = dq_stride;
+  a.dks = dk_stride;
+  a.dvs = dv_stride;
+  a.delta = (float*)d_workspace;
+  a.part = a.delta + tlf::delta_floats(*shape);
+  const hipStream_t s = (hipStream_t)stream;
+  const bool h = shape->dtype == TLF_DTYPE_BF16;
+  const hipError_t e = shape->head_dim == 16    ? tlf::launch<float, 16>(*shape, a, s)
+                       : shape->head_dim == 64  ? (h ? tlf::launch<bf16, 64>(*shape, a, s) : tlf::launch<float, 64>(*shape, a, s))
+                                                : (h ? tlf::launch<bf16, 128>(*shape, a, s) : tlf::launch<float, 128>(*shape, a, s));
+  return e == hipSuccess ? TLF_OK : TLF_E_HIP;
+}
+
+}  // extern "C"

@@ -96,7 +96,7 @@ EXPORTS = ("tlf_init", "tlf_prefill", "tlf_decode_step", "tlf_cache_stats", "tlf
            "tlf_status_str", "tlf_gs_plan", "tlf_gs_plan_ws", "tlf_gs_plan_noalloc", "tlf_gs_gather",
            "tlf_gs_scatter", "tlf_gs_expand", "tlf_ste", "tlf_probe_read", "tlf_rms_norm",
            "tlf_rms_norm_grad_ws_bytes", "tlf_rms_norm_grad", "tlf_ffn_ws_bytes", "tlf_ffn", "tlf_ffn_grad_ws_bytes", "tlf_ffn_grad",
-           "tlf_adamw")
+           "tlf_adamw", "tlf_attn_ws_bytes", "tlf_attn", "tlf_attn_grad_ws_bytes", "tlf_attn_grad")
 
 PROBE_READ_GRAIN = 32768
 
@@ -122,6 +122,21 @@ class AdamwTensor(ctypes.Structure):
         ("d_m", ctypes.c_void_p), ("d_v", ctypes.c_void_p), ("d_m_scale", ctypes.c_void_p),
         ("d_v_scale", ctypes.c_void_p), ("n", ctypes.c_int64), ("step", ctypes.c_int64),
         ("weight_decay", ctypes.c_double), ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+    ]
+
+
+ATTN_MAX_SINKS = 64
+ATTN_MAX_STRIDE = 1 << 22
+
+
+class AttnShape(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("rows_q", ctypes.c_int32), ("rows_k", ctypes.c_int32),
+        ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+        ("o_stride", ctypes.c_int64), ("d_q_offsets", ctypes.c_void_p), ("d_k_offsets", ctypes.c_void_p),
+        ("d_k_lengths", ctypes.c_void_p),
     ]
 
 
@@ -194,6 +209,13 @@ def load(path: str = LIB_PATH):
     lib.tlf_ffn_grad_ws_bytes.argtypes = [i32, i32, i32, i32, psz]
     lib.tlf_ffn_grad.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.tlf_adamw.argtypes = [ctypes.POINTER(AdamwTensor), i32, f64, f64, f64, f64, vp]
+    shape, i64 = ctypes.POINTER(AttnShape), ctypes.c_int64
+    lib.tlf_attn_ws_bytes.argtypes = [shape, psz]
+    lib.tlf_attn.argtypes = [shape, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tlf_attn_grad_ws_bytes.argtypes = [shape, psz]
+    lib.tlf_attn_grad.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+    for fn in (lib.tlf_attn_ws_bytes, lib.tlf_attn, lib.tlf_attn_grad_ws_bytes, lib.tlf_attn_grad):
+        fn.restype = ctypes.c_int
     for fn in (lib.tlf_rms_norm, lib.tlf_rms_norm_grad_ws_bytes, lib.tlf_rms_norm_grad, lib.tlf_ffn_ws_bytes, lib.tlf_ffn,
                lib.tlf_ffn_grad_ws_bytes, lib.tlf_ffn_grad, lib.tlf_adamw):
         fn.restype = ctypes.c_int

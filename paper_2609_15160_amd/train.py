@@ -405,6 +405,136 @@ def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch
     return _Ffn.apply(_aligned(x), _aligned(w_gate_up), _aligned(w_down), _wants_grad(x, w_gate_up, w_down))
 
 
+# ---------------------------------------------------------------------------
+# The block's attention: causal, over ragged rows, with a sliding window and sinks
+# ---------------------------------------------------------------------------
+
+def _rows_of_heads(t: torch.Tensor, heads: int, width: int) -> torch.Tensor:
+    """`t` ([rows, heads, width], or [rows, heads * width]) as it lies if a row's elements are contiguous and its rows
+    are 16-byte aligned, else copied."""
+    want = (width, 1) if t.dim() == 3 else (1,)
+    lies = all(n == 1 or s == w for n, s, w in zip(t.shape[1:], t.stride()[1:], want))
+    each = t.element_size()
+    if lies and t.data_ptr() % 16 == 0 and (t.shape[0] <= 1 or heads * width <= t.stride(0) <= tlf.ATTN_MAX_STRIDE and
+                                            t.stride(0) * each % 16 == 0):
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+def _row_stride(t: torch.Tensor, wide: int) -> int:
+    return t.stride(0) if t.shape[0] > 1 else -(-wide // 8) * 8
+
+
+class _Attention(torch.autograd.Function):
+    """q, k and v as they lie in one tensor of rows q | k | v (self_attention), or as three."""
+    @staticmethod
+    def forward(ctx, x, k, v, offsets, k_offsets, k_lengths, heads, kv_heads, width, window, sinks, scale, grad):
+        packed = k is None
+        q = _rows_of_heads(x, heads + 2 * kv_heads if packed else heads, width)
+        if packed:
+            q, k, v = q, q[:, heads * width:], q[:, (heads + kv_heads) * width:]
+        else:
+            k, v = _rows_of_heads(k, kv_heads, width), _rows_of_heads(v, kv_heads, width)
+        o = torch.empty((q.shape[0], heads * width) if packed else (q.shape[0], heads, width), dtype=q.dtype, device=q.device)
+        qw, kw = heads * width, kv_heads * width
+        strides = (_row_stride(q, qw + 2 * kw), _row_stride(q, qw + 2 * kw), _row_stride(q, qw + 2 * kw)) if packed else \
+            (_row_stride(q, qw), _row_stride(k, kw), _row_stride(v, kw))
+        ctx.numbers = (_DTYPE[q.dtype], offsets.numel() - 1, heads, kv_heads, width, q.shape[0], k.shape[0], window, sinks,
+                       scale, *strides, qw)
+        shape = _attn_shape(ctx.numbers, offsets, k_offsets, k_lengths)
+        lse = torch.empty((heads, q.shape[0]), dtype=torch.float32, device=q.device) if grad else None
+        ws, n = _workspace(tlf.load().tlf_attn_ws_bytes, shape, device=q.device)
+        _run(tlf.load().tlf_attn, q.device, shape, q, k, v, o, lse, ws, n)
+        if grad:
+            ctx.packed = packed
+            ctx.save_for_backward(q, None if packed else k, None if packed else v, offsets, k_offsets, k_lengths, o, lse)
+        return o
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, saved, do):
+        q, k, v, offsets, k_offsets, k_lengths, o, lse = saved
+        _, _, heads, kv_heads, width = ctx.numbers[:5]
+        qw, kw = heads * width, kv_heads * width
+        do = _aligned(do)
+        if ctx.packed:
+            k, v = q[:, qw:], q[:, qw + kw:]
+            dx = torch.empty((q.shape[0], qw + 2 * kw), dtype=q.dtype, device=q.device)
+            dq, dk, dv, strides = dx, dx[:, qw:], dx[:, qw + kw:], (qw + 2 * kw,) * 3
+        else:
+            dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+            strides = (qw, kw, kw)
+        shape = _attn_shape(ctx.numbers, offsets, k_offsets, k_lengths)
+        ws, n = _workspace(tlf.load().tlf_attn_grad_ws_bytes, shape, device=q.device)
+        _run(tlf.load().tlf_attn_grad, q.device, shape, do, q, k, v, o, lse, dq, strides[0], dk, strides[1], dv, strides[2],
+             ws, n)
+        grads = (dx, None, None) if ctx.packed else (dq, dk, dv)
+        return (*grads, *(None,) * 10)
+
+
+def _attn_shape(numbers, offsets, k_offsets, k_lengths) -> tlf.AttnShape:
+    return tlf.AttnShape(*numbers, offsets.data_ptr(), k_offsets.data_ptr(), None if k_lengths is None else k_lengths.data_ptr())
+
+
+def _attend(name, q, k, v, offsets, k_offsets, k_lengths, heads, kv_heads, width, window, sinks, scale):
+    if q.dtype not in _DTYPE or not q.is_cuda:
+        raise ValueError(f"{name}: float32 or bfloat16 CUDA tensors expected")
+    if heads < 1 or kv_heads < 1 or heads % kv_heads:
+        raise ValueError(f"{name}: {heads} heads are no multiple of {kv_heads} key heads")
+    k_offsets = offsets if k_offsets is None else k_offsets
+    for t in (offsets, k_offsets, k_lengths):
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1):
+            raise ValueError(f"{name}: offsets and lengths are int32 vectors")
+    if offsets.numel() < 1 or k_offsets.numel() != offsets.numel() or \
+            (k_lengths is not None and k_lengths.numel() != offsets.numel() - 1):
+        raise ValueError(f"{name}: one offset more than sequences, one length each")
+    if window is not None and window < 1 or sinks < 0:
+        raise ValueError(f"{name}: window {window}, sinks {sinks}")
+    _int32(name, q, k, v)
+    _same_device(q, k, v, offsets, k_offsets, k_lengths)
+    at = (offsets.contiguous(), k_offsets.contiguous(), None if k_lengths is None else k_lengths.contiguous())
+    return _Attention.apply(q, k, v, *at, heads, kv_heads, width, min(window or 0, (1 << 31) - 1), sinks,
+                            width ** -0.5 if scale is None else float(scale), _wants_grad(q, k, v))
+
+
+def self_attention(qkv: torch.Tensor, offsets: torch.Tensor, heads: int, kv_heads: int = None, window: int = None,
+                   sinks: int = 0, scale: float = None) -> torch.Tensor:
+    """Causal attention within each sequence of rows q | k | v (qkv [rows, (heads + 2 kv_heads) * width], as the block's
+    QKV projection gives them), with the gradient to qkv, one tensor.  Returns [rows, heads * width].
+
+    offsets: int32, where each sequence's rows begin, and the total (LoopPlan.offsets).  With a `window` a row sees the
+    last `window` rows of its sequence, itself included, and the first `sinks` ones; without it every earlier row.  heads
+    is a multiple of kv_heads (heads by default): consecutive heads share a key head.  Width 64 or 128 (16 too in
+    float32), sinks 64 at most, scale 1 / sqrt(width) by default.  Rows behind the last sequence give zeros.  What a row
+    does not see takes no part, whatever its values.  Scores, softmax and sums are float32; of bfloat16 tensors the
+    weights, and in the backward pass the gradients of the scores, are rounded to bfloat16 as operands."""
+    kv_heads = heads if kv_heads is None else kv_heads
+    if qkv.dim() != 2 or heads < 1 or kv_heads < 1 or qkv.shape[1] % (heads + 2 * kv_heads):
+        raise ValueError(f"self_attention: qkv {tuple(qkv.shape)}, expected [rows, ({heads} + 2 x {kv_heads}) * width]")
+    width = qkv.shape[1] // (heads + 2 * kv_heads)
+    return _attend("self_attention", qkv, None, None, offsets, None, None, heads, kv_heads, width, window, sinks, scale)
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, k_offsets: torch.Tensor = None,
+              k_lengths: torch.Tensor = None, window: int = None, sinks: int = 0, scale: float = None) -> torch.Tensor:
+    """Causal attention of each sequence's rows of q ([rows, heads, width]) to its rows of k and v ([k_rows, kv_heads,
+    width]), with gradients to all three.  As self_attention; a sequence's last query stands at its last key.
+
+    offsets, k_offsets: int32, where each sequence's rows of q, and of k and v, begin, and their ends (k_offsets: as
+    offsets).  k_lengths: int32, how many rows each sequence holds of those up to the next one's begin (all by default):
+    the new tokens' rows against a cache that has room for more.  A row that sees nothing gives zeros.  Rows of heads
+    may lie in wider ones (a stride that is a multiple of 16 bytes); else they are copied."""
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError(f"attention: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}; expected [rows, heads, "
+                         "width], twice [k_rows, kv_heads, width]")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("attention: q, k and v are of one dtype")
+    if k_offsets is None and k.shape[0] != q.shape[0]:
+        raise ValueError("attention: k and v of other rows than q need k_offsets")
+    return _attend("attention", q, k, v, offsets, k_offsets, k_lengths, q.shape[1], k.shape[1], q.shape[2], window, sinks,
+                   scale)
+
+
 def _moment(state, like, dtype8, name):
     """(moment tensor, scales or None) of one parameter, checked."""
     t, s = state if isinstance(state, (tuple, list)) else (state, None)
