@@ -577,6 +577,65 @@ int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q
                   const void* d_o, const float* d_lse, void* d_dq, int64_t dq_stride, void* d_dk, int64_t dk_stride,
                   void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream);
 
+/* The gated residual of the block with the norm that follows (Section 3.1,
+ * Appendix A: x + (1 + alpha) F, then the next operand's norm), in one pass:
+ *   t = y, or with post_norm y / sqrt(mean(y^2) + eps)
+ *   h = x + (1 + alpha[group]) t,  z = h r (1 + gamma[group]) with r = 1 / sqrt(mean(h^2) + eps)
+ *   d_x, d_h   [rows][d] float32: the residual rows before and after (one buffer for
+ *              both is allowed);
+ *   d_y, d_z   [rows][d] of y_dtype: what is added, and the next operand;
+ *   d_alpha, d_gamma  [groups][d] float32; either or, with groups = 0, both NULL (zeros);
+ *   d_group    [rows] as for tlf_rms_norm;
+ *   d_rstd, d_ystd    [rows] float32, receive r and (post_norm) y's
+ *              1 / sqrt(mean(y^2) + eps) for the gradients, or NULL.
+ * Sums and limits as tlf_rms_norm. */
+int tlf_residual_norm(const float* d_x, const void* d_y, int32_t y_dtype, const float* d_alpha, const float* d_gamma,
+                      const int32_t* d_group, int32_t groups, int32_t rows, int32_t d, int32_t post_norm, float eps,
+                      float* d_h, void* d_z, float* d_rstd, float* d_ystd, void* stream);
+
+/* Gradients of tlf_residual_norm from the gradients dh of h and dz of z (either may
+ * be NULL: zeros), its h, y, scales and the r's that it wrote:
+ *   u = dz (1 + gamma[group]),  dx = dh + r (u - h r^2 mean(u h)),  dt = dx (1 + alpha[group]),
+ *   dy = dt, or with post_norm ry (dt - y ry^2 mean(dt y)),
+ *   dalpha[k] = sum over the rows of group k of dx t,  dgamma[k] = of dz h r
+ *   d_dx [rows][d] float32, d_dy [rows][d] of y_dtype; d_dalpha and d_dgamma
+ *   [groups][d]: those of the scales that there are, or neither (NULL).
+ *   d_workspace: tlf_residual_norm_grad_ws_bytes bytes, used during the call only;
+ *   may be NULL without the scales' gradients. */
+int tlf_residual_norm_grad_ws_bytes(int32_t groups, int32_t rows, int32_t d, size_t* ws_bytes);
+int tlf_residual_norm_grad(const float* d_dh, const void* d_dz, const float* d_h, const void* d_y, int32_t y_dtype,
+                           const float* d_alpha, const float* d_gamma, const int32_t* d_group, int32_t groups,
+                           const float* d_rstd, const float* d_ystd, int32_t rows, int32_t d, int32_t post_norm, float* d_dx,
+                           void* d_dy, float* d_dalpha, float* d_dgamma, void* d_workspace, size_t ws_bytes, void* stream);
+
+/* The norm of all elements of many gradients, and the scale that clips them to
+ * max_norm, few launches for all:
+ *   *d_norm = sqrt(sum g^2),  *d_scale = 1 where that is at most max_norm, else max_norm / norm
+ * Summed in float64.  A norm that is not finite gives a scale of 0 or NaN.  d_scale
+ * may be NULL; max_norm > 0 may be infinite.  Gradients need the alignment of their
+ * elements only and may overlap.
+ *   h_grads: host array, read during the call.
+ *   d_workspace: tlf_grad_norm_ws_bytes bytes, 8-byte aligned, used during the call only. */
+typedef struct tlf_grad {
+  void* d_grad;
+  int64_t n;       /* elements, at most 2^35 */
+  int32_t dtype;
+  int32_t reserved;
+} tlf_grad;
+int tlf_grad_norm_ws_bytes(const tlf_grad* h_grads, int32_t count, size_t* ws_bytes);
+int tlf_grad_norm(const tlf_grad* h_grads, int32_t count, double max_norm, float* d_norm, float* d_scale, void* d_workspace,
+                  size_t ws_bytes, void* stream);
+
+/* g = g * *d_scale, rounded to its type; with a scale of 1 nothing is read or written.
+ * The gradients overlap neither each other nor the scale. */
+int tlf_grad_clip(const tlf_grad* h_grads, int32_t count, const float* d_scale, void* stream);
+
+/* tlf_adamw with gradients times *d_grad_scale, a device value (tlf_grad_norm's): the
+ * product is rounded to float32, with 8-bit moments not at all.  The scale overlaps
+ * nothing that is updated. */
+int tlf_adamw_scaled(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
+                     const float* d_grad_scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

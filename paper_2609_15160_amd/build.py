@@ -12,7 +12,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtlf.so")
 SOURCES = ["api.hip", "gemm.hip", "pgemm.hip", "dgemm.hip", "plan.hip", "attn.hip", "rows.hip", "cond.hip", "gs.hip",
-           "noalloc.hip", "probe.hip", "norm.hip", "ffn.hip", "adamw.hip", "wattn.hip", "wattn_grad.hip"]
+           "noalloc.hip", "probe.hip", "norm.hip", "ffn.hip", "adamw.hip", "wattn.hip", "wattn_grad.hip",
+           "resid.hip", "gradnorm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

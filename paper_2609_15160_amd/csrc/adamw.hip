@@ -61,6 +61,7 @@ struct AdamArgs {
   int32_t first[kAdamTensors + 1];  // workgroups before each tensor
   int32_t count;
   double b1, b2;
+  const float* scale;  // of the gradients, or NULL
   float eps;
 };
 static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
@@ -81,13 +82,15 @@ __device__ __forceinline__ float update(float p, float m, float v, const AdamTen
   return p * t.decay - t.rate * m * __builtin_amdgcn_rcpf(sqrtf(v) * t.root + eps);  // eps is normal
 }
 
-__global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
+// SCALED: gradients count times *a.scale (clipping), which costs no pass of their own.
+template <bool SCALED> __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
   const int k = tensor_of(a, blockIdx.x);
   const AdamTensor& t = a.t[k];
   const float b1 = (float)a.b1, b2 = (float)a.b2, c1 = (float)(1.0 - a.b1), c2 = (float)(1.0 - a.b2);
   float* m = reinterpret_cast<float*>(t.m);
   float* v = reinterpret_cast<float*>(t.v);
   const int64_t base = (int64_t)(blockIdx.x - a.first[k]) * kAdamPer;
+  const float scale = SCALED ? *a.scale : 1.f;
   if ((t.flags & kVector) && base + kAdamPer <= t.n) {
     f32x4 p4[kAdamUnroll], g4[kAdamUnroll], m4[kAdamUnroll], v4[kAdamUnroll];
 #pragma unroll
@@ -102,6 +105,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
 #pragma unroll
     for (int u = 0; u < kAdamUnroll; ++u) {
       const int64_t e = base + (u * kAdamThreads + threadIdx.x) * 4;
+      if (SCALED) g4[u] *= scale;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         m4[u][r] = b1 * m4[u][r] + c1 * g4[u][r];
@@ -116,7 +120,8 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
     return;
   }
   for (int64_t e = base + threadIdx.x; e < t.n && e < base + kAdamPer; e += kAdamThreads) {
-    const float g = t.flags & kGradBf16 ? (float)reinterpret_cast<const bf16*>(t.g)[e] : reinterpret_cast<const float*>(t.g)[e];
+    float g = t.flags & kGradBf16 ? (float)reinterpret_cast<const bf16*>(t.g)[e] : reinterpret_cast<const float*>(t.g)[e];
+    if (SCALED) g *= scale;
     const float m1 = b1 * m[e] + c1 * g, v1 = b2 * v[e] + c2 * (g * g);
     const float p = update(t.p[e], m1, v1, t, a.eps);
     t.p[e] = p;
@@ -154,13 +159,14 @@ __device__ __forceinline__ double moment(double b, double old, double c, double 
 }
 
 // One wave per block of 256 elements, four per lane.
-__global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
+template <bool SCALED> __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
   const int k = tensor_of(a, blockIdx.x);
   const AdamTensor& t = a.t[k];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   uint8_t* m = reinterpret_cast<uint8_t*>(t.m);
   uint8_t* v = reinterpret_cast<uint8_t*>(t.v);
   const double c1 = 1.0 - a.b1, c2 = 1.0 - a.b2;
+  const double scale = SCALED ? (double)*a.scale : 1.0;
 #pragma unroll 1
   for (int u = 0; u < kAdamUnroll; ++u) {
     const int64_t blk = (int64_t)(blockIdx.x - a.first[k]) * (kAdamPer / kBlock) + u * (kAdamThreads / kWave) + wave;
@@ -196,7 +202,7 @@ __global__ __launch_bounds__(kAdamThreads) void k_adamw8(AdamArgs a) {
     unsigned mtop = 0, vtop = 0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const double g = g4[r];
+      const double g = SCALED ? g4[r] * scale : (double)g4[r];
       m1[r] = moment(a.b1, (double)mo[r] * ms, c1, g);
       v1[r] = moment(a.b2, (double)vo[r] * vs, c2, g * g);
       mtop = max(mtop, magnitude((float)m1[r]));
@@ -259,14 +265,15 @@ int check(const tlf_adamw_tensor& t) {
 
 // What the step updates must overlap nothing else of the call, since the
 // workgroups run in no order; gradients may overlap each other.
-int check_overlap(const tlf_adamw_tensor* tensors, int32_t count) {
+int check_overlap(const tlf_adamw_tensor* tensors, int32_t count, const float* scale) {
   struct Range {
     uintptr_t begin, end;
     bool updated;
   };
-  const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[7 * (size_t)count + 1]);
+  const std::unique_ptr<Range[]> ranges(new (std::nothrow) Range[7 * (size_t)count + 2]);
   if (!ranges) return TLF_E_HIP;
   size_t n = 0;
+  if (scale) ranges[n++] = Range{(uintptr_t)scale, (uintptr_t)scale + sizeof(float), false};
   for (int i = 0; i < count; ++i) {
     const tlf_adamw_tensor& t = tensors[i];
     auto add = [&](const void* p, int64_t bytes, bool updated) {
@@ -292,35 +299,31 @@ int check_overlap(const tlf_adamw_tensor* tensors, int32_t count) {
   return TLF_OK;
 }
 
-}  // namespace
-
-}  // namespace tlf
-
-extern "C" int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2,
-                         double eps, void* stream) {
-  using namespace tlf;
+int step(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
+         const float* d_grad_scale, void* stream) {
   if (count < 0 || (count > 0 && !h_tensors) || !(lr >= 0.0) || !(lr < INFINITY) || !(beta1 >= 0.0) || !(beta1 < 1.0) ||
-      !(beta2 >= 0.0) || !(beta2 < 1.0) || !((float)eps >= FLT_MIN) || !((float)eps < INFINITY))
+      !(beta2 >= 0.0) || !(beta2 < 1.0) || !((float)eps >= FLT_MIN) || !((float)eps < INFINITY) || !aligned(d_grad_scale, 4))
     return TLF_E_INVALID_ARG;
   for (int i = 0; i < count; ++i) {
     const int st = check(h_tensors[i]);
     if (st != TLF_OK) return st;
   }
-  const int st = check_overlap(h_tensors, count);
+  const int st = check_overlap(h_tensors, count, d_grad_scale);
   if (st != TLF_OK) return st;
   for (int bits : {32, 8}) {
     AdamArgs a{};
     a.b1 = beta1;
     a.b2 = beta2;
     a.eps = (float)eps;
+    a.scale = d_grad_scale;
     for (int i = 0; i <= count; ++i) {
       const tlf_adamw_tensor* t = i < count ? &h_tensors[i] : nullptr;
       const bool take = t && t->state_bits == bits && t->n > 0;
       const int64_t blocks = take ? (t->n + kAdamPer - 1) / kAdamPer : 0;
       // full, or done
       if (a.count > 0 && (!t || (take && (a.count == kAdamTensors || a.first[a.count] + blocks > kAdamBlocks)))) {
-        if (bits == 32) hipLaunchKernelGGL(k_adamw, dim3(a.first[a.count]), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL(k_adamw8, dim3(a.first[a.count]), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
+        auto* kernel = bits == 32 ? (d_grad_scale ? k_adamw<true> : k_adamw<false>) : (d_grad_scale ? k_adamw8<true> : k_adamw8<false>);
+        hipLaunchKernelGGL(kernel, dim3(a.first[a.count]), dim3(kAdamThreads), 0, (hipStream_t)stream, a);
         if (hipGetLastError() != hipSuccess) return TLF_E_HIP;
         a.count = 0;
       }
@@ -347,3 +350,21 @@ extern "C" int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, doubl
   }
   return TLF_OK;
 }
+
+}  // namespace
+
+}  // namespace tlf
+
+extern "C" {
+
+int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
+              void* stream) {
+  return tlf::step(h_tensors, count, lr, beta1, beta2, eps, nullptr, stream);
+}
+
+int tlf_adamw_scaled(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, double beta1, double beta2, double eps,
+                     const float* d_grad_scale, void* stream) {
+  return d_grad_scale ? tlf::step(h_tensors, count, lr, beta1, beta2, eps, d_grad_scale, stream) : TLF_E_INVALID_ARG;
+}
+
+}  // extern "C"

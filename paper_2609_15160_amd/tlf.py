@@ -96,7 +96,9 @@ EXPORTS = ("tlf_init", "tlf_prefill", "tlf_decode_step", "tlf_cache_stats", "tlf
            "tlf_status_str", "tlf_gs_plan", "tlf_gs_plan_ws", "tlf_gs_plan_noalloc", "tlf_gs_gather",
            "tlf_gs_scatter", "tlf_gs_expand", "tlf_ste", "tlf_probe_read", "tlf_rms_norm",
            "tlf_rms_norm_grad_ws_bytes", "tlf_rms_norm_grad", "tlf_ffn_ws_bytes", "tlf_ffn", "tlf_ffn_grad_ws_bytes", "tlf_ffn_grad",
-           "tlf_adamw", "tlf_attn_ws_bytes", "tlf_attn", "tlf_attn_grad_ws_bytes", "tlf_attn_grad")
+           "tlf_adamw", "tlf_attn_ws_bytes", "tlf_attn", "tlf_attn_grad_ws_bytes", "tlf_attn_grad",
+           "tlf_residual_norm", "tlf_residual_norm_grad_ws_bytes", "tlf_residual_norm_grad", "tlf_grad_norm_ws_bytes",
+           "tlf_grad_norm", "tlf_grad_clip", "tlf_adamw_scaled")
 
 PROBE_READ_GRAIN = 32768
 
@@ -138,6 +140,10 @@ class AttnShape(ctypes.Structure):
         ("o_stride", ctypes.c_int64), ("d_q_offsets", ctypes.c_void_p), ("d_k_offsets", ctypes.c_void_p),
         ("d_k_lengths", ctypes.c_void_p),
     ]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("d_grad", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 def gs_plan_ws_bytes(rows: int) -> int:
@@ -214,7 +220,18 @@ def load(path: str = LIB_PATH):
     lib.tlf_attn.argtypes = [shape, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.tlf_attn_grad_ws_bytes.argtypes = [shape, psz]
     lib.tlf_attn_grad.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
-    for fn in (lib.tlf_attn_ws_bytes, lib.tlf_attn, lib.tlf_attn_grad_ws_bytes, lib.tlf_attn_grad):
+    lib.tlf_residual_norm.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.tlf_residual_norm_grad_ws_bytes.argtypes = [i32, i32, i32, psz]
+    lib.tlf_residual_norm_grad.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp,
+                                           sz, vp]
+    grads = ctypes.POINTER(Grad)
+    lib.tlf_grad_norm_ws_bytes.argtypes = [grads, i32, psz]
+    lib.tlf_grad_norm.argtypes = [grads, i32, f64, vp, vp, vp, sz, vp]
+    lib.tlf_grad_clip.argtypes = [grads, i32, vp, vp]
+    lib.tlf_adamw_scaled.argtypes = [ctypes.POINTER(AdamwTensor), i32, f64, f64, f64, f64, vp, vp]
+    for fn in (lib.tlf_attn_ws_bytes, lib.tlf_attn, lib.tlf_attn_grad_ws_bytes, lib.tlf_attn_grad, lib.tlf_residual_norm,
+               lib.tlf_residual_norm_grad_ws_bytes, lib.tlf_residual_norm_grad, lib.tlf_grad_norm_ws_bytes,
+               lib.tlf_grad_norm, lib.tlf_grad_clip, lib.tlf_adamw_scaled):
         fn.restype = ctypes.c_int
     for fn in (lib.tlf_rms_norm, lib.tlf_rms_norm_grad_ws_bytes, lib.tlf_rms_norm_grad, lib.tlf_ffn_ws_bytes, lib.tlf_ffn,
                lib.tlf_ffn_grad_ws_bytes, lib.tlf_ffn_grad, lib.tlf_adamw):

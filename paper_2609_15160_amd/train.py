@@ -265,7 +265,7 @@ class _NoSecond(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("rms_norm and ffn have no gradients of gradients")
+        raise RuntimeError("rms_norm, residual_norm, attention and ffn have no gradients of gradients")
 
 
 def _first_order(backward):
@@ -403,6 +403,77 @@ def ffn(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: torch.Tensor) -> torch
     _int32("ffn", x, w_gate_up)
     _same_device(x, w_gate_up, w_down)
     return _Ffn.apply(_aligned(x), _aligned(w_gate_up), _aligned(w_down), _wants_grad(x, w_gate_up, w_down))
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, y, alpha, gamma, group, eps, post, grad):
+        rows, d = x.shape
+        groups = next((t.numel() // d for t in (alpha, gamma) if t is not None), 0)
+        h, z = torch.empty_like(x), torch.empty_like(y)
+        stats = torch.empty((2, rows), dtype=torch.float32, device=x.device) if grad else None
+        rstd, ystd = (stats[0], stats[1] if post else None) if grad else (None, None)
+        _run(tlf.load().tlf_residual_norm, x.device, x, y, _DTYPE[y.dtype], alpha, gamma, group, groups, rows, d, post, eps,
+             h, z, rstd, ystd)
+        ctx.set_materialize_grads(False)
+        if grad:
+            ctx.post, ctx.groups = post, groups
+            ctx.save_for_backward(h, y, alpha, gamma, group, stats)
+        return h, z
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, saved, dh, dz):
+        h, y, alpha, gamma, group, stats = saved
+        rows, d = h.shape
+        if dh is None and dz is None:
+            return (None,) * 8
+        dh, dz = (None if t is None else _aligned(t) for t in (dh, dz))
+        dx, dy = torch.empty_like(h), torch.empty_like(y)
+        sums = any(ctx.needs_input_grad[2:4])
+        dalpha, dgamma = (torch.empty_like(t) if sums and t is not None else None for t in (alpha, gamma))
+        lib = tlf.load()
+        ws, n = None, 0
+        if sums:
+            ws, n = _workspace(lib.tlf_residual_norm_grad_ws_bytes, ctx.groups, rows, d, device=h.device)
+        _run(lib.tlf_residual_norm_grad, h.device, dh, dz, h, y, _DTYPE[y.dtype], alpha, gamma, group, ctx.groups, stats[0],
+             stats[1] if ctx.post else None, rows, d, ctx.post, dx, dy, dalpha, dgamma, ws, n)
+        return dx, dy, dalpha, dgamma, None, None, None, None
+
+
+def residual_norm(x: torch.Tensor, y: torch.Tensor, alpha: torch.Tensor = None, gamma: torch.Tensor = None,
+                  group: torch.Tensor = None, eps: float = 1e-5, post_norm: bool = False):
+    """(h, z): the residual rows h = x + (1 + alpha) y, and their RMSNorm z times 1 + gamma, the next block's operand, in
+    one pass, with gradients to x, y, alpha and gamma.
+
+    x and h are float32 [rows, d], y and z float32 or bfloat16.  alpha and gamma are None, one [d] or [1, d] scale, or
+    [groups, d] scales of which row r takes number group[r] (int32 [rows]; a row whose number is none of them takes none):
+    the AdaLN gate and modulation of each token's depth.  With post_norm y is divided by its own root mean square first: a
+    block with norms before and after.  Widths, groups, rows and sums as in rms_norm."""
+    if x.dim() != 2 or x.dtype != torch.float32 or not x.is_cuda:
+        raise ValueError("residual_norm: expected float32 [rows, d] CUDA residual rows")
+    if y.shape != x.shape or y.dtype not in _DTYPE:
+        raise ValueError(f"residual_norm: y {tuple(y.shape)} {y.dtype}, expected float32 or bfloat16 {tuple(x.shape)}")
+    d, groups = x.shape[1], None
+    for name, t in (("alpha", alpha), ("gamma", gamma)):
+        if t is None:
+            continue
+        if t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != d or t.numel() == 0:
+            raise ValueError(f"residual_norm: {name} {tuple(t.shape)} {t.dtype}, expected float32 [d] or [groups, d]")
+        if groups not in (None, t.numel() // d):
+            raise ValueError("residual_norm: alpha and gamma are of the same groups")
+        groups = t.numel() // d
+        if group is None and groups != 1:
+            raise ValueError("residual_norm: several scales need each row's group")
+    if group is not None:
+        if groups is None or group.dtype != torch.int32 or group.shape != (x.shape[0],):
+            raise ValueError("residual_norm: group is int32 [rows] and goes with alpha or gamma")
+        group = group.contiguous()
+    _int32("residual_norm", x, alpha, gamma)
+    _same_device(x, y, alpha, gamma, group)
+    alpha, gamma = (None if t is None else _aligned(t) for t in (alpha, gamma))
+    return _ResidualNorm.apply(_aligned(x), _aligned(y), alpha, gamma, group, float(eps), bool(post_norm),
+                               _wants_grad(x, y, alpha, gamma))
 
 
 # ---------------------------------------------------------------------------
@@ -553,8 +624,58 @@ def _given_twice(table) -> bool:
     return len(set(at)) < len(at)
 
 
+def _grad_table(name, grads):
+    table = (tlf.Grad * len(grads))()
+    for k, g in enumerate(grads):
+        if g.dtype not in _DTYPE or not g.is_cuda or not g.is_contiguous():
+            raise ValueError(f"{name}: gradients are contiguous float32 or bfloat16 CUDA tensors")
+        if g.device != grads[0].device:
+            raise ValueError(f"{name}: tensors on one device expected")
+        table[k] = tlf.Grad(g.data_ptr(), g.numel(), _DTYPE[g.dtype], 0)
+    return table
+
+
+def _grad_norm(name, grads, table, max_norm):
+    if max_norm is not None and not max_norm > 0:
+        raise ValueError(f"{name}: max_norm {max_norm}")
+    dev = grads[0].device
+    ws, n = _workspace(tlf.load().tlf_grad_norm_ws_bytes, table, len(grads), device=dev)
+    out = torch.empty(2, dtype=torch.float32, device=dev)
+    _run(tlf.load().tlf_grad_norm, dev, table, len(grads), float("inf") if max_norm is None else max_norm, out,
+         out.data_ptr() + 4, ws, n)
+    return out[0], out[1]
+
+
+def grad_norm(grads, max_norm: float = None):
+    """(norm, scale) of a list of gradients (contiguous float32 or bfloat16 CUDA tensors), both float32 on the device: the
+    norm of all their elements, summed in float64, and 1, or max_norm / norm where the norm is above max_norm (> 0).
+
+    The host does not wait.  adamw_ takes the scale as it is: clipping then costs no pass over the gradients.  A norm that
+    is not finite gives a scale of 0 or NaN."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("grad_norm: no gradients")
+    return _grad_norm("grad_norm", grads, _grad_table("grad_norm", grads), max_norm)
+
+
+@torch.no_grad()
+def clip_grad_norm_(grads, max_norm: float) -> torch.Tensor:
+    """Multiplies the gradients by grad_norm's scale in place, rounded to their types, and returns the norm that they had.
+    Gradients within the limit are not written.  They overlap nowhere."""
+    grads = list(grads)
+    if not grads:
+        raise ValueError("clip_grad_norm_: no gradients")
+    if max_norm is None:
+        raise ValueError("clip_grad_norm_: max_norm None")
+    table = _grad_table("clip_grad_norm_", grads)
+    norm, scale = _grad_norm("clip_grad_norm_", grads, table, max_norm)
+    _run(tlf.load().tlf_grad_clip, norm.device, table, len(grads), scale)
+    torch.autograd.graph.increment_version(grads)
+    return norm
+
+
 def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.95), eps: float = 1e-8,
-           weight_decay=0.0, copies=None) -> None:
+           weight_decay=0.0, copies=None, grad_scale: torch.Tensor = None) -> None:
     """One AdamW step over many tensors, in place (tlf_adamw; few launches for all of them).
 
     params       contiguous float32 CUDA tensors, updated
@@ -565,6 +686,7 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
                  captured into a graph is refused: its replays would repeat the corrections of one step
     weight_decay one value or one for each tensor
     copies       bfloat16 tensors that receive the updated parameters rounded, or None
+    grad_scale   a float32 CUDA value that the gradients count times (grad_norm's scale), or None
 
     What is updated overlaps nothing else of the call; gradients may overlap each other.  eps is at least the smallest
     normal float32.
@@ -579,6 +701,8 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
         return
     table = (tlf.AdamwTensor * n)()
     dev = params[0].device
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.device != dev):
+        raise ValueError("adamw_: grad_scale is one float32 value on the parameters' device")
     for k, (p, g, c) in enumerate(zip(params, grads, copies)):
         if p.dtype != torch.float32 or not p.is_cuda or not p.is_contiguous():
             raise ValueError("adamw_: parameters are contiguous float32 CUDA tensors")
@@ -602,7 +726,10 @@ def adamw_(params, grads, exp_avgs, exp_avg_sqs, step, lr: float, betas=(0.9, 0.
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("adamw_: the step number and rates are values and cannot be captured into a graph")
     try:
-        _run(tlf.load().tlf_adamw, dev, table, n, lr, betas[0], betas[1], eps)
+        if grad_scale is None:
+            _run(tlf.load().tlf_adamw, dev, table, n, lr, betas[0], betas[1], eps)
+        else:
+            _run(tlf.load().tlf_adamw_scaled, dev, table, n, lr, betas[0], betas[1], eps, grad_scale)
     except tlf.TlfError as e:
         if e.status == tlf.E_INVALID_ARG and _given_twice(table):
             raise ValueError("adamw_: a parameter, copy, moment or scale appears twice") from None
@@ -660,8 +787,14 @@ class AdamW:
                 m.copy_(torch.where(m.to(p.dtype) == p, m, p.float()))  # the same again if no step follows
 
     @torch.no_grad()
-    def step(self) -> None:
+    def step(self, max_norm: float = None):
+        """One step; with max_norm the gradients count times grad_norm's scale (they are left as they are), and their
+        norm is returned: a float32 value on the device, None without gradients."""
         have = [k for k, p in enumerate(self.params) if p.grad is not None]
+        grads = {k: self.params[k].grad.contiguous() for k in have}
+        norm = scale = None
+        if max_norm is not None and have:
+            norm, scale = grad_norm(grads.values(), max_norm)
         self._take_written(have)
         by = {}
         for k in have:
@@ -670,11 +803,12 @@ class AdamW:
             pick = lambda v: [v[k] for k in at]  # noqa: E731
             real = [self.params[k].detach() if self.masters[k] is None else self.masters[k] for k in at]
             copies = [None if self.masters[k] is None else self.params[k].detach() for k in at]
-            adamw_(real, [self.params[k].grad.contiguous() for k in at], pick(self.exp_avgs), pick(self.exp_avg_sqs),
-                   [self.steps[k] + 1 for k in at], self.lr, self.betas, self.eps, pick(self.weight_decay), copies)
+            adamw_(real, pick(grads), pick(self.exp_avgs), pick(self.exp_avg_sqs), [self.steps[k] + 1 for k in at], self.lr,
+                   self.betas, self.eps, pick(self.weight_decay), copies, **({} if scale is None else {"grad_scale": scale}))
             for k in at:
                 self.steps[k] += 1
                 self._written[k] = _writes(self.params[k])
+        return norm
 
     def zero_grad(self) -> None:
         for p in self.params:

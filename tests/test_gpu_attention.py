@@ -198,3 +198,163 @@ def test_sharp_and_growing_scores(dtype, D):
     o = train.attention(q, k, v, _offsets([n]), window=250, sinks=2)
     r = O.attention(_np(q), _np(k), _np(v), 250, 2)
     _within(o, r["o"], bounds(_np(q), _np(k), _np(v), r, 250, 2, D ** -0.5, dtype)["o"], "o")
+
+
+# ---------------------------------------------------------------------------
+# What is not seen takes no part, whatever its values; layouts, streams, order
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, D, bad):
+    """One key's values, another's key and one query's gradient not finite: the rows that see none of them are the
+    same as without, to the bounds; those that do are not finite."""
+    train = _train()
+    rng = np.random.default_rng(21)
+    n, heads = 150, 2
+    q, k, v, do = (_normal(rng, n, heads, D, dtype=dtype) for _ in range(4))
+    for window, sinks in ((None, 0), (40, 0), (40, 3)):
+        vb, kb, db = v.clone(), k.clone(), do.clone()
+        vb[70, 0, 5] = bad
+        kb[90, 1] = float("nan")
+        db[100, 0, 3] = bad
+        leaves = [t.clone().requires_grad_() for t in (q, kb, vb)]
+        o = train.attention(*leaves, _offsets([n]), window=window, sinks=sinks)
+        got = dict(zip(("o", "dq", "dk", "dv"), (o, *torch.autograd.grad(o, leaves, db))))
+        r = O.attention(_np(q), _np(kb), _np(vb), window, sinks, None, _np(db))
+        clean = O.attention(_np(q), _np(k), _np(v), window, sinks, None, _np(do))
+        lim = bounds(_np(q), _np(k), _np(v), clean, window, sinks, D ** -0.5, dtype, _np(do))
+        for name in ("o", "dq", "dk", "dv"):
+            have, want = _np(got[name]), r[name]
+            fine = np.isfinite(want)
+            assert not fine.all()
+            some = window is not None or name != "dk"  # without a window scores that are not finite reach every key
+            assert fine.any() == some, name
+            assert np.array_equal(np.isfinite(have), fine), (name, window, int((np.isfinite(have) != fine).sum()))
+            # where a finite result has the same inputs as without them, the same bounds; else it is checked as finite
+            with np.errstate(invalid="ignore"):
+                same = fine & (np.abs(want - clean[name]) <= 1e-12 * np.abs(clean[name]))
+            assert same.any() == some and np.all(np.abs(have[same] - want[same]) <= lim[name][same]), (name, window)
+
+
+@pytest.mark.parametrize("nq", [1, 40])
+def test_rows_behind_a_caches_end_are_not_read(nq):
+    """Room of a cache that is not used yet holds NaN."""
+    train = _train()
+    rng = np.random.default_rng(22)
+    room, n = 200, [150, 40, 64]
+    q = _normal(rng, 3 * nq, 4, 64, dtype="bf16")
+    k, v = (_normal(rng, 3 * room, 2, 64, dtype="bf16") for _ in range(2))
+    lengths = torch.tensor(n, dtype=torch.int32).cuda()
+    want = train.attention(q, k, v, _offsets([nq] * 3), _offsets([room] * 3), lengths, window=30, sinks=2)
+    for i, m in enumerate(n):
+        k[i * room + m:(i + 1) * room] = float("nan")
+        v[i * room + m:(i + 1) * room] = float("nan")
+    got = train.attention(q, k, v, _offsets([nq] * 3), _offsets([room] * 3), lengths, window=30, sinks=2)
+    assert torch.isfinite(got).all() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("nq", [1, 50])
+def test_strided_and_misaligned_rows(nq):
+    """Rows inside wider ones as they lie; other strides and alignments by a copy; the same results to the bit."""
+    train = _train()
+    rng = np.random.default_rng(23)
+    n = 60
+    wide = _normal(rng, n, 1000, dtype="bf16")
+    q, k, v = (wide[:, a:a + 256].view(n, 4, 64) for a in (0, 256, 512))
+    q = q[:2 * nq] if nq == 1 else q
+    args = (_offsets([1, 1]), _offsets([20, 40])) if nq == 1 else (_offsets([20, 40]),)
+    plain = [t.contiguous().requires_grad_() for t in (q, k, v)]
+    want = train.attention(*plain, *args, window=17)
+    do = _normal(rng, *want.shape, dtype="bf16")
+    grads = torch.autograd.grad(want, plain, do)
+    odd = torch.empty(n * 256 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(n, 4, 64)
+    odd.copy_(k)
+    ways = [(q, k, v), (q, odd, v), (q.transpose(0, 1).contiguous().transpose(0, 1), k, wide[:, 512:768].view(n, 4, 64))]
+    for w in ways:
+        leaves = [t.detach().requires_grad_() for t in w]
+        got = train.attention(*leaves, *args, window=17)
+        assert torch.equal(got, want)
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(got, leaves, do), grads))
+    one = k[:, :1].expand(n, 4, 64)  # one head for all, a stride of zero
+    a = train.attention(q, one, one, *args)
+    b = train.attention(q, k[:, :1], k[:, :1], *args)
+    assert torch.equal(a, b)
+
+
+def test_self_attention_of_rows_inside_wider_ones():
+    train = _train()
+    rng = np.random.default_rng(24)
+    wide = _normal(rng, 70, 800, dtype="bf16")
+    qkv = wide[:, 8:8 + 6 * 64]
+    a = qkv.detach().requires_grad_()
+    b = qkv.detach().clone().requires_grad_()
+    oa, ob = (train.self_attention(t, _offsets([30, 40]), 4, 1) for t in (a, b))
+    assert torch.equal(oa, ob)
+    assert torch.equal(torch.autograd.grad(oa.sum(), a)[0], torch.autograd.grad(ob.sum(), b)[0])
+
+
+def test_gradients_by_differences():
+    train = _train()
+    rng = np.random.default_rng(25)
+    n = [9, 0, 21]
+    q, k, v = (_normal(rng, 30, h, 16) for h in (4, 2, 2))
+    leaves = [t.requires_grad_() for t in (q, k, v)]
+    o = train.attention(*leaves, _offsets(n), window=6, sinks=2)
+    c = _normal(rng, *o.shape)
+    got = torch.autograd.grad(o, leaves, c)
+    vals = [_np(t) for t in leaves]
+    for i, g in enumerate(got):
+        step = rng.standard_normal(vals[i].shape)
+        f = []
+        for s in (1e-5, -1e-5):
+            t = [x + (s * step if j == i else 0) for j, x in enumerate(vals)]
+            f.append(sum((O.attention(*(x[a:b] for x in t), 6, 2)["o"] * _np(c)[a:b]).sum() for a, b in ((0, 9), (9, 30))))
+        slope, have = (f[0] - f[1]) / 2e-5, (_np(g) * step).sum()
+        assert abs(slope - have) <= 300 * E32 * np.abs(_np(g) * step).sum() + 1e-5, (i, slope, have)
+
+
+def test_same_from_call_to_call_and_on_other_streams():
+    train = _train()
+    rng = np.random.default_rng(26)
+    qkv = _normal(rng, 3000, 3 * 512, dtype="bf16").requires_grad_()
+    do = _normal(rng, 3000, 512, dtype="bf16")
+
+    def run():
+        o = train.self_attention(qkv, off, 8, window=100, sinks=4)
+        return o, torch.autograd.grad(o, qkv, do)[0]
+
+    off = _offsets([1200, 1, 1700])
+    want = run()
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(2):
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            outs.append(run())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for got in outs for a, b in zip(got, want))
+
+
+def test_no_rows_and_no_sequences():
+    train = _train()
+    e = torch.zeros(0, 4, 64, device="cuda", requires_grad=True)
+    o = train.attention(e, e, e, _offsets([]))
+    assert o.shape == (0, 4, 64)
+    assert torch.autograd.grad(o.sum(), e)[0].shape == (0, 4, 64)
+    t = torch.ones(5, 4, 64, device="cuda", requires_grad=True)
+    o = train.attention(t, t, t, _offsets([]))  # rows of no sequence
+    assert not o.any() and not torch.autograd.grad(o.sum(), t)[0].any()
+    k = torch.ones(3, 4, 64, device="cuda", requires_grad=True)
+    o = train.attention(e, k, k, _offsets([0]), _offsets([3]))
+    assert o.shape == (0, 4, 64) and not torch.autograd.grad(o.sum(), k)[0].any()
+    o = train.attention(t, e, e, _offsets([5]), _offsets([0]))
+    assert not o.any() and not torch.autograd.grad(o.sum(), t)[0].any()
+
+
+def test_gradients_of_gradients_are_refused():
+    train = _train()
+    t = torch.ones(5, 4, 64, device="cuda", requires_grad=True)
+    g, = torch.autograd.grad(train.attention(t, t, t, _offsets([5])).sum(), t, create_graph=True)
+    with pytest.raises(RuntimeError, match="gradients of gradients"):
+        torch.autograd.grad(g.sum(), t)

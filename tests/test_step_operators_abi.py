@@ -134,3 +134,144 @@ def _off(*v):
 def test_attention_argument_errors(call):
     with pytest.raises(ValueError, match="attention"):
         call()
+
+
+def _resid(lib, **kw):
+    a = dict(x=P, y=P, yt=BF16, alpha=P, gamma=P, group=P, groups=2, rows=3, d=8, post=0, eps=1e-5, h=P, z=P, rstd=P, ystd=P)
+    a.update(kw)
+    return lib.tlf_residual_norm(*(a[k] for k in ("x", "y", "yt", "alpha", "gamma", "group", "groups", "rows", "d", "post",
+                                                  "eps", "h", "z", "rstd", "ystd")), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(x=None), BAD), (dict(y=None), BAD), (dict(h=None), BAD), (dict(z=None), BAD), (dict(x=ODD), BAD), (dict(y=ODD), BAD),
+    (dict(h=ODD), BAD), (dict(z=ODD), BAD), (dict(alpha=ODD), BAD), (dict(gamma=ODD), BAD), (dict(yt=2), BAD),
+    (dict(rows=-1), BAD), (dict(d=0), BAD), (dict(d=6), BAD), (dict(eps=0.0), BAD), (dict(eps=math.nan), BAD),
+    (dict(groups=-1), BAD), (dict(groups=0), BAD), (dict(alpha=None, gamma=None), BAD), (dict(group=None), BAD),
+    (dict(group=0x1002), BAD), (dict(rstd=0x1002), BAD), (dict(ystd=0x1001), BAD), (dict(d=4100), UNS),
+    (dict(groups=17), UNS), (dict(rows=(1 << 30) + 1), UNS),
+])
+def test_residual_norm_refusals(lib, kw, status):
+    assert _resid(lib, **kw) == status
+
+
+def test_residual_norm_without_rows_needs_no_device(lib):
+    assert _resid(lib, rows=0, x=None, y=None, h=None, z=None) == tlf.OK
+
+
+def _resid_grad(lib, **kw):
+    a = dict(dh=P, dz=P, h=P, y=P, yt=F32, alpha=P, gamma=P, group=P, groups=2, rstd=P, ystd=P, rows=3, d=8, post=1, dx=P, dy=P,
+             dalpha=P, dgamma=P, ws=P, n=1 << 20)
+    a.update(kw)
+    return lib.tlf_residual_norm_grad(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(h=None), BAD), (dict(y=None), BAD), (dict(rstd=None), BAD), (dict(ystd=None), BAD), (dict(dx=None), BAD),
+    (dict(dy=None), BAD), (dict(group=None), BAD), (dict(ws=None), BAD), (dict(n=127), BAD), (dict(dalpha=None), BAD),
+    (dict(dgamma=None), BAD), (dict(alpha=None), BAD), (dict(gamma=None), BAD), (dict(groups=0, alpha=None, gamma=None), BAD),
+    *[({k: ODD}, BAD) for k in ("dh", "dz", "h", "y", "alpha", "gamma", "dx", "dy", "dalpha", "dgamma", "ws")],
+    (dict(d=10), BAD), (dict(yt=9), BAD), (dict(rows=-2), BAD), (dict(d=8192), UNS), (dict(groups=33), UNS),
+])
+def test_residual_norm_grad_refusals(lib, kw, status):
+    assert _resid_grad(lib, **kw) == status
+
+
+def _grads(*t):
+    return (tlf.Grad * max(1, len(t)))(*(tlf.Grad(*v, 0) for v in t))
+
+
+@pytest.mark.parametrize("t,status", [
+    ((None, 5, F32), BAD), ((P, -1, F32), BAD), ((P, 5, 2), BAD), ((0x1002, 5, F32), BAD), ((0x1001, 5, BF16), BAD),
+    ((P, (1 << 35) + 1, F32), UNS),
+])
+def test_grad_norm_refusals(lib, t, status):
+    need, g = ctypes.c_size_t(), _grads((P, 10, F32), t)
+    assert lib.tlf_grad_norm_ws_bytes(g, 2, need) == status
+    assert lib.tlf_grad_norm(g, 2, 1.0, P, P, P, BIG, None) == status
+    assert lib.tlf_grad_clip(g, 2, 0x4000, None) == status
+
+
+def test_grad_norm_other_refusals(lib):
+    g, need = _grads((P, 10, F32), (None, 0, BF16)), ctypes.c_size_t()
+    assert lib.tlf_grad_norm_ws_bytes(g, 2, need) == tlf.OK and need.value == 8
+    for bad in (0.0, -1.0, math.nan):
+        assert lib.tlf_grad_norm(g, 2, bad, P, P, P, 8, None) == BAD
+    for norm, scale, ws, n in ((None, P, P, 8), (0x1002, P, P, 8), (P, 0x1002, P, 8), (P, P, None, 8), (P, P, 0x1004, 8), (P, P, P, 7)):
+        assert lib.tlf_grad_norm(g, 2, 1.0, norm, scale, ws, n, None) == BAD
+    assert lib.tlf_grad_norm(None, 2, 1.0, P, P, P, 8, None) == BAD and lib.tlf_grad_norm(g, -1, 1.0, P, P, P, 8, None) == BAD
+    assert lib.tlf_grad_clip(g, 2, None, None) == BAD and lib.tlf_grad_clip(g, 2, 0x4002, None) == BAD
+
+
+@pytest.mark.parametrize("b,scale", [((P, 10, F32), 0x4000), ((P + 36, 10, F32), 0x4000), ((P + 38, 1, BF16), 0x4000),
+                                     ((P + 64, 10, F32), P + 36), ((P + 64, 10, F32), P + 64)])
+def test_grad_clip_refuses_overlaps(lib, b, scale):
+    assert lib.tlf_grad_clip(_grads((P, 10, F32), b), 2, scale, None) == BAD
+
+
+def _adamw(scale, **kw):
+    a = dict(d_param=0x10000, d_copy=None, d_grad=0x20000, d_m=0x30000, d_v=0x40000, n=64, step=1, weight_decay=0.0,
+             grad_dtype=F32, state_bits=32)
+    a.update(kw)
+    t = (tlf.AdamwTensor * 1)()
+    for k, v in a.items():
+        setattr(t[0], k, v)
+    return tlf.load().tlf_adamw_scaled(t, 1, 1e-3, 0.9, 0.95, 1e-8, scale, None)
+
+
+@pytest.mark.parametrize("scale", [None, 0x1002, 0x10000, 0x100fc, 0x30010, 0x40000])
+def test_scaled_adamw_refusals(scale):
+    assert _adamw(scale) == BAD
+
+
+def test_scaled_adamw_refuses_what_adamw_does():
+    assert _adamw(0x1000, step=0) == BAD and _adamw(0x1000, n=(1 << 35) + 1) == UNS and _adamw(0x1000, d_m=0x10000) == BAD
+
+
+def test_grad_struct_layout(tmp_path):
+    src = 'printf("%zu ", sizeof(tlf_grad));' + "".join(f'printf("%zu ", offsetof(tlf_grad, {f}));' for f, _ in tlf.Grad._fields_)
+    (tmp_path / "t.c").write_text('#include <stdio.h>\n#include <stddef.h>\n#include "tlf.h"\nint main(void){' + src + "return 0;}")
+    subprocess.check_call(["gcc", "-std=c99", "-I", INC, str(tmp_path / "t.c"), "-o", str(tmp_path / "t")])
+    got = [int(v) for v in subprocess.check_output([str(tmp_path / "t")]).split()]
+    assert got == [ctypes.sizeof(tlf.Grad)] + [getattr(tlf.Grad, f).offset for f, _ in tlf.Grad._fields_]
+
+
+F = torch.float32
+
+
+@pytest.mark.parametrize("call", [
+    lambda: train.residual_norm(torch.zeros(3, 8), torch.zeros(3, 8)),
+    lambda: train.residual_norm(_t(3, 8), _t(3, 8)),
+    lambda: train.residual_norm(_t(3, 2, 4, dtype=F), _t(3, 2, 4)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 4)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8, dtype=torch.float16)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), alpha=_t(8)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), alpha=_t(4, dtype=F)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), alpha=_t(2, 8, dtype=F)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), alpha=_t(0, 8, dtype=F), group=_t(3, dtype=torch.int32)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), alpha=_t(2, 8, dtype=F), gamma=_t(3, 8, dtype=F),
+                                group=_t(3, dtype=torch.int32)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), group=_t(3, dtype=torch.int32)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), gamma=_t(2, 8, dtype=F), group=_t(3, dtype=torch.int64)),
+    lambda: train.residual_norm(_t(3, 8, dtype=F), _t(3, 8), gamma=_t(2, 8, dtype=F), group=_t(2, dtype=torch.int32)),
+])
+def test_residual_norm_argument_errors(call):
+    with pytest.raises(ValueError, match="residual_norm"):
+        call()
+
+
+@pytest.mark.parametrize("fn,args", [(train.grad_norm, ()), (train.clip_grad_norm_, (1.0,))])
+@pytest.mark.parametrize("grads", [[], [torch.zeros(4)], [_t(4, dtype=torch.float16)], [_t(4, 4).T]])
+def test_grad_norm_argument_errors(fn, args, grads):
+    with pytest.raises(ValueError, match=fn.__name__):
+        fn(grads, *args)
+
+
+def test_limits_that_are_none():
+    for bad in (0.0, -1.0, math.nan):
+        with pytest.raises(ValueError, match="max_norm"):
+            train.grad_norm([_t(4)], bad)
+    with pytest.raises(ValueError, match="max_norm"):
+        train.clip_grad_norm_([_t(4)], None)
+    with pytest.raises(ValueError, match="grad_scale"):
+        train.adamw_([_t(4, dtype=F)], [_t(4)], [_t(4, dtype=F)], [_t(4, dtype=F)], 1, 1e-3, grad_scale=_t(2, dtype=F))
