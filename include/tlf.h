@@ -538,7 +538,7 @@ int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, doubl
 #define TLF_ATTN_MAX_ROWS (1 << 29)
 #define TLF_ATTN_MAX_UNITS (1 << 29)     /* rows times heads */
 #define TLF_ATTN_MAX_SEQ_HEADS (1 << 22) /* sequences times heads */
-#define TLF_ATTN_MAX_STRIDE (1 << 22)
+#define TLF_ATTN_MAX_STRIDE (1 << 21)
 typedef struct tlf_attn_shape {
   int32_t dtype;     /* of q, k, v, o and their gradients: TLF_DTYPE_F32 or TLF_DTYPE_BF16 */
   int32_t batch;     /* sequences */

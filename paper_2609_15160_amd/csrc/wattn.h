@@ -36,6 +36,11 @@ struct WSeq {
   int q0, nq, k0, n, cap;  // first rows, queries, keys, rows that the keys have room in
 };
 
+// Waves per SIMD that the registers of the kernels leave room for.  Up to 256
+// registers a wave's products take their accumulators as they take other values;
+// with more, scores are copied from and to registers that only products reach.
+template <typename T, int D> constexpr int kRoom = sizeof(T) == 4 && D == 128 ? 1 : 2;
+
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 // Tiles of STEP rows: sequence b's begin at slot off[b] / STEP + b, which leaves
@@ -74,9 +79,23 @@ __device__ __forceinline__ WSeq load_seq(const WAttnArgs& a, int b) {
   return s;
 }
 
-// Whether the key u positions before the query (u < 0: behind it) at position x is visible.
-__device__ __forceinline__ bool sees(int u, int x, int window, int sinks) {
-  return (unsigned)u < (unsigned)window || (u >= 0 && x < sinks);
+// What a tile's scores are masked by.  Each comparison is with a constant of the
+// unrolled code and is used up by one select: differences and combined masks would
+// take more instructions than the products, and more scalar registers than there are.
+enum Mask {
+  M_NONE = 0,   // every pair is visible
+  M_UPPER = 1,  // keys behind the query are not
+  M_LOWER = 2,  // keys before the window are not
+  M_ALL = 3     // both (M_UPPER | M_LOWER), and sinks
+};
+__device__ __forceinline__ int reach(int x, int window, int sinks) { return x < sinks ? INT32_MAX : window; }
+__device__ __forceinline__ bool sees(int p, int x, int far) { return (unsigned)(p - x) < (unsigned)far; }
+
+// The mask of queries at positions [p0, p1] and keys [k0, k1], or -1: nothing is visible.
+__device__ __forceinline__ int mask_of(int p0, int p1, int k0, int k1, int window, int sinks) {
+  if (k0 > p1 || (p0 - k1 >= window && k0 >= sinks)) return -1;
+  const bool low = p1 - k0 >= window && k1 >= sinks, up = k1 > p0;
+  return !low ? (up ? M_UPPER : M_NONE) : up || k0 < sinks ? M_ALL : M_LOWER;
 }
 
 // Operands of 16 bytes per lane: bf16, eight values of one MFMA over 32; float32,
@@ -123,46 +142,46 @@ template <typename T, int D> struct HeadRows {
     const int x = (r / PER) & (KEYS - 1);
     return (x & (KEYS / 2 - 1)) << 1 | x / (KEYS / 2);
   }
-  // this lane's byte offsets: of row i's chunk of step ks, of the transposed reads of dimension tile dt
-  static __device__ __forceinline__ void direct(int lane, int (&at)[KSTEPS]) {
+  // This lane's byte offsets in a tile at a multiple of RB * 16: of row i's chunk of step
+  // 0, and of the transposed reads of dimension tile 0.  The others differ by the bits
+  // that the key is added to, so they need no register.
+  static __device__ __forceinline__ unsigned direct(int lane) {
     const int i = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) at[ks] = i * RB + (((ks * 4 + g) ^ key(i)) << 4);
+    return i * RB + ((g ^ key(i)) << 4);
   }
-  static __device__ __forceinline__ frag load(const char* tile, int row, int at) {  // row: a multiple of 16
-    return *reinterpret_cast<const frag*>(tile + row * RB + at);
-  }
-  static constexpr int TR = sizeof(T) == 2 ? DT : DT * 4;  // offsets of the transposed reads
-  static __device__ __forceinline__ void transposed(int lane, int (&at)[TR]) {
+  static __device__ __forceinline__ unsigned transposed(int lane) {
     const int i = lane & 15, g = lane >> 4;
     if constexpr (sizeof(T) == 2) {
       const int r = 4 * g + (i >> 2);  // a group of 16 lanes reads 4 rows x 16 dimensions, lane i gets dimension i
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) at[dt] = r * RB + (((2 * dt + ((i >> 1) & 1)) ^ key(r)) << 4) + (i & 1) * 8;
+      return r * RB + ((((i >> 1) & 1) ^ key(r)) << 4) + (i & 1) * 8;
     } else {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int r = 4 * g + j;
-          at[dt * 4 + j] = r * RB + (((4 * dt + (i >> 2)) ^ key(r)) << 4) + (i & 3) * 4;
-        }
+      return 4 * g * RB + (((i >> 2) ^ key(4 * g)) << 4) + (i & 3) * 4;
     }
   }
-  // dimension tile dt of the rows [row, row + ROWS), row a multiple of 16
-  static __device__ __forceinline__ frag load_t(const char* tile, int row, const int (&at)[TR], int dt) {
-    const char* p = tile + row * RB;
+  // step ks of the 16 rows at LDS address `tile`, with direct()
+  static __device__ __forceinline__ frag load(unsigned tile, unsigned at, int ks) {
+    return *(const __attribute__((address_space(3))) frag*)((tile + at) ^ (ks << 6));
+  }
+  // dimension tile dt of the ROWS rows at LDS address `tile`, with transposed()
+  static __device__ __forceinline__ frag load_t(unsigned tile, unsigned at, int dt) {
     if constexpr (sizeof(T) == 2) {
+      const unsigned p = (tile + at) ^ (dt << 5);
       union { s16x4 h[2]; frag v; } u;
-      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + at[dt]));
-      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * RB + at[dt]));
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * RB));
       return u.v;
     } else {
-      frag v;
+      frag v;  // rows 4 g + j: their keys differ from that of 4 g
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(p + at[dt * 4 + j]);
+      for (int j = 0; j < 4; ++j)
+        v[j] = *(const __attribute__((address_space(3))) float*)(((tile + at) ^ ((dt << 6) ^ (key_step(j) << 4))) + j * RB);
       return v;
     }
+  }
+  // key(4 g + j) ^ key(4 g), which is the same for every g
+  static constexpr int key_step(int j) {
+    const int x = (j / PER) & (KEYS - 1);
+    return (x & (KEYS / 2 - 1)) << 1 | x / (KEYS / 2);
   }
 };
 
@@ -173,28 +192,42 @@ template <typename T, int D, int ROWS, int NTH> struct PairLoader {
   static constexpr int HALF = ROWS * H::CPR;       // chunks of a tile
   static constexpr int N = 2 * HALF / NTH;         // chunks of a thread
   static constexpr int BYTES = 2 * ROWS * H::RB;   // A, then B
-  static_assert(2 * HALF % NTH == 0 && HALF % kWave == 0, "chunks");
-  int row[N], chunk[N];  // row of the tile, byte of the chunk
+  static_assert(2 * HALF % NTH == 0 && HALF % kWave == 0 && (N == 1 || HALF % NTH == 0), "chunks");
+  static constexpr int STEP = NTH / H::CPR;                   // rows from one chunk of a thread to its next
+  static constexpr int KINDS = STEP % 16 == 0 ? 1 : 16 / STEP;  // keys repeat after 16 rows
+  static_assert(NTH % H::CPR == 0 && (N == 1 || ROWS % STEP == 0) && (STEP % 16 == 0 || 16 % STEP == 0), "rows of a thread");
+  int row0, chunk[KINDS];  // first row, byte of the chunk
   int wbase;
   __device__ __forceinline__ void init() {
     wbase = __builtin_amdgcn_readfirstlane(threadIdx.x & ~(kWave - 1));
+    row0 = threadIdx.x / H::CPR;
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-      const int q = (threadIdx.x + c * NTH) % HALF;
-      row[c] = q / H::CPR;
-      chunk[c] = ((q % H::CPR) ^ H::key(row[c])) << 4;
-    }
+    for (int c = 0; c < KINDS; ++c) chunk[c] = ((threadIdx.x % H::CPR) ^ H::key(row0 + c * STEP)) << 4;
   }
-  // a, b: this head's elements of the tile's first row; as, bs: bytes between rows; last: the last row, from the first
+  // a, b: this head's elements of the tile's first row; as, bs: bytes between rows (< 2^24); last: the last row, from the first
   __device__ __forceinline__ void issue(const void* a, const void* b, int as, int bs, int last, unsigned lds) const {
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-      const bool second = wbase + c * NTH >= HALF;
-      const int r = min(row[c], last);
-      stage16(second ? b : a, (unsigned)(r * (second ? bs : as) + chunk[c]), lds + (wbase + c * NTH) * 16);
+      // with fewer chunks than threads a thread's only one may be of either tile
+      const bool second = N == 1 ? wbase >= HALF : c * NTH >= HALF;
+      const int r = min((N == 1 && second ? row0 - ROWS : row0) + c * STEP % ROWS, last);
+      stage16(second ? b : a, __umul24(r, second ? bs : as) + chunk[c % KINDS], lds + (wbase + c * NTH) * 16);
     }
   }
 };
+
+// A loaded value waited for here.  Else the compiler waits where it is used first, in
+// the loop over tiles, and with counts that do not know of the staged loads: each tile
+// would wait for the next one's.
+template <typename F> __device__ __forceinline__ void settle(F& f) {
+  if constexpr (sizeof(F) == 16) {
+    u32x4 t = __builtin_bit_cast(u32x4, f);
+    asm volatile("" : "+v"(t));
+    f = __builtin_bit_cast(F, t);
+  } else {
+    asm volatile("" : "+v"(f));
+  }
+}
 
 __device__ __forceinline__ float sum_quads(float v) {  // over lanes l, l ^ 16, l ^ 32, l ^ 48
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);

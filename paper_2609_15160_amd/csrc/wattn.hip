@@ -64,15 +64,15 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // the sums are rescaled.  o / l does not depend on the base, and weights below
 // kSumMax are far inside float32's and bf16's range.
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
+__global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
-  constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32, NT = BN / 16;
-  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, PV = BN / H::ROWS;
+  constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NT = O::TILES;
   constexpr float kSumMax = 65536.f;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
-  __shared__ __align__(16) char lds[2 * Loader::BYTES];
+  __shared__ __align__(1024) char lds[2 * Loader::BYTES];
 
   const int u = xcd_run(blockIdx.x, gridDim.x), h = u / a.slots, slot = u - h * a.slots;
   const int b = seq_of<BM>(a.q_off, a.rows_q, a.batch, slot);
@@ -97,9 +97,11 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) qf[qn][ks] = *reinterpret_cast<const Frag*>(src + ks * 4 * H::EPC);
   }
-  int at[KSTEPS], att[H::TR];
-  H::direct(lane, at);
-  H::transposed(lane, att);
+#pragma unroll
+  for (int qn = 0; qn < QN; ++qn)
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) settle(qf[qn][ks]);
+  const unsigned at = H::direct(lane), att = H::transposed(lane);
 
   f32x4 o[DT][QN];
   float m[QN], l[QN];
@@ -112,10 +114,8 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
   }
   bool started = false;
 
-  auto use = [&](int kt, const char* kb) __attribute__((always_inline)) {
-    const int k0 = kt * BN, k1 = k0 + BN - 1;
-    if (!mine || k0 > pw1 || (pw0 - k1 >= a.window && k0 >= a.sinks)) return;
-    const bool edge = k1 > pw0 || (pw1 - k0 >= a.window && k1 >= a.sinks);
+  // one operand's rows of keys, from k0 on, at kb and their values at vb
+  auto products = [&](int mask, int k0, unsigned kb, unsigned vb) __attribute__((always_inline)) {
     f32x4 sc[QN][NT];
     auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -124,21 +124,38 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
         for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-          const Frag kf = H::load(kb, nt * 16, at[ks]);
+          const Frag kf = H::load(kb + nt * 16 * H::RB, at, ks);
 #pragma unroll
           for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = O::mma(kf, qf[qn][ks], sc[qn][nt]);
         }
       }
-      if (edge) {
+      if (mask == M_UPPER) {
 #pragma unroll
-        for (int qn = 0; qn < QN; ++qn)
+        for (int qn = 0; qn < QN; ++qn) {
+          const int last = p[qn] - k0 - 4 * g;
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int x = k0 + nt * 16 + 4 * g + r;
-              if (!sees(p[qn] - x, x, a.window, a.sinks)) sc[qn][nt][r] = -INFINITY;
-            }
+            for (int r = 0; r < 4; ++r) sc[qn][nt][r] = last >= nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
+        }
+      } else if (mask == M_LOWER) {
+#pragma unroll
+        for (int qn = 0; qn < QN; ++qn) {
+          const int before = p[qn] - k0 - 4 * g - a.window;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sc[qn][nt][r] = before < nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
+        }
+      } else if (mask == M_ALL) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int x = k0 + nt * 16 + 4 * g + r, far = reach(x, a.window, a.sinks);
+#pragma unroll
+            for (int qn = 0; qn < QN; ++qn) sc[qn][nt][r] = sees(p[qn], x, far) ? sc[qn][nt][r] : -INFINITY;
+          }
       }
     };
     scores();
@@ -190,18 +207,14 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
     }
 #pragma unroll
     for (int qn = 0; qn < QN; ++qn) l[qn] += sum[qn];
-    const char* vb = kb + BN * H::RB;
+    Frag pf[QN];
 #pragma unroll
-    for (int t = 0; t < PV; ++t) {
-      Frag pf[QN];
+    for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(sc[qn]);
 #pragma unroll
-      for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(&sc[qn][t * O::TILES]);
+    for (int dt = 0; dt < DT; ++dt) {
+      const Frag vf = H::load_t(vb, att, dt);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const Frag vf = H::load_t(vb, t * H::ROWS, att, dt);
-#pragma unroll
-        for (int qn = 0; qn < QN; ++qn) o[dt][qn] = O::mma(vf, pf[qn], o[dt][qn]);
-      }
+      for (int qn = 0; qn < QN; ++qn) o[dt][qn] = O::mma(vf, pf[qn], o[dt][qn]);
     }
   };
 
@@ -213,6 +226,7 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
     const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
     const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
     const unsigned base = lds_offset(lds);
+    const int clear0 = max(pw1, 0) - a.window + 1;  // keys from here on are in the window of all of the wave's queries
     auto issue = [&](int i) __attribute__((always_inline)) {
       const int row = (i < sinks ? i : first + i - sinks) * BN;
       ld.issue(k + row * a.ks, v + row * a.vs, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), s.n - 1 - row,
@@ -222,7 +236,15 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn(WAttnArgs a) {
     for (int i = 0; i < count; ++i) {
       wait_barrier<0>();
       if (i + 1 < count) issue(i + 1);
-      use(i < sinks ? i : first + i - sinks, lds + (i & 1) * Loader::BYTES);
+      if (!mine) continue;
+      const unsigned kb = base + (i & 1) * Loader::BYTES;
+      const int k0 = (i < sinks ? i : first + i - sinks) * BN;
+#pragma unroll 1
+      for (int t = 0; t < BN; t += H::ROWS) {
+        const bool whole = k0 + t >= clear0 && k0 + t + H::ROWS - 1 <= pw0;
+        const int mask = whole ? M_NONE : mask_of(pw0, pw1, k0 + t, k0 + t + H::ROWS - 1, a.window, a.sinks);
+        if (mask >= 0) products(mask, k0 + t, kb + t * H::RB, kb + (BN + t) * H::RB);
+      }
     }
   }
   if (!mine) return;
@@ -265,13 +287,13 @@ template <typename T, int D> struct FewPart {  // sums of one head over a range
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kFewWaves* kWave) void k_wattn_few(WAttnArgs a) {
+__global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(WAttnArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, VN = kFewKeys * H::CPR / kWave, NT = kFewKeys / 16;
   constexpr int SUMS = kFewWaves * 16 * (D + 2) * 4, ROWS = kFewWaves * kFewKeys * H::RB;
-  __shared__ __align__(16) char lds[SUMS > ROWS ? SUMS : ROWS];
+  __shared__ __align__(1024) char lds[SUMS > ROWS ? SUMS : ROWS];
   const int each = a.heads / a.kv_heads, chunks = (each + 15) / 16;
   const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
   const int gc = unit % chunks, kvh = unit / chunks % a.kv_heads, row = unit / (chunks * a.kv_heads);
@@ -295,8 +317,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void k_wattn_few(WAttnArgs a) {
   const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)row * a.qs + (h0 + min(c16, cols - 1)) * D + g * H::EPC;
 #pragma unroll
   for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *reinterpret_cast<const Frag*>(q + ks * 4 * H::EPC);
-  int att[H::TR];
-  H::transposed(lane, att);
+  const unsigned att = H::transposed(lane);
   const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
   const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
   char* mine = lds + wave * kFewKeys * H::RB;
@@ -366,7 +387,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void k_wattn_few(WAttnArgs a) {
     for (int t = 0; t < NT / O::TILES; ++t) {
       const Frag pf = O::pack(&sc[t * O::TILES]);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = O::mma(H::load_t(mine, t * H::ROWS, att, dt), pf, o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = O::mma(H::load_t(lds_offset(mine) + t * H::ROWS * H::RB, att, dt), pf, o[dt]);
     }
     asm volatile("" ::: "memory");
   }

@@ -27,7 +27,7 @@ namespace {
 
 struct GradArgs : WAttnArgs {
   int64_t dqs, dks, dvs;
-  int sink_parts;  // ranges of the queries of a sequence's first key tile, where it has sinks
+  int sink_parts;  // ranges of the queries of a sequence's first key tile, where it has sinks, else 0
 };
 
 // One query's row again from its visible keys alone (slow_row of the forward pass says why).
@@ -81,14 +81,14 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
 // queries stay in registers; a tile's keys are read as they lie and transposed, its
 // values as they lie.  dP starts from -delta, so dS = P dP takes one product.
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
+__global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
   constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
-  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, PV = BN / H::ROWS, TL = O::TILES;
+  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
-  __shared__ __align__(16) char lds[2 * Loader::BYTES];
+  __shared__ __align__(1024) char lds[2 * Loader::BYTES];
 
   const int u = xcd_run(blockIdx.x, gridDim.x), h = u / a.slots, slot = u - h * a.slots;
   const int b = seq_of<BM>(a.q_off, a.rows_q, a.batch, slot);
@@ -126,64 +126,85 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
     lse[qn] = a.lse[(int64_t)h * a.rows_q + at];
     if (g == 0 && r0 + qn * 16 + c16 < s.nq) a.delta[(int64_t)h * a.rows_q + at] = delta[qn];
   }
-  int at[KSTEPS], att[H::TR];
-  H::direct(lane, at);
-  H::transposed(lane, att);
+#pragma unroll
+  for (int qn = 0; qn < QN; ++qn) {
+    settle(lse[qn]);
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+      settle(qf[qn][ks]);
+      settle(df[qn][ks]);
+    }
+  }
+  const unsigned at = H::direct(lane), att = H::transposed(lane);
   f32x4 dq[DT][QN];
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt][qn] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto use = [&](int kt, const char* kb) __attribute__((always_inline)) {
-    const int k0 = kt * BN, k1 = k0 + BN - 1;
-    if (!mine || k0 > pw1 || (pw0 - k1 >= a.window && k0 >= a.sinks)) return;
-    const bool edge = k1 > pw0 || (pw1 - k0 >= a.window && k1 >= a.sinks);
-    const char* vb = kb + BN * H::RB;
+  // one operand's rows of keys, from k0 on, at kb and their values at vb
+  auto products = [&](int mask, int k0, unsigned kb, unsigned vb) __attribute__((always_inline)) {
+    f32x4 sc[QN][TL], dp[QN][TL];
 #pragma unroll
-    for (int t = 0; t < PV; ++t) {
-      f32x4 sc[QN][TL], dp[QN][TL];
+    for (int n = 0; n < TL; ++n) {
 #pragma unroll
-      for (int n = 0; n < TL; ++n) {
-        const int row = t * H::ROWS + n * 16;
+      for (int qn = 0; qn < QN; ++qn) {
+        sc[qn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        dp[qn][n] = f32x4{-delta[qn], -delta[qn], -delta[qn], -delta[qn]};
+      }
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        const Frag kf = H::load(kb + n * 16 * H::RB, at, ks), vf = H::load(vb + n * 16 * H::RB, at, ks);
 #pragma unroll
         for (int qn = 0; qn < QN; ++qn) {
-          sc[qn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-          dp[qn][n] = f32x4{-delta[qn], -delta[qn], -delta[qn], -delta[qn]};
-        }
-#pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-          const Frag kf = H::load(kb, row, at[ks]), vf = H::load(vb, row, at[ks]);
-#pragma unroll
-          for (int qn = 0; qn < QN; ++qn) {
-            sc[qn][n] = O::mma(kf, qf[qn][ks], sc[qn][n]);
-            dp[qn][n] = O::mma(vf, df[qn][ks], dp[qn][n]);
-          }
-        }
-#pragma unroll
-        for (int qn = 0; qn < QN; ++qn)
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            dp[qn][n][r] *= __builtin_amdgcn_exp2f(fmaf(sc[qn][n][r], a.scale_log2, -lse[qn]));
-        if (edge) {
-#pragma unroll
-          for (int qn = 0; qn < QN; ++qn)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int x = k0 + row + 4 * g + r;
-              if (!sees(p[qn] - x, x, a.window, a.sinks)) dp[qn][n][r] = 0.f;
-            }
+          sc[qn][n] = O::mma(kf, qf[qn][ks], sc[qn][n]);
+          dp[qn][n] = O::mma(vf, df[qn][ks], dp[qn][n]);
         }
       }
-      Frag pf[QN];
+    }
+    // scores that are not visible are -inf: their weights and their dS are 0
+    if (mask == M_UPPER) {
 #pragma unroll
-      for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(dp[qn]);
+      for (int qn = 0; qn < QN; ++qn) {
+        const int last = p[qn] - k0 - 4 * g;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const Frag kf = H::load_t(kb, t * H::ROWS, att, dt);
+        for (int n = 0; n < TL; ++n)
 #pragma unroll
-        for (int qn = 0; qn < QN; ++qn) dq[dt][qn] = O::mma(kf, pf[qn], dq[dt][qn]);
+          for (int r = 0; r < 4; ++r) sc[qn][n][r] = last >= n * 16 + r ? sc[qn][n][r] : -INFINITY;
       }
+    } else if (mask == M_LOWER) {
+#pragma unroll
+      for (int qn = 0; qn < QN; ++qn) {
+        const int before = p[qn] - k0 - 4 * g - a.window;
+#pragma unroll
+        for (int n = 0; n < TL; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[qn][n][r] = before < n * 16 + r ? sc[qn][n][r] : -INFINITY;
+      }
+    } else if (mask == M_ALL) {
+#pragma unroll
+      for (int n = 0; n < TL; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = k0 + n * 16 + 4 * g + r, far = reach(x, a.window, a.sinks);
+#pragma unroll
+          for (int qn = 0; qn < QN; ++qn) sc[qn][n][r] = sees(p[qn], x, far) ? sc[qn][n][r] : -INFINITY;
+        }
+    }
+    Frag pf[QN];
+#pragma unroll
+    for (int qn = 0; qn < QN; ++qn) {
+#pragma unroll
+      for (int n = 0; n < TL; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) dp[qn][n][r] *= __builtin_amdgcn_exp2f(fmaf(sc[qn][n][r], a.scale_log2, -lse[qn]));
+      pf[qn] = O::pack(dp[qn]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const Frag kf = H::load_t(kb, att, dt);
+#pragma unroll
+      for (int qn = 0; qn < QN; ++qn) dq[dt][qn] = O::mma(kf, pf[qn], dq[dt][qn]);
     }
   };
 
@@ -195,6 +216,7 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
     const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
     const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
     const unsigned base = lds_offset(lds);
+    const int clear0 = max(pw1, 0) - a.window + 1;  // keys from here on are in the window of all of the wave's queries
     auto issue = [&](int i) __attribute__((always_inline)) {
       const int row = (i < sinks ? i : first + i - sinks) * BN;
       ld.issue(k + row * a.ks, v + row * a.vs, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), s.n - 1 - row,
@@ -204,7 +226,15 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
     for (int i = 0; i < count; ++i) {
       wait_barrier<0>();
       if (i + 1 < count) issue(i + 1);
-      use(i < sinks ? i : first + i - sinks, lds + (i & 1) * Loader::BYTES);
+      if (!mine) continue;
+      const unsigned kb = base + (i & 1) * Loader::BYTES;
+      const int k0 = (i < sinks ? i : first + i - sinks) * BN;
+#pragma unroll 1
+      for (int t = 0; t < BN; t += H::ROWS) {
+        const bool whole = k0 + t >= clear0 && k0 + t + H::ROWS - 1 <= pw0;
+        const int mask = whole ? M_NONE : mask_of(pw0, pw1, k0 + t, k0 + t + H::ROWS - 1, a.window, a.sinks);
+        if (mask >= 0) products(mask, k0 + t, kb + t * H::RB, kb + (BN + t) * H::RB);
+      }
     }
   }
   if (!mine) return;
@@ -240,17 +270,17 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dq(GradArgs a) {
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
 template <typename T, int D, int NW, int KN>
-__global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
+__global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
   constexpr int KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 ? 64 : 32;
-  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, STEPS = BQ / H::ROWS, TL = O::TILES;
+  constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BQ, NW * kWave>;
-  __shared__ __align__(16) char lds[2 * Loader::BYTES];
+  __shared__ __align__(1024) char lds[2 * Loader::BYTES];
   __shared__ __align__(16) float stats[2][2][kWave];  // of each place: lse, delta
 
-  const int sink_blocks = a.sink_parts > 1 ? a.batch * a.kv_heads * a.sink_parts : 0;
+  const int sink_blocks = a.batch * a.kv_heads * a.sink_parts;  // sink_parts = 0: first tiles are as others
   int b, kvh, tile, part = 0, parts = 1;
   WSeq s;
   if ((int)blockIdx.x < sink_blocks) {  // the longest first
@@ -275,9 +305,7 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
   const int w0 = k0 + wave * KW, w1 = min(w0 + KW, s.n) - 1;  // of the wave
 
   Frag kf[KN][KSTEPS], vf[KN][KSTEPS];
-  int at[KSTEPS], att[H::TR];
-  H::direct(lane, at);
-  H::transposed(lane, att);
+  const unsigned at = H::direct(lane), att = H::transposed(lane);
   f32x4 dk[DT][KN], dv[DT][KN];
 #pragma unroll
   for (int kn = 0; kn < KN; ++kn)
@@ -287,6 +315,85 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
   // queries [j0, j1] see a key of the tile
   const int last = k0 < a.sinks || a.window > s.n - 1 - k1 ? s.n - 1 : k1 + a.window - 1;
   const int j0 = max(0, k0 - off), j1 = last - off;
+  // one operand's rows of queries, from row j on, at qb and their do at db
+  auto products = [&](int mask, int j, unsigned qb, unsigned db, const float* stat) __attribute__((always_inline)) {
+    f32x4 sc[KN][TL], dp[KN][TL];
+    f32x4 lse[TL];
+#pragma unroll
+    for (int n = 0; n < TL; ++n) {
+      lse[n] = Vec4<float>::load(stat + n * 16 + 4 * g);
+      const f32x4 delta = Vec4<float>::load(stat + kWave + n * 16 + 4 * g);
+#pragma unroll
+      for (int kn = 0; kn < KN; ++kn) {
+        sc[kn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        dp[kn][n] = -delta;
+      }
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        const Frag qf = H::load(qb + n * 16 * H::RB, at, ks), df = H::load(db + n * 16 * H::RB, at, ks);
+#pragma unroll
+        for (int kn = 0; kn < KN; ++kn) {
+          sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
+          dp[kn][n] = O::mma(df, vf[kn][ks], dp[kn][n]);
+        }
+      }
+    }
+    // scores that are not visible are -inf: their weights and their dS are 0
+    if (mask == M_UPPER) {
+#pragma unroll
+      for (int kn = 0; kn < KN; ++kn) {
+        const int first = w0 + kn * 16 + c16 - off - j - 4 * g;
+#pragma unroll
+        for (int n = 0; n < TL; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[kn][n][r] = first <= n * 16 + r ? sc[kn][n][r] : -INFINITY;
+      }
+    } else if (mask == M_LOWER) {
+#pragma unroll
+      for (int kn = 0; kn < KN; ++kn) {
+        const int x = w0 + kn * 16 + c16, end = (a.window > s.n - 1 - x ? j1 : min(x + a.window - 1 - off, j1)) - j - 4 * g;
+#pragma unroll
+        for (int n = 0; n < TL; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[kn][n][r] = end >= n * 16 + r ? sc[kn][n][r] : -INFINITY;
+      }
+    } else if (mask == M_ALL) {
+#pragma unroll
+      for (int n = 0; n < TL; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          // a row behind the last query stands before every key
+          const int q = j + n * 16 + 4 * g + r, at_q = q > j1 ? INT32_MIN / 2 : q + off;
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn) {
+            const int x = w0 + kn * 16 + c16;
+            sc[kn][n][r] = sees(at_q, x, reach(x, a.window, a.sinks)) ? sc[kn][n][r] : -INFINITY;
+          }
+        }
+    }
+    Frag pf[KN], sf[KN];
+#pragma unroll
+    for (int kn = 0; kn < KN; ++kn) {
+#pragma unroll
+      for (int n = 0; n < TL; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sc[kn][n][r] = __builtin_amdgcn_exp2f(fmaf(sc[kn][n][r], a.scale_log2, -lse[n][r]));
+          dp[kn][n][r] *= sc[kn][n][r];
+        }
+      pf[kn] = O::pack(sc[kn]);
+      sf[kn] = O::pack(dp[kn]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const Frag df = H::load_t(db, att, dt), qf = H::load_t(qb, att, dt);
+#pragma unroll
+      for (int kn = 0; kn < KN; ++kn) {
+        dv[dt][kn] = O::mma(df, pf[kn], dv[dt][kn]);
+        dk[dt][kn] = O::mma(qf, sf[kn], dk[dt][kn]);
+      }
+    }
+  };
   if (k0 < s.n && j0 <= j1) {
 #pragma unroll
     for (int kn = 0; kn < KN; ++kn) {
@@ -299,6 +406,13 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
         vf[kn][ks] = *reinterpret_cast<const Frag*>(v + ks * 4 * H::EPC);
       }
     }
+#pragma unroll
+    for (int kn = 0; kn < KN; ++kn)
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        settle(kf[kn][ks]);
+        settle(vf[kn][ks]);
+      }
     Loader ld;
     ld.init();
     const int tiles = (j1 - j0 + BQ) / BQ, all = tiles * each;
@@ -326,66 +440,17 @@ __global__ __launch_bounds__(NW* kWave) void k_wattn_dkv(GradArgs a) {
       const int place = (i - begin) & 1;
       wait_barrier<0>();
       if (i + 1 < end) issue(place ^ 1);
-      const int j = j0 + ut * BQ, jl = min(j + BQ - 1, j1), pa = j + off, pb = jl + off;
+      const int j = j0 + ut * BQ;
       if (++ut == tiles) ut = 0;
-      if (w0 > w1 || pb < w0 || (pa - w1 >= a.window && w0 >= a.sinks)) continue;
-      const bool edge = pa < w1 || jl < j + BQ - 1 || (pb - w0 >= a.window && w1 >= a.sinks);
-      const char* qb = lds + place * Loader::BYTES;
-      const char* db = qb + BQ * H::RB;
-#pragma unroll
-      for (int t = 0; t < STEPS; ++t) {
-        f32x4 sc[KN][TL], dp[KN][TL];
-#pragma unroll
-        for (int n = 0; n < TL; ++n) {
-          const int row = t * H::ROWS + n * 16;
-          const f32x4 lse = Vec4<float>::load(&stats[place][0][row + 4 * g]);
-          const f32x4 delta = Vec4<float>::load(&stats[place][1][row + 4 * g]);
-#pragma unroll
-          for (int kn = 0; kn < KN; ++kn) {
-            sc[kn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-            dp[kn][n] = -delta;
-          }
-#pragma unroll
-          for (int ks = 0; ks < KSTEPS; ++ks) {
-            const Frag qf = H::load(qb, row, at[ks]), df = H::load(db, row, at[ks]);
-#pragma unroll
-            for (int kn = 0; kn < KN; ++kn) {
-              sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
-              dp[kn][n] = O::mma(df, vf[kn][ks], dp[kn][n]);
-            }
-          }
-#pragma unroll
-          for (int kn = 0; kn < KN; ++kn)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              sc[kn][n][r] = __builtin_amdgcn_exp2f(fmaf(sc[kn][n][r], a.scale_log2, -lse[r]));
-              dp[kn][n][r] *= sc[kn][n][r];
-            }
-          if (edge) {
-#pragma unroll
-            for (int kn = 0; kn < KN; ++kn)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int x = w0 + kn * 16 + c16, q = j + row + 4 * g + r;
-                if (q > j1 || !sees(q + off - x, x, a.window, a.sinks)) sc[kn][n][r] = dp[kn][n][r] = 0.f;
-              }
-          }
-        }
-        Frag pf[KN], sf[KN];
-#pragma unroll
-        for (int kn = 0; kn < KN; ++kn) {
-          pf[kn] = O::pack(sc[kn]);
-          sf[kn] = O::pack(dp[kn]);
-        }
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const Frag df = H::load_t(db, t * H::ROWS, att, dt), qf = H::load_t(qb, t * H::ROWS, att, dt);
-#pragma unroll
-          for (int kn = 0; kn < KN; ++kn) {
-            dv[dt][kn] = O::mma(df, pf[kn], dv[dt][kn]);
-            dk[dt][kn] = O::mma(qf, sf[kn], dk[dt][kn]);
-          }
-        }
+      if (w0 > w1) continue;
+      const unsigned qb = base + place * Loader::BYTES;
+#pragma unroll 1
+      for (int t = 0; t < BQ; t += H::ROWS) {
+        const int ja = j + t, jl = min(ja + H::ROWS - 1, j1);
+        if (ja > j1) break;
+        int mask = mask_of(ja + off, jl + off, w0, w1, a.window, a.sinks);
+        if (jl < ja + H::ROWS - 1 && mask >= 0) mask = (mask & M_UPPER) || w0 < a.sinks ? M_ALL : M_LOWER;  // rows behind j1
+        if (mask >= 0) products(mask, ja, qb + t * H::RB, qb + (BQ + t) * H::RB, &stats[place][0][t]);
       }
     }
   }
@@ -469,10 +534,11 @@ template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wa
 constexpr int kManyWaves = 4;
 template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }  // KN: registers
 
-// Ranges of a first tile's queries, each as long as four other tiles' at least.
+// Ranges of a first tile's queries, each as long as two other tiles' at least; 0: there
+// are no sinks.
 int sink_parts(const tlf_attn_shape& t) {
-  if (t.window <= 0 || t.sinks <= 0 || t.batch <= 0) return 1;
-  const int64_t rows = t.rows_q / t.batch, other = 4 * ((int64_t)t.window + 128);
+  if (t.window <= 0 || t.sinks <= 0 || t.batch <= 0) return 0;
+  const int64_t rows = t.rows_q / t.batch, other = 2 * ((int64_t)t.window + 128);
   return (int)std::max<int64_t>(1, std::min<int64_t>(16, rows / other));
 }
 
@@ -480,17 +546,17 @@ bool many_keys(const tlf_attn_shape& t) { return slots_of<128>(t.rows_k, t.batch
 
 int64_t delta_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }
 int64_t part_floats(const tlf_attn_shape& t) {
-  const int parts = many_keys(t) ? sink_parts(t) : 1;
+  const int parts = many_keys(t) ? sink_parts(t) : 0;
   return parts > 1 ? (int64_t)t.batch * t.kv_heads * parts * 128 * 2 * t.head_dim : 0;
 }
 
 template <typename T, int D, int NW> hipError_t launch_keys(const tlf_attn_shape& t, GradArgs a, hipStream_t s) {
   constexpr int KN = key_tiles<T, D>(), KT = NW * KN * 16;
   a.slots = (int)slots_of<KT>(t.rows_k, t.batch);
-  const int64_t sinks = a.sink_parts > 1 ? (int64_t)a.batch * a.kv_heads * a.sink_parts : 0;
+  const int64_t sinks = (int64_t)a.batch * a.kv_heads * a.sink_parts;
   hipLaunchKernelGGL((k_wattn_dkv<T, D, NW, KN>), dim3((unsigned)(sinks + (int64_t)a.slots * a.kv_heads)), dim3(NW * kWave), 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || sinks == 0) return e;
+  if (e != hipSuccess || a.sink_parts <= 1) return e;
   hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / 4))), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -508,7 +574,7 @@ template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, GradArgs
     if (e != hipSuccess) return e;
   }
   if (t.rows_k == 0) return hipSuccess;
-  a.sink_parts = many_keys(t) ? sink_parts(t) : 1;
+  a.sink_parts = many_keys(t) ? sink_parts(t) : 0;
   return many_keys(t) ? launch_keys<T, D, kManyWaves>(t, a, s) : launch_keys<T, D, 1>(t, a, s);
 }
 

@@ -128,7 +128,7 @@ class AdamwTensor(ctypes.Structure):
 
 
 ATTN_MAX_SINKS = 64
-ATTN_MAX_STRIDE = 1 << 22
+ATTN_MAX_STRIDE = 1 << 21
 
 
 class AttnShape(ctypes.Structure):

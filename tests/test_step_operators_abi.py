@@ -35,7 +35,7 @@ SHAPES = [
     (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=math.nan), BAD), (dict(scale=math.inf), BAD),
     (dict(q_stride=252), BAD), (dict(q_stride=248), BAD), (dict(k_stride=120), BAD), (dict(v_stride=-128), BAD),
     (dict(o_stride=0), BAD), (dict(d_q_offsets=None), BAD), (dict(d_k_offsets=None), BAD), (dict(head_dim=32), UNS),
-    (dict(head_dim=16), UNS), (dict(sinks=65), UNS), (dict(q_stride=(1 << 22) + 8), UNS), (dict(rows_q=1 << 30), UNS),
+    (dict(head_dim=16), UNS), (dict(sinks=65), UNS), (dict(q_stride=(1 << 21) + 8), UNS), (dict(rows_q=1 << 30), UNS),
     (dict(rows_k=1 << 30), UNS), (dict(rows_q=1 << 28), UNS), (dict(batch=1 << 21), UNS),
     (dict(heads=2048, kv_heads=2, q_stride=1 << 17, o_stride=1 << 17), UNS),
 ]
@@ -93,7 +93,7 @@ def test_struct_layouts_match_the_header(tmp_path):
     subprocess.check_call(["gcc", "-std=c99", "-I", INC, str(tmp_path / "t.c"), "-o", str(tmp_path / "t")])
     assert [int(v) for v in subprocess.check_output([str(tmp_path / "t")]).split()] == want
     text = open(os.path.join(INC, "tlf.h")).read()
-    assert f"TLF_ATTN_MAX_SINKS {tlf.ATTN_MAX_SINKS}\n" in text and tlf.ATTN_MAX_STRIDE == 1 << 22
+    assert f"TLF_ATTN_MAX_SINKS {tlf.ATTN_MAX_SINKS}\n" in text and tlf.ATTN_MAX_STRIDE == 1 << 21
 
 
 class _Cuda(torch.Tensor):
