@@ -22,7 +22,8 @@ namespace tlf {
 struct WAttnArgs {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
-  float *lse, *delta;               // [heads][rows_q]: log2 of the softmax sums, o . do
+  float* lse;                       // [heads][rows_q]: log2 of the softmax sums
+  float *nlse, *ndelta;             // [heads][rows_q]: -lse in units of q . k, -o . do
   float* part;
   const int32_t *q_off, *k_off, *k_len;
   int64_t qs, ks, vs, os;           // elements between rows; gradients lie as what they belong to
@@ -158,23 +159,25 @@ template <typename T, int D> struct HeadRows {
       return 4 * g * RB + (((i >> 2) ^ key(4 * g)) << 4) + (i & 3) * 4;
     }
   }
-  // step ks of the 16 rows at LDS address `tile`, with direct()
-  static __device__ __forceinline__ frag load(unsigned tile, unsigned at, int ks) {
-    return *(const __attribute__((address_space(3))) frag*)((tile + at) ^ (ks << 6));
+  // A tile's read addresses: its LDS address plus direct() or transposed() for step ks or
+  // dimension tile dt; rows that are multiples of 16 further on are an offset to it.
+  static __device__ __forceinline__ unsigned step(unsigned at, int ks) { return at ^ (ks << 6); }
+  static __device__ __forceinline__ unsigned tile(unsigned at, int dt) { return at ^ (dt << (sizeof(T) == 2 ? 5 : 6)); }
+  static __device__ __forceinline__ frag load(unsigned at, int row) {
+    return *(const __attribute__((address_space(3))) frag*)(at + row * RB);
   }
-  // dimension tile dt of the ROWS rows at LDS address `tile`, with transposed()
-  static __device__ __forceinline__ frag load_t(unsigned tile, unsigned at, int dt) {
+  // the ROWS rows from `row` on
+  static __device__ __forceinline__ frag load_t(unsigned at, int row) {
     if constexpr (sizeof(T) == 2) {
-      const unsigned p = (tile + at) ^ (dt << 5);
       union { s16x4 h[2]; frag v; } u;
-      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 16 * RB));
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + row * RB));
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + (row + 16) * RB));
       return u.v;
     } else {
       frag v;  // rows 4 g + j: their keys differ from that of 4 g
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        v[j] = *(const __attribute__((address_space(3))) float*)(((tile + at) ^ ((dt << 6) ^ (key_step(j) << 4))) + j * RB);
+        v[j] = *(const __attribute__((address_space(3))) float*)((at ^ (key_step(j) << 4)) + (row + j) * RB);
       return v;
     }
   }
@@ -184,6 +187,12 @@ template <typename T, int D> struct HeadRows {
     return (x & (KEYS / 2 - 1)) << 1 | x / (KEYS / 2);
   }
 };
+
+// Transposed operands on their way: the first kAhead dimension tiles are read before
+// the softmax's arithmetic, each later one when one of them has been used.  Left to
+// itself the compiler reads each right before its use, to save registers.
+constexpr int kAhead = 2;
+__device__ __forceinline__ void pin() { __builtin_amdgcn_sched_barrier(0); }
 
 // Two tiles of ROWS rows each (A and B, of one head) from global memory into LDS,
 // asynchronously.  Rows past the last one are read from the last one.

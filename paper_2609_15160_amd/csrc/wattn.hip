@@ -114,8 +114,8 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
   }
   bool started = false;
 
-  // one operand's rows of keys, from k0 on, at kb and their values at vb
-  auto products = [&](int mask, int k0, unsigned kb, unsigned vb) __attribute__((always_inline)) {
+  // one operand's rows of keys, from k0 on, row t of the tile whose read addresses are ka (keys) and va (values)
+  auto products = [&](int mask, int k0, int t, const unsigned (&ka)[KSTEPS], const unsigned (&va)[DT]) __attribute__((always_inline)) {
     f32x4 sc[QN][NT];
     auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
         for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KSTEPS; ++ks) {
-          const Frag kf = H::load(kb + nt * 16 * H::RB, at, ks);
+          const Frag kf = H::load(ka[ks], t + nt * 16);
 #pragma unroll
           for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = O::mma(kf, qf[qn][ks], sc[qn][nt]);
         }
@@ -159,6 +159,10 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
       }
     };
     scores();
+    Frag vf[kAhead];
+#pragma unroll
+    for (int dt = 0; dt < kAhead && dt < DT; ++dt) vf[dt] = H::load_t(va[dt], t);
+    pin();
     bool move = !started;
     float sum[QN];
     if (!move) {
@@ -212,9 +216,10 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
     for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(sc[qn]);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const Frag vf = H::load_t(vb, att, dt);
 #pragma unroll
-      for (int qn = 0; qn < QN; ++qn) o[dt][qn] = O::mma(vf, pf[qn], o[dt][qn]);
+      for (int qn = 0; qn < QN; ++qn) o[dt][qn] = O::mma(vf[dt % kAhead], pf[qn], o[dt][qn]);
+      if (dt + kAhead < DT) vf[dt % kAhead] = H::load_t(va[dt + kAhead], t);
+      pin();
     }
   };
 
@@ -239,11 +244,16 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
       if (!mine) continue;
       const unsigned kb = base + (i & 1) * Loader::BYTES;
       const int k0 = (i < sinks ? i : first + i - sinks) * BN;
-#pragma unroll 1
+      unsigned ka[KSTEPS], va[DT];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) ka[ks] = H::step(kb + at, ks);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) va[dt] = H::tile(kb + BN * H::RB + att, dt);
+#pragma unroll
       for (int t = 0; t < BN; t += H::ROWS) {
         const bool whole = k0 + t >= clear0 && k0 + t + H::ROWS - 1 <= pw0;
         const int mask = whole ? M_NONE : mask_of(pw0, pw1, k0 + t, k0 + t + H::ROWS - 1, a.window, a.sinks);
-        if (mask >= 0) products(mask, k0 + t, kb + t * H::RB, kb + (BN + t) * H::RB);
+        if (mask >= 0) products(mask, k0 + t, t, ka, va);
       }
     }
   }
@@ -317,10 +327,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)row * a.qs + (h0 + min(c16, cols - 1)) * D + g * H::EPC;
 #pragma unroll
   for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *reinterpret_cast<const Frag*>(q + ks * 4 * H::EPC);
-  const unsigned att = H::transposed(lane);
   const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
   const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
   char* mine = lds + wave * kFewKeys * H::RB;
+  const unsigned att = lds_offset(mine) + H::transposed(lane);
 
   Frag kf[NT][KSTEPS];
   uint4 vf[VN];
@@ -387,7 +397,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
     for (int t = 0; t < NT / O::TILES; ++t) {
       const Frag pf = O::pack(&sc[t * O::TILES]);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = O::mma(H::load_t(lds_offset(mine) + t * H::ROWS * H::RB, att, dt), pf, o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = O::mma(H::load_t(H::tile(att, dt), t * H::ROWS), pf, o[dt]);
     }
     asm volatile("" ::: "memory");
   }

@@ -71,7 +71,7 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
       d.load(reinterpret_cast<const T*>(a.dout) + row * a.os + h * D);
       const float w = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.scale_log2, -a.lse[(int64_t)h * a.rows_q + row]));
       dv.add(w, d);
-      dk.add(w * (d.dot(v) - a.delta[(int64_t)h * a.rows_q + row]), q);
+      dk.add(w * (d.dot(v) + a.ndelta[(int64_t)h * a.rows_q + row]), q);
     }
   dk.store(reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D, a.scale);
   dv.store(reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D, 1.f);
@@ -124,7 +124,10 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
     }
     delta[qn] = sum_quads(t);
     lse[qn] = a.lse[(int64_t)h * a.rows_q + at];
-    if (g == 0 && r0 + qn * 16 + c16 < s.nq) a.delta[(int64_t)h * a.rows_q + at] = delta[qn];
+    if (g == 0 && r0 + qn * 16 + c16 < s.nq) {  // for k_wattn_dkv, whose products start from them
+      a.ndelta[(int64_t)h * a.rows_q + at] = -delta[qn];
+      a.nlse[(int64_t)h * a.rows_q + at] = -lse[qn] / a.scale_log2;
+    }
   }
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
@@ -142,8 +145,9 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) dq[dt][qn] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // one operand's rows of keys, from k0 on, at kb and their values at vb
-  auto products = [&](int mask, int k0, unsigned kb, unsigned vb) __attribute__((always_inline)) {
+  // one operand's rows of keys, from k0 on, row t of the tile whose read addresses are ka (keys; values BN rows
+  // further) and ta (keys transposed)
+  auto products = [&](int mask, int k0, int t, const unsigned (&ka)[KSTEPS], const unsigned (&ta)[DT]) __attribute__((always_inline)) {
     f32x4 sc[QN][TL], dp[QN][TL];
 #pragma unroll
     for (int n = 0; n < TL; ++n) {
@@ -154,7 +158,7 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
       }
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) {
-        const Frag kf = H::load(kb + n * 16 * H::RB, at, ks), vf = H::load(vb + n * 16 * H::RB, at, ks);
+        const Frag kf = H::load(ka[ks], t + n * 16), vf = H::load(ka[ks], BN + t + n * 16);
 #pragma unroll
         for (int qn = 0; qn < QN; ++qn) {
           sc[qn][n] = O::mma(kf, qf[qn][ks], sc[qn][n]);
@@ -162,6 +166,10 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
         }
       }
     }
+    Frag tk[kAhead];
+#pragma unroll
+    for (int dt = 0; dt < kAhead && dt < DT; ++dt) tk[dt] = H::load_t(ta[dt], t);
+    pin();
     // scores that are not visible are -inf: their weights and their dS are 0
     if (mask == M_UPPER) {
 #pragma unroll
@@ -202,9 +210,10 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const Frag kf = H::load_t(kb, att, dt);
 #pragma unroll
-      for (int qn = 0; qn < QN; ++qn) dq[dt][qn] = O::mma(kf, pf[qn], dq[dt][qn]);
+      for (int qn = 0; qn < QN; ++qn) dq[dt][qn] = O::mma(tk[dt % kAhead], pf[qn], dq[dt][qn]);
+      if (dt + kAhead < DT) tk[dt % kAhead] = H::load_t(ta[dt + kAhead], t);
+      pin();
     }
   };
 
@@ -229,11 +238,16 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
       if (!mine) continue;
       const unsigned kb = base + (i & 1) * Loader::BYTES;
       const int k0 = (i < sinks ? i : first + i - sinks) * BN;
-#pragma unroll 1
+      unsigned ka[KSTEPS], ta[DT];
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) ka[ks] = H::step(kb + at, ks);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) ta[dt] = H::tile(kb + att, dt);
+#pragma unroll
       for (int t = 0; t < BN; t += H::ROWS) {
         const bool whole = k0 + t >= clear0 && k0 + t + H::ROWS - 1 <= pw0;
         const int mask = whole ? M_NONE : mask_of(pw0, pw1, k0 + t, k0 + t + H::ROWS - 1, a.window, a.sinks);
-        if (mask >= 0) products(mask, k0 + t, kb + t * H::RB, kb + (BN + t) * H::RB);
+        if (mask >= 0) products(mask, k0 + t, t, ka, ta);
       }
     }
   }
@@ -265,20 +279,21 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
 
 // One workgroup: a tile of NW * KN * 16 keys of one key head, whose rows stay in
 // registers (each wave KN tiles of 16), over tiles of BQ queries of every head that
-// shares them; q and do, with their lse and delta, come through two places in LDS.
+// shares them; q and do, with their lse and delta, which the products of the scores and of dP
+// start from, come through two places in LDS.
 // A tile's keys are seen by the queries from its first position to the window's end
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
 template <typename T, int D, int NW, int KN>
-__global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
+__global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void k_wattn_dkv(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
-  constexpr int KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 ? 64 : 32;
+  constexpr int KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 && D == 64 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BQ, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
-  __shared__ __align__(16) float stats[2][2][kWave];  // of each place: lse, delta
+  __shared__ __align__(16) float stats[2][2][kWave];  // of each place: nlse, ndelta
 
   const int sink_blocks = a.batch * a.kv_heads * a.sink_parts;  // sink_parts = 0: first tiles are as others
   int b, kvh, tile, part = 0, parts = 1;
@@ -315,22 +330,20 @@ __global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2))
   // queries [j0, j1] see a key of the tile
   const int last = k0 < a.sinks || a.window > s.n - 1 - k1 ? s.n - 1 : k1 + a.window - 1;
   const int j0 = max(0, k0 - off), j1 = last - off;
-  // one operand's rows of queries, from row j on, at qb and their do at db
-  auto products = [&](int mask, int j, unsigned qb, unsigned db, const float* stat) __attribute__((always_inline)) {
+  // one operand's rows of queries, from row j on, with read addresses qa and ta (transposed); their do lies BQ rows further
+  auto products = [&](int mask, int j, unsigned qa, unsigned ta, const float* stat) __attribute__((always_inline)) {
     f32x4 sc[KN][TL], dp[KN][TL];
-    f32x4 lse[TL];
 #pragma unroll
     for (int n = 0; n < TL; ++n) {
-      lse[n] = Vec4<float>::load(stat + n * 16 + 4 * g);
-      const f32x4 delta = Vec4<float>::load(stat + kWave + n * 16 + 4 * g);
+      const f32x4 nlse = Vec4<float>::load(stat + n * 16 + 4 * g), ndelta = Vec4<float>::load(stat + kWave + n * 16 + 4 * g);
 #pragma unroll
       for (int kn = 0; kn < KN; ++kn) {
-        sc[kn][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        dp[kn][n] = -delta;
+        sc[kn][n] = nlse;
+        dp[kn][n] = ndelta;
       }
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) {
-        const Frag qf = H::load(qb + n * 16 * H::RB, at, ks), df = H::load(db + n * 16 * H::RB, at, ks);
+        const Frag qf = H::load(H::step(qa, ks), n * 16), df = H::load(H::step(qa, ks), BQ + n * 16);
 #pragma unroll
         for (int kn = 0; kn < KN; ++kn) {
           sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
@@ -378,7 +391,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2))
       for (int n = 0; n < TL; ++n)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          sc[kn][n][r] = __builtin_amdgcn_exp2f(fmaf(sc[kn][n][r], a.scale_log2, -lse[n][r]));
+          sc[kn][n][r] = __builtin_amdgcn_exp2f(sc[kn][n][r] * a.scale_log2);
           dp[kn][n][r] *= sc[kn][n][r];
         }
       pf[kn] = O::pack(sc[kn]);
@@ -386,7 +399,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2))
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      const Frag df = H::load_t(db, att, dt), qf = H::load_t(qb, att, dt);
+      const Frag df = H::load_t(H::tile(ta, dt), BQ), qf = H::load_t(H::tile(ta, dt), 0);
 #pragma unroll
       for (int kn = 0; kn < KN; ++kn) {
         dv[dt][kn] = O::mma(df, pf[kn], dv[dt][kn]);
@@ -427,8 +440,8 @@ __global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2))
       // 64 values each, of which the tile uses the first BQ
       const int64_t stat = (int64_t)h * a.rows_q + row;
       const unsigned to = sbase + place * (unsigned)sizeof(stats[0]), lane4 = (unsigned)min(lane, most) * 4u;
-      if (wave == 0) stage4(a.lse + stat, lane4, to);
-      if (wave == (NW > 1 ? 1 : 0)) stage4(a.delta + stat, lane4, to + (unsigned)sizeof(stats[0][0]));
+      if (wave == 0) stage4(a.nlse + stat, lane4, to);
+      if (wave == (NW > 1 ? 1 : 0)) stage4(a.ndelta + stat, lane4, to + (unsigned)sizeof(stats[0][0]));
       if (++it == tiles) {
         it = 0;
         ++ih;
@@ -450,7 +463,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 128 ? 1 : sizeof(T) == 2 ? 3 : 2))
         if (ja > j1) break;
         int mask = mask_of(ja + off, jl + off, w0, w1, a.window, a.sinks);
         if (jl < ja + H::ROWS - 1 && mask >= 0) mask = (mask & M_UPPER) || w0 < a.sinks ? M_ALL : M_LOWER;  // rows behind j1
-        if (mask >= 0) products(mask, ja, qb + t * H::RB, qb + (BQ + t) * H::RB, &stats[place][0][t]);
+        if (mask >= 0) products(mask, ja, qb + t * H::RB + at, qb + t * H::RB + att, &stats[place][0][t]);
       }
     }
   }
@@ -532,7 +545,7 @@ template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wa
 }
 
 constexpr int kManyWaves = 4;
-template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }  // KN: registers
+template <typename T, int D> constexpr int key_tiles() { return D == 128 ? 1 : 2; }  // KN: registers
 
 // Ranges of a first tile's queries, each as long as two other tiles' at least; 0: there
 // are no sinks.
@@ -544,7 +557,7 @@ int sink_parts(const tlf_attn_shape& t) {
 
 bool many_keys(const tlf_attn_shape& t) { return slots_of<128>(t.rows_k, t.batch) * t.kv_heads >= 512; }
 
-int64_t delta_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }
+int64_t stat_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }
 int64_t part_floats(const tlf_attn_shape& t) {
   const int parts = many_keys(t) ? sink_parts(t) : 0;
   return parts > 1 ? (int64_t)t.batch * t.kv_heads * parts * 128 * 2 * t.head_dim : 0;
@@ -587,7 +600,7 @@ extern "C" {
 int tlf_attn_grad_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes) {
   const int st = tlf::wattn_check(shape);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  *ws_bytes = (size_t)(tlf::delta_floats(*shape) + tlf::part_floats(*shape)) * sizeof(float);
+  *ws_bytes = (size_t)(2 * tlf::stat_floats(*shape) + tlf::part_floats(*shape)) * sizeof(float);
   return TLF_OK;
 }
 
@@ -623,8 +636,9 @@ int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q
   a.dqs = dq_stride;
   a.dks = dk_stride;
   a.dvs = dv_stride;
-  a.delta = (float*)d_workspace;
-  a.part = a.delta + tlf::delta_floats(*shape);
+  a.nlse = (float*)d_workspace;
+  a.ndelta = a.nlse + tlf::stat_floats(*shape);
+  a.part = a.ndelta + tlf::stat_floats(*shape);
   const hipStream_t s = (hipStream_t)stream;
   const bool h = shape->dtype == TLF_DTYPE_BF16;
   const hipError_t e = shape->head_dim == 16    ? tlf::launch<float, 16>(*shape, a, s)
