@@ -25,13 +25,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 8192;                     // elements of a workgroup
 constexpr int kTensors = 160;                  // of a launch: its arguments stay below 4 KiB
-constexpr int64_t kBlocks = (1 << 24) - 1;     // of a launch, which has fewer than 2^32 threads
+constexpr int64_t kGroups = 4096;              // workgroups of a launch, which take its pieces in turn
 constexpr int kTotalThreads = 1024;
+constexpr int64_t kMost = (int64_t)1 << 35;    // elements of a tensor
+static_assert(kTensors * (kMost / kPer) < INT32_MAX, "pieces of a launch");
 
 struct GradArgs {
   void* g[kTensors];
   int64_t n[kTensors];              // times four, plus the flags below
-  int32_t first[kTensors + 1];      // workgroups before each tensor
+  int32_t first[kTensors + 1];      // pieces before each tensor
   int32_t count;
   double* part;
   const float* scale;
@@ -40,7 +42,7 @@ enum { kBf16 = 1, kVector = 2 };
 static_assert(sizeof(GradArgs) <= 4096, "kernel arguments");
 
 __device__ __forceinline__ int tensor_of(const GradArgs& a, int block) {
-  int lo = 0, hi = a.count - 1;  // the last tensor whose workgroups start at or before this one
+  int lo = 0, hi = a.count - 1;  // the last tensor whose pieces start at or before this one
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.first[mid] <= block) lo = mid;
@@ -110,11 +112,14 @@ __device__ __forceinline__ double wave_total(double v) {
 
 __global__ __launch_bounds__(kThreads) void k_grad_squares(GradArgs a) {
   __shared__ double sums[kThreads / kWave];
-  const int k = tensor_of(a, blockIdx.x);
-  const int64_t n = a.n[k] >> 2, base = (int64_t)(blockIdx.x - a.first[k]) * kPer;
-  const bool vec = a.n[k] & kVector;
-  double s = a.n[k] & kBf16 ? squares(reinterpret_cast<const bf16*>(a.g[k]), n, base, vec)
-                            : squares(reinterpret_cast<const float*>(a.g[k]), n, base, vec);
+  double s = 0.0;
+  for (int block = blockIdx.x; block < a.first[a.count]; block += gridDim.x) {
+    const int k = tensor_of(a, block);
+    const int64_t n = a.n[k] >> 2, base = (int64_t)(block - a.first[k]) * kPer;
+    const bool vec = a.n[k] & kVector;
+    s += a.n[k] & kBf16 ? squares(reinterpret_cast<const bf16*>(a.g[k]), n, base, vec)
+                        : squares(reinterpret_cast<const float*>(a.g[k]), n, base, vec);
+  }
   s = wave_total(s);
   if (lane_id() == 0) sums[threadIdx.x / kWave] = s;
   __syncthreads();
@@ -162,42 +167,39 @@ template <typename T> __device__ __forceinline__ void scale_all(T* g, int64_t n,
 __global__ __launch_bounds__(kThreads) void k_grad_scale(GradArgs a) {
   const float f = *a.scale;
   if (f == 1.f) return;
-  const int k = tensor_of(a, blockIdx.x);
-  const int64_t n = a.n[k] >> 2, base = (int64_t)(blockIdx.x - a.first[k]) * kPer;
-  const bool vec = a.n[k] & kVector;
-  if (a.n[k] & kBf16) scale_all(reinterpret_cast<bf16*>(a.g[k]), n, base, vec, f);
-  else scale_all(reinterpret_cast<float*>(a.g[k]), n, base, vec, f);
+  for (int block = blockIdx.x; block < a.first[a.count]; block += gridDim.x) {
+    const int k = tensor_of(a, block);
+    const int64_t n = a.n[k] >> 2, base = (int64_t)(block - a.first[k]) * kPer;
+    const bool vec = a.n[k] & kVector;
+    if (a.n[k] & kBf16) scale_all(reinterpret_cast<bf16*>(a.g[k]), n, base, vec, f);
+    else scale_all(reinterpret_cast<float*>(a.g[k]), n, base, vec, f);
+  }
 }
 
 int64_t blocks_of(int64_t n) { return (n + kPer - 1) / kPer; }
 
-int check(const tlf_grad* grads, int32_t count, int64_t* blocks) {
+int check(const tlf_grad* grads, int32_t count) {
   if (count < 0 || (count > 0 && !grads)) return TLF_E_INVALID_ARG;
-  *blocks = 0;
   int st = TLF_OK;
   for (int i = 0; i < count; ++i) {
     const tlf_grad& t = grads[i];
     if (t.n < 0 || (t.dtype != TLF_DTYPE_F32 && t.dtype != TLF_DTYPE_BF16)) return TLF_E_INVALID_ARG;
     if (t.n > 0 && (!t.d_grad || ((uintptr_t)t.d_grad & (t.dtype == TLF_DTYPE_BF16 ? 1u : 3u)) != 0)) return TLF_E_INVALID_ARG;
-    if (t.n > (int64_t)1 << 35) st = TLF_E_UNSUPPORTED;
-    *blocks += st == TLF_OK ? blocks_of(t.n) : 0;
+    if (t.n > kMost) st = TLF_E_UNSUPPORTED;
   }
   return st;
 }
 
-// Launches `kernel` over all tensors, as many of them at a time as its arguments hold.
-template <typename K> hipError_t launch(K kernel, const tlf_grad* grads, int32_t count, double* part, const float* scale, hipStream_t s) {
+// The launches over all tensors, as many of them at a time as the arguments hold:
+// go(arguments, workgroups) for each.
+template <typename F> int launches(const tlf_grad* grads, int32_t count, F go) {
   GradArgs a{};
-  a.part = part;
-  a.scale = scale;
   for (int i = 0; i <= count; ++i) {
     const tlf_grad* t = i < count ? &grads[i] : nullptr;
     const int64_t blocks = t ? blocks_of(t->n) : 0;
-    if (a.count > 0 && (!t || a.count == kTensors || a.first[a.count] + blocks > kBlocks)) {  // full, or done
-      hipLaunchKernelGGL(kernel, dim3(a.first[a.count]), dim3(kThreads), 0, s, a);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      if (a.part) a.part += a.first[a.count];
+    if (a.count > 0 && (!t || a.count == kTensors)) {  // full, or done; its pieces are less than 2^31
+      const int st = go(a, (int)std::min<int64_t>(a.first[a.count], kGroups));
+      if (st != TLF_OK) return st;
       a.count = 0;
     }
     if (blocks == 0) continue;
@@ -207,7 +209,17 @@ template <typename K> hipError_t launch(K kernel, const tlf_grad* grads, int32_t
     a.first[a.count + 1] = a.first[a.count] + (int32_t)blocks;
     ++a.count;
   }
-  return hipSuccess;
+  return TLF_OK;
+}
+
+// Workgroups of all launches, each of which has a sum.
+int64_t sums_of(const tlf_grad* grads, int32_t count) {
+  int64_t n = 0;
+  launches(grads, count, [&](GradArgs&, int groups) {
+    n += groups;
+    return TLF_OK;
+  });
+  return n;
 }
 
 }  // namespace
@@ -217,31 +229,36 @@ template <typename K> hipError_t launch(K kernel, const tlf_grad* grads, int32_t
 extern "C" {
 
 int tlf_grad_norm_ws_bytes(const tlf_grad* h_grads, int32_t count, size_t* ws_bytes) {
-  int64_t blocks = 0;
-  const int st = tlf::check(h_grads, count, &blocks);
+  const int st = tlf::check(h_grads, count);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  *ws_bytes = (size_t)blocks * sizeof(double);
+  *ws_bytes = (size_t)tlf::sums_of(h_grads, count) * sizeof(double);
   return TLF_OK;
 }
 
 int tlf_grad_norm(const tlf_grad* h_grads, int32_t count, double max_norm, float* d_norm, float* d_scale, void* d_workspace,
                   size_t ws_bytes, void* stream) {
-  int64_t blocks = 0;
-  const int st = tlf::check(h_grads, count, &blocks);
+  int st = tlf::check(h_grads, count);
   if (st != TLF_OK) return st;
   if (!(max_norm > 0.0) || !d_norm || ((uintptr_t)d_norm & 3u) != 0 || ((uintptr_t)d_scale & 3u) != 0) return TLF_E_INVALID_ARG;
-  if (blocks > 0 && (!d_workspace || ((uintptr_t)d_workspace & 7u) != 0 || ws_bytes < (size_t)blocks * sizeof(double)))
+  const int64_t sums = tlf::sums_of(h_grads, count);
+  if (sums > 0 && (!d_workspace || ((uintptr_t)d_workspace & 7u) != 0 || ws_bytes < (size_t)sums * sizeof(double)))
     return TLF_E_INVALID_ARG;
   const hipStream_t s = (hipStream_t)stream;
-  if (tlf::launch(tlf::k_grad_squares, h_grads, count, (double*)d_workspace, nullptr, s) != hipSuccess) return TLF_E_HIP;
-  hipLaunchKernelGGL(tlf::k_grad_total, dim3(1), dim3(tlf::kTotalThreads), 0, s, (const double*)d_workspace, blocks, max_norm,
+  double* part = (double*)d_workspace;
+  st = tlf::launches(h_grads, count, [&](tlf::GradArgs& a, int groups) {
+    a.part = part;
+    part += groups;
+    hipLaunchKernelGGL(tlf::k_grad_squares, dim3(groups), dim3(tlf::kThreads), 0, s, a);
+    return hipGetLastError() == hipSuccess ? TLF_OK : TLF_E_HIP;
+  });
+  if (st != TLF_OK) return st;
+  hipLaunchKernelGGL(tlf::k_grad_total, dim3(1), dim3(tlf::kTotalThreads), 0, s, (const double*)d_workspace, sums, max_norm,
                      d_norm, d_scale);
   return hipGetLastError() == hipSuccess ? TLF_OK : TLF_E_HIP;
 }
 
 int tlf_grad_clip(const tlf_grad* h_grads, int32_t count, const float* d_scale, void* stream) {
-  int64_t blocks = 0;
-  const int st = tlf::check(h_grads, count, &blocks);
+  const int st = tlf::check(h_grads, count);
   if (st != TLF_OK) return st;
   if (!d_scale || ((uintptr_t)d_scale & 3u) != 0) return TLF_E_INVALID_ARG;
   // workgroups run in no order: what they write overlaps nothing else of the call
@@ -260,7 +277,11 @@ int tlf_grad_clip(const tlf_grad* h_grads, int32_t count, const float* d_scale, 
   std::sort(ranges.get(), ranges.get() + n, [](const Range& a, const Range& b) { return a.begin < b.begin; });
   for (size_t k = 1; k < n; ++k)
     if (ranges[k].begin < ranges[k - 1].end) return TLF_E_INVALID_ARG;
-  return tlf::launch(tlf::k_grad_scale, h_grads, count, nullptr, d_scale, (hipStream_t)stream) == hipSuccess ? TLF_OK : TLF_E_HIP;
+  return tlf::launches(h_grads, count, [&](tlf::GradArgs& a, int groups) {
+    a.scale = d_scale;
+    hipLaunchKernelGGL(tlf::k_grad_scale, dim3(groups), dim3(tlf::kThreads), 0, (hipStream_t)stream, a);
+    return hipGetLastError() == hipSuccess ? TLF_OK : TLF_E_HIP;
+  });
 }
 
 }  // extern "C"

@@ -273,6 +273,15 @@ __global__ __launch_bounds__(MAXT) void k_resid_grad(ResidArgs a, int chunk, int
   }
 }
 
+// Rows of a workgroup: 8 waves per compute unit where the rows allow it, all that the
+// registers let run at a time, and 8 rows at least, so that the sums stay a small part
+// of the traffic and few rows still spread.
+int resid_chunk(int rows, int d) {
+  const int waves = (d + kGammaCols - 1) / kGammaCols, most = 2048 / waves;
+  const int c = (rows + most - 1) / most;
+  return c < 8 ? 8 : c;
+}
+
 constexpr int kLaunchRows = 1 << 24;  // a launch has fewer than 2^32 threads
 
 template <typename T, bool GRAD, bool POST, bool PAST> hipError_t launch_rows(ResidArgs a, hipStream_t s) {
@@ -318,7 +327,7 @@ void launch_sums(const ResidArgs& a, int chunk, int chunks, float* part, hipStre
 template <typename T, bool POST, bool PAST>
 hipError_t launch_grad(const ResidArgs& a, float* dalpha, float* dgamma, float* part, hipStream_t s) {
   if (!dalpha && !dgamma) return a.rows > 0 ? launch_rows<T, true, POST, PAST>(a, s) : hipSuccess;
-  const int chunk = grad_chunk(a.rows, a.d), chunks = grad_chunks(a.rows, a.d), n = a.groups * a.d;
+  const int chunk = resid_chunk(a.rows, a.d), chunks = (a.rows + chunk - 1) / chunk, n = a.groups * a.d;
   if (chunks > 0) {
     if (a.d <= 1024) launch_sums<T, 256, 2, POST, PAST>(a, chunk, chunks, part, s);
     else if (a.d <= 2048) launch_sums<T, 512, 2, POST, PAST>(a, chunk, chunks, part, s);
@@ -380,7 +389,8 @@ int tlf_residual_norm(const float* d_x, const void* d_y, int32_t y_dtype, const 
 int tlf_residual_norm_grad_ws_bytes(int32_t groups, int32_t rows, int32_t d, size_t* ws_bytes) {
   const int st = tlf::check(TLF_DTYPE_F32, groups, rows, d);
   if (st != TLF_OK || !ws_bytes) return st != TLF_OK ? st : TLF_E_INVALID_ARG;
-  *ws_bytes = (size_t)tlf::grad_chunks(rows, d) * 2 * groups * d * sizeof(float);
+  const int chunk = tlf::resid_chunk(rows, d);
+  *ws_bytes = (size_t)((rows + chunk - 1) / chunk) * 2 * groups * d * sizeof(float);
   return TLF_OK;
 }
 

@@ -309,12 +309,17 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   const int gc = unit % chunks, kvh = unit / chunks % a.kv_heads, row = unit / (chunks * a.kv_heads);
   const int h0 = kvh * each + gc * 16, cols = min(each - gc * 16, 16);
 
-  int b = 0;  // the last sequence that begins at or before the row
-  for (int hi = a.batch; hi > b;) {
-    const int step = (hi - b + kWave - 1) / kWave, x = b + (lane_id() + 1) * step;
-    const bool before = x <= hi && a.q_off[min(x, hi)] <= row;
-    b += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * step;
-    hi = min(hi, b + step - 1);
+  // The last sequence that begins at or before the row: with a row of each sequence it is
+  // the row's own number, which is tried first (the search costs two trips to memory).
+  int b = min(row, a.batch);
+  if (a.q_off[b] > row || (b < a.batch && row >= a.q_off[b + 1])) {
+    b = 0;
+    for (int hi = a.batch; hi > b;) {
+      const int step = (hi - b + kWave - 1) / kWave, x = b + (lane_id() + 1) * step;
+      const bool before = x <= hi && a.q_off[min(x, hi)] <= row;
+      b += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * step;
+      hi = min(hi, b + step - 1);
+    }
   }
   const WSeq s = load_seq(a, b);
   const int p = row - s.q0 + s.n - s.nq;
