@@ -58,11 +58,15 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // visible tiles of BN keys, which all waves share from two places in LDS (one tile
 // is used while the next arrives; one barrier a tile).
 //
-// The softmax base m of a query moves only where it must: a tile's weights are
-// exp2(s - m) at once, and only if a lane's weights of a tile add up to more than
-// kSumMax, or a query has no base yet, the tile is done again with a new base and
-// the sums are rescaled.  o / l does not depend on the base, and weights below
-// kSumMax are far inside float32's and bf16's range.
+// The softmax base of a query is the largest score of the first tile that it sees a
+// key of: weights are exp2(s - base) at once, without a maximum per tile.  Where a
+// query's sum has grown past kSumMax the base moves up and the sums are scaled down,
+// exactly, by a power of two; o / l does not depend on it.  Weights that leave float32's
+// range within a tile (scores 127 above the base in base 2) make the row not finite, and
+// it is done again by slow_row.  The sum is of the weights before their rounding: the sum
+// of the rounded ones, a product with ones, saves an add for each weight (forward pass of
+// 8 x 4096 x 16 x 64, window 1024: 171 us) but is off by as much as a weight, and with
+// it every weight of the backward pass.
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
   using H = HeadRows<T, D>;
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
   typedef typename O::frag Frag;
   constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NT = O::TILES;
-  constexpr float kSumMax = 65536.f;
+  constexpr float kSumMax = 0x1p60f;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
 
@@ -102,13 +106,12 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) settle(qf[qn][ks]);
   const unsigned at = H::direct(lane), att = H::transposed(lane);
-
   f32x4 o[DT][QN];
-  float m[QN], l[QN];
+  float ls[QN], base[QN];  // this lane's part of the sum of weights; the base, -inf: none yet
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
-    m[qn] = -INFINITY;
-    l[qn] = 0.f;
+    base[qn] = -INFINITY;
+    ls[qn] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt][qn] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -117,72 +120,50 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
   // one operand's rows of keys, from k0 on, row t of the tile whose read addresses are ka (keys) and va (values)
   auto products = [&](int mask, int k0, int t, const unsigned (&ka)[KSTEPS], const unsigned (&va)[DT]) __attribute__((always_inline)) {
     f32x4 sc[QN][NT];
-    auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int ks = 0; ks < KSTEPS; ++ks) {
-          const Frag kf = H::load(ka[ks], t + nt * 16);
+      for (int ks = 0; ks < KSTEPS; ++ks) {
+        const Frag kf = H::load(ka[ks], t + nt * 16);
 #pragma unroll
-          for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = O::mma(kf, qf[qn][ks], sc[qn][nt]);
-        }
+        for (int qn = 0; qn < QN; ++qn) sc[qn][nt] = O::mma(kf, qf[qn][ks], sc[qn][nt]);
       }
-      if (mask == M_UPPER) {
+    }
+    if (mask == M_UPPER) {
 #pragma unroll
-        for (int qn = 0; qn < QN; ++qn) {
-          const int last = p[qn] - k0 - 4 * g;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sc[qn][nt][r] = last >= nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
-        }
-      } else if (mask == M_LOWER) {
-#pragma unroll
-        for (int qn = 0; qn < QN; ++qn) {
-          const int before = p[qn] - k0 - 4 * g - a.window;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sc[qn][nt][r] = before < nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
-        }
-      } else if (mask == M_ALL) {
+      for (int qn = 0; qn < QN; ++qn) {
+        const int last = p[qn] - k0 - 4 * g;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int x = k0 + nt * 16 + 4 * g + r, far = reach(x, a.window, a.sinks);
-#pragma unroll
-            for (int qn = 0; qn < QN; ++qn) sc[qn][nt][r] = sees(p[qn], x, far) ? sc[qn][nt][r] : -INFINITY;
-          }
+          for (int r = 0; r < 4; ++r) sc[qn][nt][r] = last >= nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
       }
-    };
-    scores();
+    } else if (mask == M_LOWER) {
+#pragma unroll
+      for (int qn = 0; qn < QN; ++qn) {
+        const int before = p[qn] - k0 - 4 * g - a.window;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[qn][nt][r] = before < nt * 16 + r ? sc[qn][nt][r] : -INFINITY;
+      }
+    } else if (mask == M_ALL) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int x = k0 + nt * 16 + 4 * g + r, far = reach(x, a.window, a.sinks);
+#pragma unroll
+          for (int qn = 0; qn < QN; ++qn) sc[qn][nt][r] = sees(p[qn], x, far) ? sc[qn][nt][r] : -INFINITY;
+        }
+    }
     Frag vf[kAhead];
 #pragma unroll
     for (int dt = 0; dt < kAhead && dt < DT; ++dt) vf[dt] = H::load_t(va[dt], t);
     pin();
-    bool move = !started;
-    float sum[QN];
-    if (!move) {
-      bool over = false;
-#pragma unroll
-      for (int qn = 0; qn < QN; ++qn) {
-        sum[qn] = 0.f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            sc[qn][nt][r] = __builtin_amdgcn_exp2f(fmaf(sc[qn][nt][r], a.scale_log2, -m[qn]));
-            sum[qn] += sc[qn][nt][r];
-          }
-        over |= !(sum[qn] <= kSumMax);
-      }
-      move = __builtin_amdgcn_ballot_w64(over) != 0;
-      if (move) scores();
-    }
-    if (move) {
+    if (!started) {
       bool none = false;
 #pragma unroll
       for (int qn = 0; qn < QN; ++qn) {
@@ -191,26 +172,23 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qn][nt][r]);
-        mx = fmaxf(m[qn], max_quads(mx) * a.scale_log2);
-        const float base = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(m[qn] - base);
-        none |= mx == -INFINITY;
-        m[qn] = mx;
-        l[qn] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt][qn] *= alpha;
-        sum[qn] = 0.f;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            sc[qn][nt][r] = __builtin_amdgcn_exp2f(fmaf(sc[qn][nt][r], a.scale_log2, -base));
-            sum[qn] += sc[qn][nt][r];
-          }
+        mx = ceilf(max_quads(mx) * a.scale_log2);  // whole numbers: moving it is exact too
+        if (base[qn] == -INFINITY) base[qn] = mx;
+        none |= base[qn] == -INFINITY;
       }
       started = __builtin_amdgcn_ballot_w64(none) == 0;
     }
 #pragma unroll
-    for (int qn = 0; qn < QN; ++qn) l[qn] += sum[qn];
+    for (int qn = 0; qn < QN; ++qn) {
+      const float from = started || base[qn] != -INFINITY ? base[qn] : 0.f;  // without a base all weights are 0
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          sc[qn][nt][r] = __builtin_amdgcn_exp2f(fmaf(sc[qn][nt][r], a.scale_log2, -from));
+          ls[qn] += sc[qn][nt][r];
+        }
+    }
     Frag pf[QN];
 #pragma unroll
     for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(sc[qn]);
@@ -223,6 +201,19 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
     }
   };
 
+  auto move_base = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int qn = 0; qn < QN; ++qn) {
+      const float sum = sum_quads(ls[qn]);
+      const int up = sum > 1.f && sum < INFINITY ? min((int)(__float_as_uint(sum) >> 23) - 127, 100) : 0;
+      const float f = __uint_as_float((unsigned)(127 - up) << 23);  // 2^-up
+      base[qn] += (float)up;
+      ls[qn] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt][qn] *= f;
+    }
+  };
+
   if (s.n > 0 && p1 >= 0) {
     Loader ld;
     ld.init();
@@ -232,10 +223,19 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
     const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
     const unsigned base = lds_offset(lds);
     const int clear0 = max(pw1, 0) - a.window + 1;  // keys from here on are in the window of all of the wave's queries
+    const T *kp = k, *vp = v;  // of the tile that is issued next, and its rows up to the last
+    int left = s.n - 1;
     auto issue = [&](int i) __attribute__((always_inline)) {
-      const int row = (i < sinks ? i : first + i - sinks) * BN;
-      ld.issue(k + row * a.ks, v + row * a.vs, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), s.n - 1 - row,
-               base + (i & 1) * Loader::BYTES);
+      if (i == sinks) {
+        const int row = first * BN;
+        kp = k + row * a.ks;
+        vp = v + row * a.vs;
+        left = s.n - 1 - row;
+      }
+      ld.issue(kp, vp, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), left, base + (i & 1) * Loader::BYTES);
+      kp += BN * a.ks;
+      vp += BN * a.vs;
+      left -= BN;
     };
     issue(0);
     for (int i = 0; i < count; ++i) {
@@ -255,13 +255,14 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
         const int mask = whole ? M_NONE : mask_of(pw0, pw1, k0 + t, k0 + t + H::ROWS - 1, a.window, a.sinks);
         if (mask >= 0) products(mask, k0 + t, t, ka, va);
       }
+      if (__builtin_amdgcn_ballot_w64(ls[0] > kSumMax || ls[1] > kSumMax)) move_base();
     }
   }
   if (!mine) return;
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
     const int row = r0 + qn * 16 + c16;
-    const float sum = sum_quads(l[qn]), inv = p[qn] < 0 ? 0.f : 1.f / sum;
+    const float sum = sum_quads(ls[qn]), inv = p[qn] < 0 ? 0.f : 1.f / sum;
     bool good = true;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T
       } else {
         Vec4<T>::store(dst + g * 4, o[0][qn]);
       }
-      if (a.lse && g == 0) a.lse[(int64_t)h * a.rows_q + s.q0 + row] = p[qn] < 0 ? INFINITY : m[qn] + log2f(sum);
+      if (a.lse && g == 0) a.lse[(int64_t)h * a.rows_q + s.q0 + row] = p[qn] < 0 ? INFINITY : base[qn] + log2f(sum);
     }
     for (; again; again &= again - 1) slow_row<T, D>(a, s, h, r0 + qn * 16 + __builtin_ctzll(again));
   }

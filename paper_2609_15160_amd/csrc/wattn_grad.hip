@@ -226,10 +226,19 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
     const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
     const unsigned base = lds_offset(lds);
     const int clear0 = max(pw1, 0) - a.window + 1;  // keys from here on are in the window of all of the wave's queries
+    const T *kp = k, *vp = v;  // of the tile that is issued next, and its rows up to the last
+    int left = s.n - 1;
     auto issue = [&](int i) __attribute__((always_inline)) {
-      const int row = (i < sinks ? i : first + i - sinks) * BN;
-      ld.issue(k + row * a.ks, v + row * a.vs, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), s.n - 1 - row,
-               base + (i & 1) * Loader::BYTES);
+      if (i == sinks) {
+        const int row = first * BN;
+        kp = k + row * a.ks;
+        vp = v + row * a.vs;
+        left = s.n - 1 - row;
+      }
+      ld.issue(kp, vp, (int)(a.ks * sizeof(T)), (int)(a.vs * sizeof(T)), left, base + (i & 1) * Loader::BYTES);
+      kp += BN * a.ks;
+      vp += BN * a.vs;
+      left -= BN;
     };
     issue(0);
     for (int i = 0; i < count; ++i) {
@@ -285,7 +294,7 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
 template <typename T, int D, int NW, int KN>
-__global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void k_wattn_dkv(GradArgs a) {
+__global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
@@ -293,6 +302,9 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BQ, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
+  constexpr bool VLDS = sizeof(T) == 2 && D == 128;  // the values' rows in LDS, each wave's own: with them in registers a
+                                                      // wave has 16 keys and reads q and do twice as often
+  __shared__ __align__(1024) char vrows[VLDS ? KT * H::RB : 16];
   __shared__ __align__(16) float stats[2][2][kWave];  // of each place: nlse, ndelta
 
   const int sink_blocks = a.batch * a.kv_heads * a.sink_parts;  // sink_parts = 0: first tiles are as others
@@ -319,7 +331,7 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
   const int k0 = tile * KT, k1 = min(k0 + KT, s.n) - 1;     // keys of the tile
   const int w0 = k0 + wave * KW, w1 = min(w0 + KW, s.n) - 1;  // of the wave
 
-  Frag kf[KN][KSTEPS], vf[KN][KSTEPS];
+  Frag kf[KN][KSTEPS], vf[VLDS ? 1 : KN][VLDS ? 1 : KSTEPS];
   const unsigned at = H::direct(lane), att = H::transposed(lane);
   f32x4 dk[DT][KN], dv[DT][KN];
 #pragma unroll
@@ -330,6 +342,7 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
   // queries [j0, j1] see a key of the tile
   const int last = k0 < a.sinks || a.window > s.n - 1 - k1 ? s.n - 1 : k1 + a.window - 1;
   const int j0 = max(0, k0 - off), j1 = last - off;
+  const unsigned va = lds_offset(vrows) + wave * KW * H::RB + at;
   // one operand's rows of queries, from row j on, with read addresses qa and ta (transposed); their do lies BQ rows further
   auto products = [&](int mask, int j, unsigned qa, unsigned ta, const float* stat) __attribute__((always_inline)) {
     f32x4 sc[KN][TL], dp[KN][TL];
@@ -341,15 +354,35 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
         sc[kn][n] = nlse;
         dp[kn][n] = ndelta;
       }
+    }
+    if constexpr (VLDS) {
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) {
-        const Frag qf = H::load(H::step(qa, ks), n * 16), df = H::load(H::step(qa, ks), BQ + n * 16);
+        Frag v[KN];
 #pragma unroll
-        for (int kn = 0; kn < KN; ++kn) {
-          sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
-          dp[kn][n] = O::mma(df, vf[kn][ks], dp[kn][n]);
+        for (int kn = 0; kn < KN; ++kn) v[kn] = H::load(H::step(va, ks), kn * 16);
+#pragma unroll
+        for (int n = 0; n < TL; ++n) {
+          const Frag qf = H::load(H::step(qa, ks), n * 16), df = H::load(H::step(qa, ks), BQ + n * 16);
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn) {
+            sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
+            dp[kn][n] = O::mma(df, v[kn], dp[kn][n]);
+          }
         }
       }
+    } else {
+#pragma unroll
+      for (int n = 0; n < TL; ++n)
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+          const Frag qf = H::load(H::step(qa, ks), n * 16), df = H::load(H::step(qa, ks), BQ + n * 16);
+#pragma unroll
+          for (int kn = 0; kn < KN; ++kn) {
+            sc[kn][n] = O::mma(qf, kf[kn][ks], sc[kn][n]);
+            dp[kn][n] = O::mma(df, vf[kn][ks], dp[kn][n]);
+          }
+        }
     }
     // scores that are not visible are -inf: their weights and their dS are 0
     if (mask == M_UPPER) {
@@ -416,7 +449,9 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) {
         kf[kn][ks] = *reinterpret_cast<const Frag*>(k + ks * 4 * H::EPC);
-        vf[kn][ks] = *reinterpret_cast<const Frag*>(v + ks * 4 * H::EPC);
+        const Frag f = *reinterpret_cast<const Frag*>(v + ks * 4 * H::EPC);
+        if constexpr (VLDS) *reinterpret_cast<Frag*>(vrows + wave * KW * H::RB + H::step(H::direct(lane), ks) + kn * 16 * H::RB) = f;
+        else vf[kn][ks] = f;
       }
     }
 #pragma unroll
@@ -424,30 +459,48 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) {
         settle(kf[kn][ks]);
-        settle(vf[kn][ks]);
+        if constexpr (!VLDS) settle(vf[kn][ks]);
       }
     Loader ld;
     ld.init();
     const int tiles = (j1 - j0 + BQ) / BQ, all = tiles * each;
     const int begin = (int)((int64_t)all * part / parts), end = (int)((int64_t)all * (part + 1) / parts);
     const unsigned base = lds_offset(lds), sbase = lds_offset(stats);
-    int ih = begin / tiles, it = begin % tiles;  // head of the group and tile that are issued next
+    // the tile that is issued next: of head ih of the group, its first row, where it lies
+    int ih = begin / tiles, ij = j0 + begin % tiles * BQ;
+    const T *qp, *dp;
+    const float *lp, *ep;
+    auto at_row = [&]() __attribute__((always_inline)) {
+      const int h = kvh * each + ih;
+      const int64_t row = s.q0 + ij, stat = (int64_t)h * a.rows_q + row;
+      qp = reinterpret_cast<const T*>(a.q) + row * a.qs + h * D;
+      dp = reinterpret_cast<const T*>(a.dout) + row * a.os + h * D;
+      lp = a.nlse + stat;
+      ep = a.ndelta + stat;
+    };
+    at_row();
     auto issue = [&](int place) __attribute__((always_inline)) {
-      const int h = kvh * each + ih, j = j0 + it * BQ, most = s.nq - 1 - j;
-      const int64_t row = s.q0 + j;
-      ld.issue(reinterpret_cast<const T*>(a.q) + row * a.qs + h * D, reinterpret_cast<const T*>(a.dout) + row * a.os + h * D,
-               (int)(a.qs * sizeof(T)), (int)(a.os * sizeof(T)), most, base + place * Loader::BYTES);
+      const int most = s.nq - 1 - ij;
+      ld.issue(qp, dp, (int)(a.qs * sizeof(T)), (int)(a.os * sizeof(T)), most, base + place * Loader::BYTES);
       // 64 values each, of which the tile uses the first BQ
-      const int64_t stat = (int64_t)h * a.rows_q + row;
       const unsigned to = sbase + place * (unsigned)sizeof(stats[0]), lane4 = (unsigned)min(lane, most) * 4u;
-      if (wave == 0) stage4(a.nlse + stat, lane4, to);
-      if (wave == (NW > 1 ? 1 : 0)) stage4(a.ndelta + stat, lane4, to + (unsigned)sizeof(stats[0][0]));
-      if (++it == tiles) {
-        it = 0;
+      if (wave == 0) stage4(lp, lane4, to);
+      if (wave == (NW > 1 ? 1 : 0)) stage4(ep, lane4, to + (unsigned)sizeof(stats[0][0]));
+      ij += BQ;
+      if (ij <= j1) {
+        qp += BQ * a.qs;
+        dp += BQ * a.os;
+        lp += BQ;
+        ep += BQ;
+      } else {
+        ij = j0;
         ++ih;
+        at_row();
       }
     };
     if (begin < end) issue(0);
+    // queries that see all of the wave's keys
+    const int clear0 = w1 - off, clear1 = w1 < a.sinks || a.window > s.n - 1 - w0 ? j1 : min(j1, w0 + a.window - 1 - off);
     int ut = begin % tiles;  // tile that is used next
     for (int i = begin; i < end; ++i) {
       const int place = (i - begin) & 1;
@@ -461,8 +514,11 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 3)) void
       for (int t = 0; t < BQ; t += H::ROWS) {
         const int ja = j + t, jl = min(ja + H::ROWS - 1, j1);
         if (ja > j1) break;
-        int mask = mask_of(ja + off, jl + off, w0, w1, a.window, a.sinks);
-        if (jl < ja + H::ROWS - 1 && mask >= 0) mask = (mask & M_UPPER) || w0 < a.sinks ? M_ALL : M_LOWER;  // rows behind j1
+        int mask = M_NONE;
+        if (ja < clear0 || ja + H::ROWS - 1 > clear1) {
+          mask = mask_of(ja + off, jl + off, w0, w1, a.window, a.sinks);
+          if (jl < ja + H::ROWS - 1 && mask >= 0) mask = (mask & M_UPPER) || w0 < a.sinks ? M_ALL : M_LOWER;  // rows behind j1
+        }
         if (mask >= 0) products(mask, ja, qb + t * H::RB + at, qb + t * H::RB + att, &stats[place][0][t]);
       }
     }
@@ -545,7 +601,7 @@ template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wa
 }
 
 constexpr int kManyWaves = 4;
-template <typename T, int D> constexpr int key_tiles() { return D == 128 ? 1 : 2; }  // KN: registers
+template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }  // KN: registers
 
 // Ranges of a first tile's queries, each as long as two other tiles' at least; 0: there
 // are no sinks.
