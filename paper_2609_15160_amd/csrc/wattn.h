@@ -42,6 +42,12 @@ struct WSeq {
 // with more, scores are copied from and to registers that only products reach.
 template <typename T, int D> constexpr int kRoom = sizeof(T) == 4 && D == 128 ? 1 : 2;
 
+// Waves of a workgroup of the tile kernels.  One wave each, which would spread few rows
+// over more compute units, was slower at every size (12 x 64 heads, bf16, forward, dq and
+// dkv, us with four and with one: 4 x 200 rows 9, 10, 11 and 10, 10, 12; 8 x 800 26, 30,
+// 36 and 48, 46, 59; float32 4 x 200 21, 28, 36 and 21, 28, 35).
+constexpr int kTileWaves = 4;
+
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
 // Tiles of STEP rows: sequence b's begin at slot off[b] / STEP + b, which leaves

@@ -67,12 +67,12 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // of the rounded ones, a product with ones, saves an add for each weight (forward pass of
 // 8 x 4096 x 16 x 64, window 1024: 171 us) but is off by as much as a weight, and with
 // it every weight of the backward pass.
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
+template <typename T, int D>
+__global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
-  constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int NW = kTileWaves, QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NT = O::TILES;
   constexpr float kSumMax = 0x1p60f;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
@@ -537,8 +537,14 @@ WAttnArgs wattn_args(const tlf_attn_shape& t) {
 
 namespace {
 
-// Few rows: two for each sequence at most.
-bool is_few(const tlf_attn_shape& t) { return t.rows_q <= 2 * (int64_t)t.batch; }
+// One row for each sequence, or up to eight where the tile kernel would have fewer
+// workgroups than there are compute units (12 x 64 heads, us of this kernel and the tile
+// kernel: 256 sequences x 100 keys, 1 row each 17 and 22, 2 rows 30 and 23; 64 x 600, 1
+// row 26 and 25, 2 rows 38 and 25; 8 x 3000, 2 rows 23 and 64, 8 rows 52 and 64).
+bool is_few(const tlf_attn_shape& t) {
+  if (t.rows_q <= t.batch) return true;
+  return t.rows_q <= 8 * (int64_t)t.batch && slots_of<128>(t.rows_q, t.batch) * t.heads < 256;
+}
 
 // Ranges of the keys of a row, for four workgroups on a compute unit, and 256 keys of
 // a workgroup at least.
@@ -562,12 +568,7 @@ template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, WAttnArg
     return hipGetLastError();
   }
   a.slots = (int)slots_of<128>(t.rows_q, t.batch);
-  if ((int64_t)a.slots * t.heads >= 512) {
-    hipLaunchKernelGGL((k_wattn<T, D, 4>), dim3((unsigned)(a.slots * t.heads)), dim3(4 * kWave), 0, s, a);
-  } else {
-    a.slots = (int)slots_of<32>(t.rows_q, t.batch);
-    hipLaunchKernelGGL((k_wattn<T, D, 1>), dim3((unsigned)(a.slots * t.heads)), dim3(kWave), 0, s, a);
-  }
+  hipLaunchKernelGGL((k_wattn<T, D>), dim3((unsigned)(a.slots * t.heads)), dim3(kTileWaves * kWave), 0, s, a);
   return hipGetLastError();
 }
 

@@ -80,12 +80,12 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
 // Tiles, waves and LDS as the forward kernel's (k_wattn).  q and do of the wave's 32
 // queries stay in registers; a tile's keys are read as they lie and transposed, its
 // values as they lie.  dP starts from -delta, so dS = P dP takes one product.
-template <typename T, int D, int NW>
-__global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
+template <typename T, int D>
+__global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
-  constexpr int QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int NW = kTileWaves, QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
@@ -286,6 +286,9 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
   }
 }
 
+// Tiles of 16 keys that a wave's registers hold the sums of.
+template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }
+
 // One workgroup: a tile of NW * KN * 16 keys of one key head, whose rows stay in
 // registers (each wave KN tiles of 16), over tiles of BQ queries of every head that
 // shares them; q and do, with their lse and delta, which the products of the scores and of dP
@@ -293,12 +296,12 @@ __global__ __launch_bounds__(NW* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs 
 // A tile's keys are seen by the queries from its first position to the window's end
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
-template <typename T, int D, int NW, int KN>
-__global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
+template <typename T, int D>
+__global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
   using H = HeadRows<T, D>;
   using O = Opnd<T>;
   typedef typename O::frag Frag;
-  constexpr int KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 && D == 64 ? 64 : 32;
+  constexpr int NW = kTileWaves, KN = key_tiles<T, D>(), KW = 16 * KN, KT = NW * KW, BQ = sizeof(T) == 2 && D == 64 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, TL = O::TILES;
   using Loader = PairLoader<T, D, BQ, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
@@ -485,7 +488,7 @@ __global__ __launch_bounds__(NW* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 
       // 64 values each, of which the tile uses the first BQ
       const unsigned to = sbase + place * (unsigned)sizeof(stats[0]), lane4 = (unsigned)min(lane, most) * 4u;
       if (wave == 0) stage4(lp, lane4, to);
-      if (wave == (NW > 1 ? 1 : 0)) stage4(ep, lane4, to + (unsigned)sizeof(stats[0][0]));
+      if (wave == 1) stage4(ep, lane4, to + (unsigned)sizeof(stats[0][0]));
       ij += BQ;
       if (ij <= j1) {
         qp += BQ * a.qs;
@@ -600,9 +603,6 @@ template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wa
   }
 }
 
-constexpr int kManyWaves = 4;
-template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }  // KN: registers
-
 // Ranges of a first tile's queries, each as long as two other tiles' at least; 0: there
 // are no sinks.
 int sink_parts(const tlf_attn_shape& t) {
@@ -611,40 +611,30 @@ int sink_parts(const tlf_attn_shape& t) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(16, rows / other));
 }
 
-bool many_keys(const tlf_attn_shape& t) { return slots_of<128>(t.rows_k, t.batch) * t.kv_heads >= 512; }
-
 int64_t stat_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }
 int64_t part_floats(const tlf_attn_shape& t) {
-  const int parts = many_keys(t) ? sink_parts(t) : 0;
+  const int parts = sink_parts(t);
   return parts > 1 ? (int64_t)t.batch * t.kv_heads * parts * 128 * 2 * t.head_dim : 0;
-}
-
-template <typename T, int D, int NW> hipError_t launch_keys(const tlf_attn_shape& t, GradArgs a, hipStream_t s) {
-  constexpr int KN = key_tiles<T, D>(), KT = NW * KN * 16;
-  a.slots = (int)slots_of<KT>(t.rows_k, t.batch);
-  const int64_t sinks = (int64_t)a.batch * a.kv_heads * a.sink_parts;
-  hipLaunchKernelGGL((k_wattn_dkv<T, D, NW, KN>), dim3((unsigned)(sinks + (int64_t)a.slots * a.kv_heads)), dim3(NW * kWave), 0, s, a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.sink_parts <= 1) return e;
-  hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / 4))), dim3(256), 0, s, a);
-  return hipGetLastError();
 }
 
 template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, GradArgs a, hipStream_t s) {
   if (t.rows_q > 0) {
     a.slots = (int)slots_of<128>(t.rows_q, t.batch);
-    if ((int64_t)a.slots * t.heads >= 512) {
-      hipLaunchKernelGGL((k_wattn_dq<T, D, 4>), dim3((unsigned)(a.slots * t.heads)), dim3(4 * kWave), 0, s, a);
-    } else {
-      a.slots = (int)slots_of<32>(t.rows_q, t.batch);
-      hipLaunchKernelGGL((k_wattn_dq<T, D, 1>), dim3((unsigned)(a.slots * t.heads)), dim3(kWave), 0, s, a);
-    }
+    hipLaunchKernelGGL((k_wattn_dq<T, D>), dim3((unsigned)(a.slots * t.heads)), dim3(kTileWaves * kWave), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (t.rows_k == 0) return hipSuccess;
-  a.sink_parts = many_keys(t) ? sink_parts(t) : 0;
-  return many_keys(t) ? launch_keys<T, D, kManyWaves>(t, a, s) : launch_keys<T, D, 1>(t, a, s);
+  constexpr int KT = kTileWaves * key_tiles<T, D>() * 16;
+  static_assert(KT >= TLF_ATTN_MAX_SINKS, "sinks lie in a sequence's first tile");
+  a.slots = (int)slots_of<KT>(t.rows_k, t.batch);
+  a.sink_parts = sink_parts(t);
+  const int64_t blocks = ((int64_t)a.slots + (int64_t)a.batch * a.sink_parts) * a.kv_heads;
+  hipLaunchKernelGGL((k_wattn_dkv<T, D>), dim3((unsigned)blocks), dim3(kTileWaves * kWave), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.sink_parts <= 1) return e;
+  hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / 4))), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
