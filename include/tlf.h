@@ -539,6 +539,8 @@ int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, doubl
 #define TLF_ATTN_MAX_UNITS (1 << 29)     /* rows times heads */
 #define TLF_ATTN_MAX_SEQ_HEADS (1 << 22) /* sequences times heads */
 #define TLF_ATTN_MAX_STRIDE (1 << 21)
+#define TLF_ATTN_MIN_SCALE 1e-12f
+#define TLF_ATTN_MAX_SCALE 1e12f
 typedef struct tlf_attn_shape {
   int32_t dtype;     /* of q, k, v, o and their gradients: TLF_DTYPE_F32 or TLF_DTYPE_BF16 */
   int32_t batch;     /* sequences */
@@ -549,7 +551,7 @@ typedef struct tlf_attn_shape {
   int32_t rows_k;    /* rows of k and v */
   int32_t window;    /* 0: every earlier key is visible (sinks is then without effect) */
   int32_t sinks;
-  float scale;       /* > 0; 1 / sqrt(head_dim) usually */
+  float scale;       /* from TLF_ATTN_MIN_SCALE to TLF_ATTN_MAX_SCALE; 1 / sqrt(head_dim) usually */
   /* Elements between rows, multiples of 16 bytes; a row's heads lie one behind the
    * other.  do lies as o. */
   int64_t q_stride, k_stride, v_stride, o_stride;

@@ -59,11 +59,13 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // is used while the next arrives; one barrier a tile).
 //
 // The softmax base of a query is the largest score of the first tile that it sees a
-// key of: weights are exp2(s - base) at once, without a maximum per tile.  Where a
+// key of, or kLeast if that is less (its only key there may be one of little weight):
+// weights are exp2(s - base) at once, without a maximum per tile.  Where a
 // query's sum has grown past kSumMax the base moves up and the sums are scaled down,
 // exactly, by a power of two; o / l does not depend on it.  Weights that leave float32's
 // range within a tile (scores 127 above the base in base 2) make the row not finite, and
-// it is done again by slow_row.  The sum is of the weights before their rounding: the sum
+// sums less than kSumMin are of weights near its end (scores of -112 and less, all of
+// them): such a row is done again by slow_row.  The sum is of the weights before their rounding: the sum
 // of the rounded ones, a product with ones, saves an add for each weight (forward pass of
 // 8 x 4096 x 16 x 64, window 1024: 171 us) but is off by as much as a weight, and with
 // it every weight of the backward pass.
@@ -74,7 +76,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
   typedef typename O::frag Frag;
   constexpr int NW = kTileWaves, QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NT = O::TILES;
-  constexpr float kSumMax = 0x1p60f;
+  constexpr float kSumMax = 0x1p60f, kSumMin = 0x1p-80f, kLeast = -32.f;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
 
@@ -83,7 +85,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
   const WSeq s = load_seq(a, b);
   // a sequence's last tiles see the most keys and come first
   const int tile = (s.nq + BM - 1) / BM - 1 - (slot - slot_of<BM>(a.q_off, a.rows_q, b));
-  if (tile < 0) return;
+  if (tile < 0 || tile * BM >= s.nq) return;  // offsets that do not ascend may say either
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
   const int kvh = h / (a.heads / a.kv_heads), off = s.n - s.nq;
   const int p0 = tile * BM + off, p1 = min(tile * BM + BM, s.nq) - 1 + off;  // positions of the tile
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 #pragma unroll
           for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[qn][nt][r]);
         mx = ceilf(max_quads(mx) * a.scale_log2);  // whole numbers: moving it is exact too
-        if (base[qn] == -INFINITY) base[qn] = mx;
+        if (base[qn] == -INFINITY && mx != -INFINITY) base[qn] = fmaxf(mx, kLeast);
         none |= base[qn] == -INFINITY;
       }
       started = __builtin_amdgcn_ballot_w64(none) == 0;
@@ -263,7 +265,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
   for (int qn = 0; qn < QN; ++qn) {
     const int row = r0 + qn * 16 + c16;
     const float sum = sum_quads(ls[qn]), inv = p[qn] < 0 ? 0.f : 1.f / sum;
-    bool good = true;
+    bool good = p[qn] < 0 || sum >= kSumMin;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       o[dt][qn] *= inv;
@@ -324,7 +326,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   }
   const WSeq s = load_seq(a, b);
   const int p = row - s.q0 + s.n - s.nq;
-  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near), nv = s.n > 0 && p >= 0 ? sinks + p + 1 - near : 0;
+  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
+  const int nv = s.n > 0 && p >= 0 && (unsigned)(row - s.q0) < (unsigned)s.nq ? sinks + p + 1 - near : 0;
   const int per = ((nv + kFewKeys - 1) / kFewKeys + a.splits - 1) / a.splits * kFewKeys;
   const int xa = min(nv, split * per), xb = min(nv, xa + per);  // of the visible keys, sinks first
 
@@ -496,7 +499,7 @@ int wattn_check(const tlf_attn_shape* t) {
   if (!t) return TLF_E_INVALID_ARG;
   if (t->dtype != TLF_DTYPE_F32 && t->dtype != TLF_DTYPE_BF16) return TLF_E_INVALID_ARG;
   if (t->batch < 0 || t->rows_q < 0 || t->rows_k < 0 || t->heads < 1 || t->kv_heads < 1 || t->head_dim < 1 || t->window < 0 ||
-      t->sinks < 0 || t->heads % t->kv_heads != 0 || !(t->scale > 0.f) || !(t->scale < INFINITY))
+      t->sinks < 0 || t->heads % t->kv_heads != 0 || !(t->scale >= TLF_ATTN_MIN_SCALE) || !(t->scale <= TLF_ATTN_MAX_SCALE))
     return TLF_E_INVALID_ARG;
   const int64_t per = t->dtype == TLF_DTYPE_BF16 ? 8 : 4;  // elements of 16 bytes
   for (const int64_t v : {t->q_stride, t->k_stride, t->v_stride, t->o_stride})

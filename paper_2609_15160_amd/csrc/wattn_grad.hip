@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(G
   const int b = seq_of<BM>(a.q_off, a.rows_q, a.batch, slot);
   const WSeq s = load_seq(a, b);
   const int tile = (s.nq + BM - 1) / BM - 1 - (slot - slot_of<BM>(a.q_off, a.rows_q, b));
-  if (tile < 0) return;
+  if (tile < 0 || tile * BM >= s.nq) return;  // offsets that do not ascend may say either
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
   const int kvh = h / (a.heads / a.kv_heads), off = s.n - s.nq;
   const int p0 = tile * BM + off, p1 = min(tile * BM + BM, s.nq) - 1 + off;
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(G
 template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }
 
 // One workgroup: a tile of NW * KN * 16 keys of one key head, whose rows stay in
-// registers (each wave KN tiles of 16), over tiles of BQ queries of every head that
+// registers (each wave KN tiles of 16; the values of 128-wide bf16 heads in LDS), over tiles of BQ queries of every head that
 // shares them; q and do, with their lse and delta, which the products of the scores and of dP
 // start from, come through two places in LDS.
 // A tile's keys are seen by the queries from its first position to the window's end
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 
     b = seq_of<KT>(a.k_off, a.rows_k, a.batch, slot);
     s = load_seq(a, b);
     tile = slot - slot_of<KT>(a.k_off, a.rows_k, b);
-    if (tile * KT >= s.cap || (tile == 0 && sink_blocks > 0 && s.n > 0)) return;
+    if (tile < 0 || tile * KT >= s.cap || (tile == 0 && sink_blocks > 0 && s.n > 0)) return;
   }
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
   const int each = a.heads / a.kv_heads, off = s.n - s.nq;
@@ -570,36 +570,40 @@ __global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 
   }
 }
 
-// The first tiles' sums over the ranges of their queries: a wave per key.
+// The first tiles' sums over the ranges of their queries: a wave per key, four in turn
+// (a workgroup for every four keys would pass 2^32 threads at 2^19 sequences' heads).
+constexpr int kSinkKeys = 16;  // of a workgroup
 template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wattn_sinks(GradArgs a) {
-  constexpr int N = (2 * D + kWave - 1) / kWave;
-  const int unit = blockIdx.x / (KT / 4), key = (blockIdx.x % (KT / 4)) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int b = unit / a.kv_heads, kvh = unit % a.kv_heads, lane = lane_id();
+  constexpr int N = (2 * D + kWave - 1) / kWave, BLOCKS = KT / kSinkKeys;
+  const int unit = blockIdx.x / BLOCKS, b = unit / a.kv_heads, kvh = unit % a.kv_heads, lane = lane_id();
   const WSeq s = load_seq(a, b);
-  if (s.n == 0 || key >= s.cap) return;  // without keys the tile's own workgroup has written its zeros
-  T* dk = reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D;
-  T* dv = reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D;
-  const float* src = a.part + (int64_t)unit * a.sink_parts * KT * 2 * D + key * 2 * D;
-  float t[N];
-  bool good = true;
+  if (s.n == 0) return;  // the tile's own workgroup has written its zeros
+  const int key0 = blockIdx.x % BLOCKS * kSinkKeys, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  for (int key = key0 + wave; key < min(key0 + kSinkKeys, s.cap); key += 256 / kWave) {
+    T* dk = reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D;
+    T* dv = reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D;
+    const float* src = a.part + (int64_t)unit * a.sink_parts * KT * 2 * D + key * 2 * D;
+    float t[N];
+    bool good = true;
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int d = e * kWave + lane;
-    t[e] = 0.f;
-    if (d < 2 * D && key < s.n)
-      for (int k = 0; k < a.sink_parts; ++k) t[e] += src[(int64_t)k * KT * 2 * D + d];
-    if (d < D) t[e] *= a.scale;
-    good &= finite1(t[e]);
-  }
-  if (__builtin_amdgcn_ballot_w64(!good)) {
-    slow_dkv<T, D>(a, s, kvh, key);
-    return;
-  }
+    for (int e = 0; e < N; ++e) {
+      const int d = e * kWave + lane;
+      t[e] = 0.f;
+      if (d < 2 * D && key < s.n)
+        for (int k = 0; k < a.sink_parts; ++k) t[e] += src[(int64_t)k * KT * 2 * D + d];
+      if (d < D) t[e] *= a.scale;
+      good &= finite1(t[e]);
+    }
+    if (__builtin_amdgcn_ballot_w64(!good)) {
+      slow_dkv<T, D>(a, s, kvh, key);
+      continue;
+    }
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    const int d = e * kWave + lane;
-    if (d < D) dk[d] = from_f<T>(t[e]);
-    else if (d < 2 * D) dv[d - D] = from_f<T>(t[e]);
+    for (int e = 0; e < N; ++e) {
+      const int d = e * kWave + lane;
+      if (d < D) dk[d] = from_f<T>(t[e]);
+      else if (d < 2 * D) dv[d - D] = from_f<T>(t[e]);
+    }
   }
 }
 
@@ -633,7 +637,7 @@ template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, GradArgs
   hipLaunchKernelGGL((k_wattn_dkv<T, D>), dim3((unsigned)blocks), dim3(kTileWaves * kWave), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.sink_parts <= 1) return e;
-  hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / 4))), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_wattn_sinks<T, D, KT>), dim3((unsigned)((int64_t)a.batch * a.kv_heads * (KT / kSinkKeys))), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -788,8 +788,8 @@ class AdamW:
 
     @torch.no_grad()
     def step(self, max_norm: float = None):
-        """One step; with max_norm the gradients count times grad_norm's scale (they are left as they are), and their
-        norm is returned: a float32 value on the device, None without gradients."""
+        """One step; with max_norm the gradients, all on one device, count times grad_norm's scale (they are left as they
+        are), and their norm is returned: a float32 value on the device, None without gradients."""
         have = [k for k, p in enumerate(self.params) if p.grad is not None]
         grads = {k: self.params[k].grad.contiguous() for k in have}
         norm = scale = None

@@ -200,6 +200,32 @@ def test_sharp_and_growing_scores(dtype, D):
     _within(o, r["o"], bounds(_np(q), _np(k), _np(v), r, 250, 2, D ** -0.5, dtype)["o"], "o")
 
 
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("scores", ["low", "lower", "lowest", "low first", "lowest first", "high first"])
+def test_scores_far_from_zero(dtype, D, nq, scores):
+    """Weights relative to any fixed base would leave float32's range, or reach its subnormal end."""
+    train = _train()
+    rng = np.random.default_rng(5)
+    n = 200
+    q = _normal(rng, nq, 1, D, std=0.1, dtype=dtype)
+    k, v = (_normal(rng, n, 1, D, std=s, dtype=dtype) for s in (0.1, 1.0))
+    do = _normal(rng, nq, 1, D, dtype=dtype)
+    rest = {"low": -95.0, "lower": -110.0, "lowest": -900.0}.get(scores, 10.0)
+    first = {"low first": -70.0, "lowest first": -1e4, "high first": 200.0}.get(scores, rest)
+    q[:, 0, 0], k[:, 0, 0] = 8.0, rest / 8
+    k[torch.arange(0, n, 50), 0, 0] = first / 8  # the first keys of several windows too
+    for window, sinks in ((None, 0), (51, 0), (30, 3)):
+        leaves = [t.detach().clone().requires_grad_() for t in (q, k, v)]
+        o = train.attention(*leaves, _offsets([nq]), _offsets([n]), window=window, sinks=sinks, scale=1.0)
+        got = dict(zip(("o", "dq", "dk", "dv"), (o, *torch.autograd.grad(o, leaves, do))))
+        arrays = [_np(t) for t in (q, k, v)]
+        r = O.attention(*arrays, window, sinks, 1.0, _np(do))
+        lim = bounds(*arrays, r, window, sinks, 1.0, dtype, _np(do))
+        for name in got:
+            _within(got[name], r[name], lim[name], (name, window))
+
+
 # ---------------------------------------------------------------------------
 # What is not seen takes no part, whatever its values; layouts, streams, order
 # ---------------------------------------------------------------------------

@@ -32,7 +32,7 @@ def _shape(**kw):
 SHAPES = [
     (dict(dtype=2), BAD), (dict(batch=-1), BAD), (dict(rows_q=-1), BAD), (dict(rows_k=-1), BAD), (dict(heads=0), BAD),
     (dict(kv_heads=0), BAD), (dict(kv_heads=3), BAD), (dict(head_dim=0), BAD), (dict(window=-1), BAD), (dict(sinks=-1), BAD),
-    (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=math.nan), BAD), (dict(scale=math.inf), BAD),
+    (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=math.nan), BAD), (dict(scale=math.inf), BAD), (dict(scale=1e-13), BAD), (dict(scale=1.1e12), BAD),
     (dict(q_stride=252), BAD), (dict(q_stride=248), BAD), (dict(k_stride=120), BAD), (dict(v_stride=-128), BAD),
     (dict(o_stride=0), BAD), (dict(d_q_offsets=None), BAD), (dict(d_k_offsets=None), BAD), (dict(head_dim=32), UNS),
     (dict(head_dim=16), UNS), (dict(sinks=65), UNS), (dict(q_stride=(1 << 21) + 8), UNS), (dict(rows_q=1 << 30), UNS),
