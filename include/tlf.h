@@ -563,12 +563,16 @@ typedef struct tlf_attn_shape {
 
 /*   d_lse  [heads][rows_q] float32, receives log2 of each softmax sum, base
  *          included (tlf_attn_grad reads it; +inf where nothing is visible), or NULL.
+ *   d_o_low [rows_q] rows as o's, bf16 tensors only: receives what o lost where it was
+ *          rounded (tlf_attn_grad reads it: without it the gradients of rows that few
+ *          keys have most of the weight of are less exact), or NULL.
  *   d_workspace: tlf_attn_ws_bytes bytes (may be 0), used during the call only. */
 int tlf_attn_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes);
 int tlf_attn(const tlf_attn_shape* shape, const void* d_q, const void* d_k, const void* d_v, void* d_o, float* d_lse,
-             void* d_workspace, size_t ws_bytes, void* stream);
+             void* d_o_low, void* d_workspace, size_t ws_bytes, void* stream);
 
-/* Gradients of tlf_attn from its inputs, its o and the lse that it wrote:
+/* Gradients of tlf_attn from its inputs, its o and the lse and o_low (or NULL) that it
+ * wrote:
  *   P = exp2(log2(e) scale q . k - lse),  dS = P (do . v - do . o),
  *   dq = scale dS k,  dk = scale dS^T q,  dv = P^T do
  * with sums over the queries and over the heads that share a key head.  P and dS
@@ -576,8 +580,8 @@ int tlf_attn(const tlf_attn_shape* shape, const void* d_q, const void* d_k, cons
  * every row of them; their strides are elements between rows. */
 int tlf_attn_grad_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes);
 int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q, const void* d_k, const void* d_v,
-                  const void* d_o, const float* d_lse, void* d_dq, int64_t dq_stride, void* d_dk, int64_t dk_stride,
-                  void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream);
+                  const void* d_o, const float* d_lse, const void* d_o_low, void* d_dq, int64_t dq_stride, void* d_dk,
+                  int64_t dk_stride, void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream);
 
 /* The gated residual of the block with the norm that follows (Section 3.1,
  * Appendix A: x + (1 + alpha) F, then the next operand's norm), in one pass:

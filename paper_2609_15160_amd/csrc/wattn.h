@@ -22,6 +22,7 @@ namespace tlf {
 struct WAttnArgs {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
+  void* low;                        // [rows_q] as o: what its rounding took, or NULL
   float* lse;                       // [heads][rows_q]: log2 of the softmax sums
   float *nlse, *ndelta;             // [heads][rows_q]: -lse in units of q . k, -o . do
   float* part;
@@ -114,6 +115,8 @@ template <> struct Opnd<bf16> {
   static __device__ __forceinline__ f32x4 mma(frag a, frag b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
+  static __device__ __forceinline__ frag ones() { return __builtin_bit_cast(frag, make_uint4(kOnes, kOnes, kOnes, kOnes)); }
+  static constexpr unsigned kOnes = 0x3F803F80u;
   static __device__ __forceinline__ frag pack(const f32x4* s) {  // the rows of two score tiles
     return __builtin_bit_cast(frag, make_uint4(pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]),
                                                pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])));
@@ -262,6 +265,12 @@ __device__ __forceinline__ float sum_wave(float v) {
   return v;
 }
 
+// What rounding to T takes from v.
+template <typename T> __device__ __forceinline__ float lost(float v) { return v - to_f<T>(from_f<T>(v)); }
+template <typename T> __device__ __forceinline__ f32x4 lost4(f32x4 v) {
+  return f32x4{lost<T>(v[0]), lost<T>(v[1]), lost<T>(v[2]), lost<T>(v[3])};
+}
+
 // By the bits: a difference v - v may be fused with the product that v comes from.
 __device__ __forceinline__ bool finite1(float v) { return (__float_as_uint(v) & 0x7FFFFFFFu) < 0x7F800000u; }
 __device__ __forceinline__ bool finite4(f32x4 v) { return finite1(v[0]) && finite1(v[1]) && finite1(v[2]) && finite1(v[3]); }
@@ -286,6 +295,13 @@ template <typename T, int D> struct LaneRow {
     for (int e = 0; e < N; ++e) {
       const int d = e * kWave + lane_id();
       if (d < D) p[d] = from_f<T>(v[e] * f);
+    }
+  }
+  __device__ __forceinline__ void store_lost(T* p, float f) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int d = e * kWave + lane_id();
+      if (d < D) p[d] = from_f<T>(lost<T>(v[e] * f));
     }
   }
   __device__ __forceinline__ void add(float f, const LaneRow& o) {

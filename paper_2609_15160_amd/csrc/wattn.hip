@@ -4,9 +4,14 @@
 //   s = scale q . k,  o = sum over the visible keys of exp(s - m) v / sum of exp(s - m)
 //
 // Scores, softmax statistics and sums are float32; the weights exp(s - m) are
-// rounded to bf16 as operands of the product with bf16 values (each by 2^-9 of
-// itself at most, which the sum over keys averages; the sum that divides is of the
-// weights before that).
+// rounded to bf16 as operands of the product with bf16 values (each by 2^-8 of
+// itself at most, which the sum over keys averages).  The sum that divides o is of the
+// rounded weights, so that o stays a mean of values (error against 64 bits, causal
+// over 300 keys with scores of variance 16: 0.0018, with the unrounded sum 0.0023); the
+// lse, which the gradients' weights are of, has the sum before the rounding.
+// What o loses where it is rounded is kept beside it for the gradients: their delta =
+// do . o is subtracted from numbers that are nearly equal to it where few keys have
+// most of the weight (gradients' error there 0.0025, from o alone 0.0033).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -51,6 +56,7 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
     if (o.all_nan()) break;
   }
   o.store(reinterpret_cast<T*>(a.out) + (int64_t)(s.q0 + row) * a.os + h * D, 1.f / l);
+  if (a.low) o.store_lost(reinterpret_cast<T*>(a.low) + (int64_t)(s.q0 + row) * a.os + h * D, 1.f / l);
   if (a.lse && lane_id() == 0) a.lse[(int64_t)h * a.rows_q + s.q0 + row] = m + log2f(l);
 }
 
@@ -65,10 +71,8 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // exactly, by a power of two; o / l does not depend on it.  Weights that leave float32's
 // range within a tile (scores 127 above the base in base 2) make the row not finite, and
 // sums less than kSumMin are of weights near its end (scores of -112 and less, all of
-// them): such a row is done again by slow_row.  The sum is of the weights before their rounding: the sum
-// of the rounded ones, a product with ones, saves an add for each weight (forward pass of
-// 8 x 4096 x 16 x 64, window 1024: 171 us) but is off by as much as a weight, and with
-// it every weight of the backward pass.
+// them): such a row is done again by slow_row.  The sum of the rounded weights is a
+// product with ones.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
   using H = HeadRows<T, D>;
@@ -76,6 +80,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
   typedef typename O::frag Frag;
   constexpr int NW = kTileWaves, QN = 2, QW = 16 * QN, BM = NW * QW, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, NT = O::TILES;
+  constexpr bool kRounds = sizeof(T) == 2;
   constexpr float kSumMax = 0x1p60f, kSumMin = 0x1p-80f, kLeast = -32.f;
   using Loader = PairLoader<T, D, BN, NW * kWave>;
   __shared__ __align__(1024) char lds[2 * Loader::BYTES];
@@ -110,10 +115,12 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
   const unsigned at = H::direct(lane), att = H::transposed(lane);
   f32x4 o[DT][QN];
   float ls[QN], base[QN];  // this lane's part of the sum of weights; the base, -inf: none yet
+  f32x4 lr[QN];            // the sum of the rounded weights, in each row
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
     base[qn] = -INFINITY;
     ls[qn] = 0.f;
+    lr[qn] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt][qn] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -193,7 +200,10 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
     }
     Frag pf[QN];
 #pragma unroll
-    for (int qn = 0; qn < QN; ++qn) pf[qn] = O::pack(sc[qn]);
+    for (int qn = 0; qn < QN; ++qn) {
+      pf[qn] = O::pack(sc[qn]);
+      if constexpr (kRounds) lr[qn] = O::mma(O::ones(), pf[qn], lr[qn]);
+    }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -211,6 +221,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
       const float f = __uint_as_float((unsigned)(127 - up) << 23);  // 2^-up
       base[qn] += (float)up;
       ls[qn] *= f;
+      lr[qn] *= f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt][qn] *= f;
     }
@@ -264,7 +275,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
     const int row = r0 + qn * 16 + c16;
-    const float sum = sum_quads(ls[qn]), inv = p[qn] < 0 ? 0.f : 1.f / sum;
+    const float sum = sum_quads(ls[qn]), inv = p[qn] < 0 ? 0.f : 1.f / (kRounds ? lr[qn][0] : sum);
     bool good = p[qn] < 0 || sum >= kSumMin;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -279,6 +290,12 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
       if constexpr (DT >= 2) {
 #pragma unroll
         for (int dt = 0; dt < DT; dt += 2) store_pair<T>(dst + dt * 16, o[dt][qn], o[dt + 1][qn], lane);
+        if constexpr (kRounds) {
+          T* low = reinterpret_cast<T*>(a.low) + (int64_t)(s.q0 + row) * a.os + h * D;
+          if (a.low)
+#pragma unroll
+            for (int dt = 0; dt < DT; dt += 2) store_pair<T>(low + dt * 16, lost4<T>(o[dt][qn]), lost4<T>(o[dt + 1][qn]), lane);
+        }
       } else {
         Vec4<T>::store(dst + g * 4, o[0][qn]);
       }
@@ -296,7 +313,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 // one is used.  Bound by HBM: every visible key and value is read once.
 constexpr int kFewWaves = 4, kFewKeys = 32;
 template <typename T, int D> struct FewPart {  // sums of one head over a range
-  static constexpr int FLOATS = D + 4;         // o, then m, l, the row's visible keys
+  static constexpr int FLOATS = D + 4;         // o, then m, l, the row's visible keys, l of the rounded weights
 };
 
 template <typename T, int D>
@@ -305,7 +322,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   using O = Opnd<T>;
   typedef typename O::frag Frag;
   constexpr int KSTEPS = H::KSTEPS, DT = H::DT, VN = kFewKeys * H::CPR / kWave, NT = kFewKeys / 16;
-  constexpr int SUMS = kFewWaves * 16 * (D + 2) * 4, ROWS = kFewWaves * kFewKeys * H::RB;
+  constexpr int SUMS = kFewWaves * 16 * (D + 3) * 4, ROWS = kFewWaves * kFewKeys * H::RB;
   __shared__ __align__(1024) char lds[SUMS > ROWS ? SUMS : ROWS];
   const int each = a.heads / a.kv_heads, chunks = (each + 15) / 16;
   const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
@@ -361,6 +378,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  f32x4 lr = f32x4{0.f, 0.f, 0.f, 0.f};  // of the rounded weights, in each row
   constexpr int TURN = kFewWaves * kFewKeys;
   int x = xa + wave * kFewKeys;
   if (x < xb) load(x);
@@ -389,10 +407,11 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
         if (x + t * 16 + 4 * g + r >= xb) sc[t][r] = -INFINITY;
         mx = fmaxf(mx, sc[t][r]);
       }
-    mx = fmaxf(m, max_quads(mx) * a.scale_log2);
+    mx = fmaxf(m, ceilf(max_quads(mx) * a.scale_log2));  // whole numbers: the sums are scaled exactly
     const float base = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(m - base);
     m = mx;
     l *= alpha;
+    lr *= alpha;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) o[dt] *= alpha;
 #pragma unroll
@@ -405,6 +424,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
 #pragma unroll
     for (int t = 0; t < NT / O::TILES; ++t) {
       const Frag pf = O::pack(&sc[t * O::TILES]);
+      if constexpr (sizeof(T) == 2) lr = O::mma(O::ones(), pf, lr);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[dt] = O::mma(H::load_t(H::tile(att, dt), t * H::ROWS), pf, o[dt]);
     }
@@ -412,19 +432,20 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   }
   l = sum_quads(l);
   __syncthreads();
-  float* os = reinterpret_cast<float*>(lds);  // [wave][column][D], then [wave][column] of m and of l
-  float *ms = os + kFewWaves * 16 * D, *ls = ms + kFewWaves * 16;
+  float* os = reinterpret_cast<float*>(lds);  // [wave][column][D], then [wave][column] of m, of l and of lr
+  float *ms = os + kFewWaves * 16 * D, *ls = ms + kFewWaves * 16, *rs = ls + kFewWaves * 16;
   float* dst = os + (wave * 16 + c16) * D + 4 * g;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) Vec4<float>::store(dst + dt * 16, o[dt]);
   if (g == 0) {
     ms[wave * 16 + c16] = m;
     ls[wave * 16 + c16] = l;
+    rs[wave * 16 + c16] = sizeof(T) == 2 ? lr[0] : l;
   }
   __syncthreads();
   for (int e = threadIdx.x; e < cols * D; e += kFewWaves * kWave) {
     const int c = e / D, d = e % D;
-    float top = -INFINITY, sum = 0.f, t = 0.f;
+    float top = -INFINITY, sum = 0.f, sumr = 0.f, t = 0.f;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, ms[w * 16 + c]);
     const float base = top == -INFINITY ? 0.f : top;  // no key of the range, or none with a score
@@ -432,6 +453,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
     for (int w = 0; w < kFewWaves; ++w) {
       const float f = __builtin_amdgcn_exp2f(ms[w * 16 + c] - base);
       sum += f * ls[w * 16 + c];
+      sumr += f * rs[w * 16 + c];
       t += f * os[(w * 16 + c) * D + d];
     }
     if (a.splits > 1) {
@@ -441,11 +463,14 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
         part[D] = top;
         part[D + 1] = sum;
         part[D + 2] = __uint_as_float((unsigned)nv);
+        part[D + 3] = sumr;
       }
       continue;
     }
     // without a visible key zeros; visible keys of which none has a score are 0 / 0
-    reinterpret_cast<T*>(a.out)[(int64_t)row * a.os + (h0 + c) * D + d] = from_f<T>(nv == 0 ? 0.f : t / sum);
+    const float o = nv == 0 ? 0.f : t / sumr;
+    reinterpret_cast<T*>(a.out)[(int64_t)row * a.os + (h0 + c) * D + d] = from_f<T>(o);
+    if (a.low) reinterpret_cast<T*>(a.low)[(int64_t)row * a.os + (h0 + c) * D + d] = from_f<T>(lost<T>(o));
     if (a.lse && d == 0) a.lse[(int64_t)(h0 + c) * a.rows_q + row] = nv == 0 ? INFINITY : top + log2f(sum);
   }
 }
@@ -469,27 +494,34 @@ template <typename T, int D> __global__ __launch_bounds__(kJoinThreads) void k_w
 #pragma unroll
   for (int w = 0; w < kJoinThreads / kWave; ++w) top = fmaxf(top, tops[w]);
   const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
+  float sum = 0.f, sumr = 0.f;
   f32x4 t = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int k = set; k < a.splits; k += SETS) {
     const float* s = part + (int64_t)k * F;
     const float f = __builtin_amdgcn_exp2f(s[D] - base);
     sum += f * s[D + 1];
+    sumr += f * s[D + 3];
     t += f * Vec4<float>::load(s + d);
   }
   Vec4<float>::store(&sums[set][d], t);
-  if (d == 0) sums[set][D] = sum;
+  if (d == 0) {
+    sums[set][D] = sum;
+    sums[set][D + 1] = sumr;
+  }
   __syncthreads();
   if (threadIdx.x >= D) return;
-  float all = 0.f, l = 0.f;
+  float all = 0.f, l = 0.f, lr = 0.f;
   for (int k = 0; k < SETS; ++k) {
     all += sums[k][threadIdx.x];
     l += sums[k][D];
+    lr += sums[k][D + 1];
   }
   // whether the row has visible keys at all, as k_wattn_few found
   const bool none = __float_as_uint(part[D + 2]) == 0u;
-  reinterpret_cast<T*>(a.out)[(int64_t)row * a.os + h * D + threadIdx.x] = from_f<T>(none ? 0.f : all / l);
+  const float o = none ? 0.f : all / lr;
+  reinterpret_cast<T*>(a.out)[(int64_t)row * a.os + h * D + threadIdx.x] = from_f<T>(o);
+  if (a.low) reinterpret_cast<T*>(a.low)[(int64_t)row * a.os + h * D + threadIdx.x] = from_f<T>(lost<T>(o));
   if (a.lse && threadIdx.x == 0) a.lse[(int64_t)h * a.rows_q + row] = none ? INFINITY : top + log2f(l);
 }
 
@@ -590,14 +622,15 @@ int tlf_attn_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes) {
 }
 
 int tlf_attn(const tlf_attn_shape* shape, const void* d_q, const void* d_k, const void* d_v, void* d_o, float* d_lse,
-             void* d_workspace, size_t ws_bytes, void* stream) {
+             void* d_o_low, void* d_workspace, size_t ws_bytes, void* stream) {
   size_t need = 0;
   const int st = tlf_attn_ws_bytes(shape, &need);
   if (st != TLF_OK) return st;
+  if (d_o_low && shape->dtype != TLF_DTYPE_BF16) return TLF_E_INVALID_ARG;
   if (shape->rows_q == 0) return TLF_OK;
   if (!d_q || !d_o || (shape->rows_k > 0 && (!d_k || !d_v)) || (need > 0 && (!d_workspace || ws_bytes < need)))
     return TLF_E_INVALID_ARG;
-  for (const void* p : {d_q, d_k, d_v, (const void*)d_o, (const void*)d_workspace})
+  for (const void* p : {d_q, d_k, d_v, (const void*)d_o, (const void*)d_o_low, (const void*)d_workspace})
     if (((uintptr_t)p & 15u) != 0) return TLF_E_INVALID_ARG;
   for (const void* p : {(const void*)d_lse, (const void*)shape->d_q_offsets, (const void*)shape->d_k_offsets, (const void*)shape->d_k_lengths})
     if (((uintptr_t)p & 3u) != 0) return TLF_E_INVALID_ARG;
@@ -607,6 +640,7 @@ int tlf_attn(const tlf_attn_shape* shape, const void* d_q, const void* d_k, cons
   a.v = d_v;
   a.out = d_o;
   a.lse = d_lse;
+  a.low = d_o_low;
   a.part = (float*)d_workspace;
   const hipStream_t s = (hipStream_t)stream;
   const bool h = shape->dtype == TLF_DTYPE_BF16;

@@ -40,7 +40,12 @@ __device__ __forceinline__ void slow_dq(const GradArgs& a, const WSeq& s, int h,
   q.load(reinterpret_cast<const T*>(a.q) + (int64_t)(s.q0 + row) * a.qs + h * D);
   d.load(reinterpret_cast<const T*>(a.dout) + (int64_t)(s.q0 + row) * a.os + h * D);
   x.load(reinterpret_cast<const T*>(a.o) + (int64_t)(s.q0 + row) * a.os + h * D);
-  const float delta = d.dot(x), lse = a.lse[(int64_t)h * a.rows_q + s.q0 + row];
+  float delta = d.dot(x);
+  if (a.low) {
+    x.load(reinterpret_cast<const T*>(a.low) + (int64_t)(s.q0 + row) * a.os + h * D);
+    delta += d.dot(x);
+  }
+  const float lse = a.lse[(int64_t)h * a.rows_q + s.q0 + row];
   o.zero();
   const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
   for (int i = 0; i < sinks + p + 1 - near; ++i) {
@@ -79,7 +84,7 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
 
 // Tiles, waves and LDS as the forward kernel's (k_wattn).  q and do of the wave's 32
 // queries stay in registers; a tile's keys are read as they lie and transposed, its
-// values as they lie.  dP starts from -delta, so dS = P dP takes one product.
+// values as they lie.  delta is of o with what its rounding took.  dP starts from -delta, so dS = P dP takes one product.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
   using H = HeadRows<T, D>;
@@ -113,7 +118,8 @@ __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(G
     const T* q = reinterpret_cast<const T*>(a.q) + at * a.qs + wide;
     const T* d = reinterpret_cast<const T*>(a.dout) + at * a.os + wide;
     const T* o = reinterpret_cast<const T*>(a.o) + at * a.os + wide;
-    float t = 0.f;
+    const T* low = reinterpret_cast<const T*>(a.low ? a.low : a.o) + at * a.os + wide;
+    float t = 0.f, tl = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) {
       qf[qn][ks] = *reinterpret_cast<const Frag*>(q + ks * 4 * H::EPC);
@@ -121,8 +127,13 @@ __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(G
       const Frag of = *reinterpret_cast<const Frag*>(o + ks * 4 * H::EPC);
 #pragma unroll
       for (int e = 0; e < H::EPC; ++e) t = fmaf((float)df[qn][ks][e], (float)of[e], t);
+      if constexpr (sizeof(T) == 2) {  // read in any case: behind a branch it would be one more trip to memory
+        const Frag lf = *reinterpret_cast<const Frag*>(low + ks * 4 * H::EPC);
+#pragma unroll
+        for (int e = 0; e < H::EPC; ++e) tl = fmaf((float)df[qn][ks][e], (float)lf[e], tl);
+      }
     }
-    delta[qn] = sum_quads(t);
+    delta[qn] = sum_quads(a.low ? t + tl : t);
     lse[qn] = a.lse[(int64_t)h * a.rows_q + at];
     if (g == 0 && r0 + qn * 16 + c16 < s.nq) {  // for k_wattn_dkv, whose products start from them
       a.ndelta[(int64_t)h * a.rows_q + at] = -delta[qn];
@@ -655,8 +666,8 @@ int tlf_attn_grad_ws_bytes(const tlf_attn_shape* shape, size_t* ws_bytes) {
 }
 
 int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q, const void* d_k, const void* d_v,
-                  const void* d_o, const float* d_lse, void* d_dq, int64_t dq_stride, void* d_dk, int64_t dk_stride,
-                  void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream) {
+                  const void* d_o, const float* d_lse, const void* d_o_low, void* d_dq, int64_t dq_stride, void* d_dk,
+                  int64_t dk_stride, void* d_dv, int64_t dv_stride, void* d_workspace, size_t ws_bytes, void* stream) {
   size_t need = 0;
   const int st = tlf_attn_grad_ws_bytes(shape, &need);
   if (st != TLF_OK) return st;
@@ -667,8 +678,9 @@ int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q
   if (std::max({dq_stride, dk_stride, dv_stride}) > TLF_ATTN_MAX_STRIDE) return TLF_E_UNSUPPORTED;
   if (shape->rows_q > 0 && (!d_do || !d_q || !d_o || !d_lse || !d_dq)) return TLF_E_INVALID_ARG;
   if (shape->rows_k > 0 && (!d_k || !d_v || !d_dk || !d_dv)) return TLF_E_INVALID_ARG;
+  if (d_o_low && shape->dtype != TLF_DTYPE_BF16) return TLF_E_INVALID_ARG;
   if (need > 0 && (!d_workspace || ws_bytes < need)) return TLF_E_INVALID_ARG;
-  for (const void* p : {d_do, d_q, d_k, d_v, d_o, (const void*)d_dq, (const void*)d_dk, (const void*)d_dv, (const void*)d_workspace})
+  for (const void* p : {d_do, d_q, d_k, d_v, d_o, d_o_low, (const void*)d_dq, (const void*)d_dk, (const void*)d_dv, (const void*)d_workspace})
     if (((uintptr_t)p & 15u) != 0) return TLF_E_INVALID_ARG;
   for (const void* p : {(const void*)d_lse, (const void*)shape->d_q_offsets, (const void*)shape->d_k_offsets, (const void*)shape->d_k_lengths})
     if (((uintptr_t)p & 3u) != 0) return TLF_E_INVALID_ARG;
@@ -680,6 +692,7 @@ int tlf_attn_grad(const tlf_attn_shape* shape, const void* d_do, const void* d_q
   a.o = d_o;
   a.dout = d_do;
   a.lse = const_cast<float*>(d_lse);
+  a.low = const_cast<void*>(d_o_low);
   a.dq = d_dq;
   a.dk = d_dk;
   a.dv = d_dv;

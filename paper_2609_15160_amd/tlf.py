@@ -217,9 +217,9 @@ def load(path: str = LIB_PATH):
     lib.tlf_adamw.argtypes = [ctypes.POINTER(AdamwTensor), i32, f64, f64, f64, f64, vp]
     shape, i64 = ctypes.POINTER(AttnShape), ctypes.c_int64
     lib.tlf_attn_ws_bytes.argtypes = [shape, psz]
-    lib.tlf_attn.argtypes = [shape, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tlf_attn.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.tlf_attn_grad_ws_bytes.argtypes = [shape, psz]
-    lib.tlf_attn_grad.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
+    lib.tlf_attn_grad.argtypes = [shape, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     lib.tlf_residual_norm.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp, vp, vp]
     lib.tlf_residual_norm_grad_ws_bytes.argtypes = [i32, i32, i32, psz]
     lib.tlf_residual_norm_grad.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp,

@@ -3,16 +3,22 @@ straight-through estimator (Appendix B) as autograd functions over libtlf.
 
 Argument marshalling only: the active set, the gather, the scatter, their
 gradients and the estimator all run in libtlf's HIP kernels, on the current
-torch stream.  The attention half of the block is the caller's.
+torch stream.
 
     p = plan(depth, batch, seq_len, loop)     # loop i's active rows
     x = gather(h, p)                          # [p.count, d], Eq. 6
     h = scatter(h, block(x), p)               # Eq. 7 (scatter_ writes into h)
 
-Of the block, the FFN half is here: rms_norm (with the AdaLN scale of each row's
-group), ffn, and the optimizer's step, adamw_ and AdamW.
+Of the block, all but its projections (torch.nn.functional.linear) is here: rms_norm
+(with the AdaLN scale of each row's group), self_attention among the gathered rows
+(Eq. 10; with a sliding window and sinks if asked), residual_norm (the gated residual
+and the next norm in one pass), ffn, and the optimizer's step: adamw_ and AdamW, and
+grad_norm and clip_grad_norm_.
 
-    y = ffn(rms_norm(x, gamma, group, dtype=torch.bfloat16), w_gate_up, w_down)
+    z = rms_norm(x, gamma_msa, group, dtype=torch.bfloat16)
+    a = self_attention(linear(z, w_qkv), p.offsets, heads)
+    x, z = residual_norm(x, linear(a, w_o), alpha_msa, gamma_mlp, group)
+    x, z = residual_norm(x, ffn(z, w_gate_up, w_down), alpha_mlp, next_gamma_msa, group)
 """
 from __future__ import annotations
 
@@ -214,9 +220,10 @@ def ste(score: torch.Tensor, depth: torch.Tensor) -> torch.Tensor:
 # ---------------------------------------------------------------------------
 # The block's FFN half: RMSNorm, the gated FFN, and the optimizer's step
 #
-# rms_norm and ffn may be captured into a graph, their backward pass with them if
-# no graph from before the capture holds the same leaves: autograd runs a leaf's
-# gradient on the stream where the leaf was first used.
+# rms_norm, ffn, residual_norm and the attention may be captured into a graph, their
+# backward pass with them if no graph from before the capture holds the same leaves:
+# autograd runs a leaf's gradient on the stream where the leaf was first used.
+# grad_norm and clip_grad_norm_ may be captured too.
 # ---------------------------------------------------------------------------
 
 _DTYPE = {torch.float32: tlf.DTYPE_F32, torch.bfloat16: tlf.DTYPE_BF16}
@@ -514,17 +521,18 @@ class _Attention(torch.autograd.Function):
                        scale, *strides, qw)
         shape = _attn_shape(ctx.numbers, offsets, k_offsets, k_lengths)
         lse = torch.empty((heads, q.shape[0]), dtype=torch.float32, device=q.device) if grad else None
+        low = torch.empty_like(o) if grad and o.dtype == torch.bfloat16 else None  # what o's rounding takes
         ws, n = _workspace(tlf.load().tlf_attn_ws_bytes, shape, device=q.device)
-        _run(tlf.load().tlf_attn, q.device, shape, q, k, v, o, lse, ws, n)
+        _run(tlf.load().tlf_attn, q.device, shape, q, k, v, o, lse, low, ws, n)
         if grad:
             ctx.packed = packed
-            ctx.save_for_backward(q, None if packed else k, None if packed else v, offsets, k_offsets, k_lengths, o, lse)
+            ctx.save_for_backward(q, None if packed else k, None if packed else v, offsets, k_offsets, k_lengths, o, lse, low)
         return o
 
     @staticmethod
     @_first_order
     def backward(ctx, saved, do):
-        q, k, v, offsets, k_offsets, k_lengths, o, lse = saved
+        q, k, v, offsets, k_offsets, k_lengths, o, lse, low = saved
         _, _, heads, kv_heads, width = ctx.numbers[:5]
         qw, kw = heads * width, kv_heads * width
         do = _aligned(do)
@@ -537,8 +545,8 @@ class _Attention(torch.autograd.Function):
             strides = (qw, kw, kw)
         shape = _attn_shape(ctx.numbers, offsets, k_offsets, k_lengths)
         ws, n = _workspace(tlf.load().tlf_attn_grad_ws_bytes, shape, device=q.device)
-        _run(tlf.load().tlf_attn_grad, q.device, shape, do, q, k, v, o, lse, dq, strides[0], dk, strides[1], dv, strides[2],
-             ws, n)
+        _run(tlf.load().tlf_attn_grad, q.device, shape, do, q, k, v, o, lse, low, dq, strides[0], dk, strides[1], dv,
+             strides[2], ws, n)
         grads = (dx, None, None) if ctx.packed else (dq, dk, dv)
         return (*grads, *(None,) * 10)
 

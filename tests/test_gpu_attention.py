@@ -226,6 +226,41 @@ def test_scores_far_from_zero(dtype, D, nq, scores):
             _within(got[name], r[name], lim[name], (name, window))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nq,window,std", [(300, None, 1.0), (300, None, 2.0), (300, 40, 3.0), (4, None, 2.0), (1, None, 2.0)])
+def test_roundings_are_those_of_the_operands(D, nq, window, std):
+    """bfloat16 tensors, rows that few keys have most of the weight of: equal in norm to the formula with its operands
+    (weights, gradients of scores) and results rounded and nothing else, o as the gradients take it among that, to 2^-10.
+    Left over are values next to a rounding's border that float32's errors move across it: a score is off by less than
+    (D + 8) 2^-24 of the sum of its magnitudes, some 2^-13 in all here, so that of the values at most 2^-13 / 2^-8 move by
+    2^-8: in norm 2^-8 2^-2.5 at the very most, and with typical errors (2^-19 of a score) 2^-8 2^-5.5 = 2^-13.5."""
+    train = _train()
+    rng = np.random.default_rng(6)
+    n, heads = 300, 4
+    q = _normal(rng, nq, heads, D, std=std, dtype="bf16")
+    k, v = (_normal(rng, n, heads, D, std=s, dtype="bf16") for s in (std, 1.0))
+    do = _normal(rng, nq, heads, D, dtype="bf16")
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    o = train.attention(*leaves, _offsets([nq]), _offsets([n]), window=window)
+    got = [_np(t) for t in (o, *torch.autograd.grad(o, leaves, do))]
+    q, k, v, do = map(_np, (q, k, v, do))
+
+    def bf(x):
+        return torch.from_numpy(x).float().bfloat16().double().numpy()
+
+    want, scale, seen = [np.zeros(t.shape) for t in (q, q, k, v)], D ** -0.5, O.visible(nq, n, window, 0)
+    for h in range(heads):
+        s = np.where(seen, scale * np.log2(np.e) * (q[:, h] @ k[:, h].T), -np.inf)
+        w = np.exp2(s - np.ceil(s.max(1, keepdims=True)))
+        p = w / w.sum(1, keepdims=True)
+        oh = bf(w) @ v[:, h] / bf(w).sum(1, keepdims=True)
+        ds = bf(p * (do[:, h] @ v[:, h].T - (do[:, h] * oh).sum(1, keepdims=True)))
+        for t, x in zip(want, (oh, scale * ds @ k[:, h], scale * ds.T @ q[:, h], bf(p).T @ do[:, h])):
+            t[:, h] = bf(x)
+    for name, a, b in zip(("o", "dq", "dk", "dv"), got, want):
+        assert np.linalg.norm(a - b) <= 2.0 ** -10 * np.linalg.norm(b), (name, np.linalg.norm(a - b) / np.linalg.norm(b))
+
+
 # ---------------------------------------------------------------------------
 # What is not seen takes no part, whatever its values; layouts, streams, order
 # ---------------------------------------------------------------------------

@@ -45,42 +45,46 @@ SHAPES = [
 def test_attention_shape_refusals(lib, kw, status):
     need, s = ctypes.c_size_t(), _shape(**kw)
     assert lib.tlf_attn_ws_bytes(s, need) == status and lib.tlf_attn_grad_ws_bytes(s, need) == status
-    assert lib.tlf_attn(s, P, P, P, P, P, P, BIG, None) == status
-    assert lib.tlf_attn_grad(s, P, P, P, P, P, P, P, 256, P, 128, P, 128, P, BIG, None) == status
+    assert lib.tlf_attn(s, P, P, P, P, P, P, P, BIG, None) == status
+    assert lib.tlf_attn_grad(s, P, P, P, P, P, P, P, P, 256, P, 128, P, 128, P, BIG, None) == status
 
 
 @pytest.mark.parametrize("at", range(1, 5))
 @pytest.mark.parametrize("bad", [None, ODD])
 def test_attention_pointer_refusals(lib, at, bad):
-    args = [_shape(), P, P, P, P, P, P, BIG, None]
+    args = [_shape(), P, P, P, P, P, P, P, BIG, None]
     args[at] = bad
     assert lib.tlf_attn(*args) == BAD
 
 
 def test_attention_other_refusals(lib):
-    assert lib.tlf_attn(None, P, P, P, P, P, P, BIG, None) == BAD
+    assert lib.tlf_attn(None, P, P, P, P, P, P, P, BIG, None) == BAD
     assert lib.tlf_attn_ws_bytes(_shape(), None) == BAD and lib.tlf_attn_grad_ws_bytes(_shape(), None) == BAD
-    assert lib.tlf_attn(_shape(), P, P, P, P, 0x1002, P, BIG, None) == BAD
-    assert lib.tlf_attn(_shape(d_q_offsets=0x1002), P, P, P, P, P, P, BIG, None) == BAD
-    assert lib.tlf_attn(_shape(d_k_lengths=0x1001), P, P, P, P, P, P, BIG, None) == BAD
+    assert lib.tlf_attn(_shape(), P, P, P, P, 0x1002, P, P, BIG, None) == BAD
+    assert lib.tlf_attn(_shape(d_q_offsets=0x1002), P, P, P, P, P, P, P, BIG, None) == BAD
+    assert lib.tlf_attn(_shape(d_k_lengths=0x1001), P, P, P, P, P, P, P, BIG, None) == BAD
     need, few = ctypes.c_size_t(), _shape(rows_q=3, rows_k=300000, window=0)
     assert lib.tlf_attn_ws_bytes(few, need) == tlf.OK and need.value > 0
-    assert lib.tlf_attn(few, P, P, P, P, None, P, need.value - 1, None) == BAD
-    assert lib.tlf_attn(few, P, P, P, P, None, None, BIG, None) == BAD
-    assert lib.tlf_attn(_shape(rows_q=0), None, P, P, None, None, None, 0, None) == tlf.OK
+    assert lib.tlf_attn(few, P, P, P, P, None, None, P, need.value - 1, None) == BAD
+    assert lib.tlf_attn(few, P, P, P, P, None, None, None, BIG, None) == BAD
+    assert lib.tlf_attn(_shape(rows_q=0), None, P, P, None, None, None, None, 0, None) == tlf.OK
+    assert lib.tlf_attn(_shape(), P, P, P, P, P, ODD, P, BIG, None) == BAD
+    f32 = _shape(dtype=F32)  # whose o is not rounded
+    assert lib.tlf_attn(f32, P, P, P, P, P, P, P, BIG, None) == BAD
+    assert lib.tlf_attn_grad(f32, P, P, P, P, P, P, P, P, 256, P, 128, P, 128, P, BIG, None) == BAD
 
 
-@pytest.mark.parametrize("at,bad", [(k, b) for k in (1, 2, 3, 4, 5, 7, 9, 11, 13) for b in (None, ODD)] +
-                         [(6, None), (6, 0x1002), (8, 248), (8, 257), (10, 120), (12, 120), (14, 4)])
+@pytest.mark.parametrize("at,bad", [(k, b) for k in (1, 2, 3, 4, 5, 8, 10, 12, 14) for b in (None, ODD)] +
+                         [(6, None), (6, 0x1002), (7, ODD), (9, 248), (9, 257), (11, 120), (13, 120), (15, 4)])
 def test_attention_gradient_refusals(lib, at, bad):
-    args = [_shape(), P, P, P, P, P, P, P, 256, P, 128, P, 128, P, BIG, None]
+    args = [_shape(), P, P, P, P, P, P, P, P, 256, P, 128, P, 128, P, BIG, None]
     args[at] = bad
     assert lib.tlf_attn_grad(*args) == BAD
 
 
 def test_attention_gradient_of_nothing(lib):
     s = _shape(rows_q=0, rows_k=0, batch=0)
-    assert lib.tlf_attn_grad(s, None, None, None, None, None, None, None, 256, None, 128, None, 128, None, 0, None) == tlf.OK
+    assert lib.tlf_attn_grad(s, None, None, None, None, None, None, None, None, 256, None, 128, None, 128, None, 0, None) == tlf.OK
 
 
 def test_struct_layouts_match_the_header(tmp_path):
