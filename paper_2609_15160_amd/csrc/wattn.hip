@@ -310,7 +310,9 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 // visible keys, its four waves 32 keys each in turn, and adds the waves' sums in
 // LDS.  Keys come straight from memory as operands, values through a wave's own LDS
 // rows for the transposed read; both of the next turn are on their way while this
-// one is used.  Bound by HBM: every visible key and value is read once.
+// one is used.  The base is the largest score itself, whose weight 1 is not rounded (error
+// over 512 keys with scores of variance 16: 0.0018, with whole bases 0.0019; of variance
+// 1 0.0023 and 0.0024).  Bound by HBM: every visible key and value is read once.
 constexpr int kFewWaves = 4, kFewKeys = 32;
 template <typename T, int D> struct FewPart {  // sums of one head over a range
   static constexpr int FLOATS = D + 4;         // o, then m, l, the row's visible keys, l of the rounded weights
@@ -407,7 +409,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
         if (x + t * 16 + 4 * g + r >= xb) sc[t][r] = -INFINITY;
         mx = fmaxf(mx, sc[t][r]);
       }
-    mx = fmaxf(m, ceilf(max_quads(mx) * a.scale_log2));  // whole numbers: the sums are scaled exactly
+    mx = fmaxf(m, max_quads(mx) * a.scale_log2);
     const float base = mx == -INFINITY ? 0.f : mx, alpha = __builtin_amdgcn_exp2f(m - base);
     m = mx;
     l *= alpha;
