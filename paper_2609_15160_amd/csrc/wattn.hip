@@ -327,34 +327,35 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
   constexpr int SUMS = kFewWaves * 16 * (D + 3) * 4, ROWS = kFewWaves * kFewKeys * H::RB;
   __shared__ __align__(1024) char lds[SUMS > ROWS ? SUMS : ROWS];
   const int each = a.heads / a.kv_heads, chunks = (each + 15) / 16;
-  const int split = blockIdx.x % a.splits, unit = blockIdx.x / a.splits;
+  const int lin = xcd_run(blockIdx.x, gridDim.x), split = lin % a.splits, unit = lin / a.splits;
   const int gc = unit % chunks, kvh = unit / chunks % a.kv_heads, row = unit / (chunks * a.kv_heads);
   const int h0 = kvh * each + gc * 16, cols = min(each - gc * 16, 16);
-
-  // The last sequence that begins at or before the row: with a row of each sequence it is
-  // the row's own number, which is tried first (the search costs two trips to memory).
-  int b = min(row, a.batch);
-  if (a.q_off[b] > row || (b < a.batch && row >= a.q_off[b + 1])) {
-    b = 0;
-    for (int hi = a.batch; hi > b;) {
-      const int step = (hi - b + kWave - 1) / kWave, x = b + (lane_id() + 1) * step;
-      const bool before = x <= hi && a.q_off[min(x, hi)] <= row;
-      b += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * step;
-      hi = min(hi, b + step - 1);
-    }
-  }
-  const WSeq s = load_seq(a, b);
-  const int p = row - s.q0 + s.n - s.nq;
-  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
-  const int nv = s.n > 0 && p >= 0 && (unsigned)(row - s.q0) < (unsigned)s.nq ? sinks + p + 1 - near : 0;
-  const int per = ((nv + kFewKeys - 1) / kFewKeys + a.splits - 1) / a.splits * kFewKeys;
-  const int xa = min(nv, split * per), xb = min(nv, xa + per);  // of the visible keys, sinks first
 
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), c16 = lane & 15, g = lane >> 4;
   Frag qf[KSTEPS];
   const T* q = reinterpret_cast<const T*>(a.q) + (int64_t)row * a.qs + (h0 + min(c16, cols - 1)) * D + g * H::EPC;
 #pragma unroll
   for (int ks = 0; ks < KSTEPS; ++ks) qf[ks] = *reinterpret_cast<const Frag*>(q + ks * 4 * H::EPC);
+
+  // The last sequence that begins at or before the row: with a row of each sequence it is
+  // the row's own number, which is tried first (the search costs two trips to memory).
+  WSeq s = load_seq(a, min(row, a.batch));
+  if (s.q0 > row || row >= s.q0 + s.nq) {
+    int b = 0;
+    for (int hi = a.batch; hi > b;) {
+      const int step = (hi - b + kWave - 1) / kWave, x = b + (lane + 1) * step;
+      const bool before = x <= hi && a.q_off[min(x, hi)] <= row;
+      b += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * step;
+      hi = min(hi, b + step - 1);
+    }
+    s = load_seq(a, b);
+  }
+  const int p = row - s.q0 + s.n - s.nq;
+  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
+  const int nv = s.n > 0 && p >= 0 && (unsigned)(row - s.q0) < (unsigned)s.nq ? sinks + p + 1 - near : 0;
+  const int per = ((nv + kFewKeys - 1) / kFewKeys + a.splits - 1) / a.splits * kFewKeys;
+  const int xa = min(nv, split * per), xb = min(nv, xa + per);  // of the visible keys, sinks first
+
   const T* k = reinterpret_cast<const T*>(a.k) + (int64_t)s.k0 * a.ks + kvh * D;
   const T* v = reinterpret_cast<const T*>(a.v) + (int64_t)s.k0 * a.vs + kvh * D;
   char* mine = lds + wave * kFewKeys * H::RB;
