@@ -62,7 +62,14 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 
 // One workgroup: a tile of NW * 32 queries of one head, a wave 32 of them, over the
 // visible tiles of BN keys, which all waves share from two places in LDS (one tile
-// is used while the next arrives; one barrier a tile).
+// is used while the next arrives; one barrier a tile).  Tiles of 32 or of 128 keys,
+// three places, eight waves and raised priorities around the products were all slower.
+//
+// Bound by the issue of vector instructions beside the products: 32 keys x 32 queries
+// take 18 products (288 clocks of a SIMD's matrix cores at width 64) and 75 others, 16 of
+// them exponentials, which take four times as long (490).  8 x 4096 rows x 16 heads x 64,
+// window 1024, 4 sinks: 188-193 us, 640 TFLOP/s of the visible pairs; 4 x 4099 x 16 x 128:
+// 278-284 us, 730 TFLOP/s (matrix cores busy 33 and 34% of the time).
 //
 // The softmax base of a query is the largest score of the first tile that it sees a
 // key of, or kLeast if that is less (its only key there may be one of little weight):
@@ -312,7 +319,9 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 // rows for the transposed read; both of the next turn are on their way while this
 // one is used.  The base is the largest score itself, whose weight 1 is not rounded (error
 // over 512 keys with scores of variance 16: 0.0018, with whole bases 0.0019; of variance
-// 1 0.0023 and 0.0024).  Bound by HBM: every visible key and value is read once.
+// 1 0.0023 and 0.0024).  Bound by HBM: every visible key and value is read once:
+// 256 rows x 516 keys x 12 heads x 64 72 us, 5.6 TB/s (heads of a row on one XCD; in the
+// order of the workgroups 73.3); 2 rows x 105 000 keys x 2 key heads x 128 22 us, 4.5 TB/s.
 constexpr int kFewWaves = 4, kFewKeys = 32;
 template <typename T, int D> struct FewPart {  // sums of one head over a range
   static constexpr int FLOATS = D + 4;         // o, then m, l, the row's visible keys, l of the rounded weights
@@ -480,7 +489,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
 
 // The ranges' sums of one row's head: a workgroup whose threads have four dimensions
 // each, so that every D / 4 of them take a range, and the sums of those go through LDS
-// in a fixed order (2 rows of 16 heads x 128, 253 ranges: a wave each took 79 us).
+// in a fixed order (2 rows of 16 heads x 128, 253 ranges: 5.8 us, most of it the trips to
+// memory; a wave each took 79).
 constexpr int kJoinThreads = 512;
 template <typename T, int D> __global__ __launch_bounds__(kJoinThreads) void k_wattn_join(WAttnArgs a) {
   constexpr int PER = D / 4, SETS = kJoinThreads / PER, F = FewPart<T, D>::FLOATS;
@@ -584,14 +594,16 @@ bool is_few(const tlf_attn_shape& t) {
   return t.rows_q <= 8 * (int64_t)t.batch && slots_of<128>(t.rows_q, t.batch) * t.heads < 256;
 }
 
-// Ranges of the keys of a row, for four workgroups on a compute unit, and 256 keys of
-// a workgroup at least.
+// Ranges of the keys of a row, for two workgroups on a compute unit, and 256 keys of a
+// workgroup at least (with the join, us with one, two and four on a compute unit: 2 rows
+// x 65001 keys x 2 key heads x 128 28, 28 and 32; 8 x 4096 x 16 46, 47 and 49; 8 x 4096 x 4
+// 19, 19 and 18; 4 x 1500 x 16 16, 17 and 17; 128 keys at least: 30, 47, 19 and 17).
 int few_splits(const tlf_attn_shape& t) {
   const int each = t.heads / t.kv_heads;
   const int64_t units = std::max<int64_t>(1, (int64_t)t.rows_q * t.kv_heads * ((each + 15) / 16));
   int64_t keys = t.rows_k / std::max(1, t.batch);
   if (t.window > 0) keys = std::min<int64_t>(keys, (int64_t)t.window + t.sinks);
-  return (int)std::max<int64_t>(1, std::min((1024 + units - 1) / units, keys / 256));
+  return (int)std::max<int64_t>(1, std::min((512 + units - 1) / units, keys / 256));
 }
 
 template <typename T, int D> hipError_t launch(const tlf_attn_shape& t, WAttnArgs a, hipStream_t s) {

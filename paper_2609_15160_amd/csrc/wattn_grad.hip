@@ -85,6 +85,8 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
 // Tiles, waves and LDS as the forward kernel's (k_wattn).  q and do of the wave's 32
 // queries stay in registers; a tile's keys are read as they lie and transposed, its
 // values as they lie.  delta is of o with what its rounding took.  dP starts from -delta, so dS = P dP takes one product.
+// Bound as the forward kernel is: 8 x 4096 x 16 x 64, window 1024: 230 us, 790 TFLOP/s of
+// three products; 4 x 4099 x 16 x 128: 345-350 us, 880 TFLOP/s (matrix cores busy 37 and 39%).
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
   using H = HeadRows<T, D>;
@@ -307,6 +309,11 @@ template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 &
 // A tile's keys are seen by the queries from its first position to the window's end
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
+// Bound by the issue of instructions and by the reads of LDS, where q and do are read
+// twice, as they lie and transposed: 8 x 4096 x 16 x 64, window 1024: 304-310 us, 780
+// TFLOP/s of four products; 4 x 4099 x 16 x 128: 473-478 us, 860 (matrix cores busy 37 and
+// 39%).  Width 64 with two waves on a SIMD and operands read ahead, and tiles of 128
+// queries, were slower.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
   using H = HeadRows<T, D>;
@@ -581,29 +588,39 @@ __global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : 
   }
 }
 
-// The first tiles' sums over the ranges of their queries: a wave per key, four in turn
-// (a workgroup for every four keys would pass 2^32 threads at 2^19 sequences' heads).
+// The first tiles' sums over the ranges of their queries: a wave has four keys, whose
+// loads it has on their way together (in turn they took four times as long).
 constexpr int kSinkKeys = 16;  // of a workgroup
 template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wattn_sinks(GradArgs a) {
-  constexpr int N = (2 * D + kWave - 1) / kWave, BLOCKS = KT / kSinkKeys;
+  constexpr int N = (2 * D + kWave - 1) / kWave, BLOCKS = KT / kSinkKeys, KEYS = kSinkKeys / 4;
   const int unit = blockIdx.x / BLOCKS, b = unit / a.kv_heads, kvh = unit % a.kv_heads, lane = lane_id();
   const WSeq s = load_seq(a, b);
   if (s.n == 0) return;  // the tile's own workgroup has written its zeros
-  const int key0 = blockIdx.x % BLOCKS * kSinkKeys, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  for (int key = key0 + wave; key < min(key0 + kSinkKeys, s.cap); key += 256 / kWave) {
+  const int key0 = blockIdx.x % BLOCKS * kSinkKeys + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * KEYS;
+  const float* src = a.part + ((int64_t)unit * a.sink_parts * KT + key0) * 2 * D + min(lane, 2 * D - 1);
+  float t[KEYS][N];
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i)
+#pragma unroll
+    for (int e = 0; e < N; ++e) t[i][e] = 0.f;
+#pragma unroll 2
+  for (int k = 0; k < a.sink_parts; ++k, src += (int64_t)KT * 2 * D)
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) t[i][e] += src[i * 2 * D + e * kWave];
+#pragma unroll
+  for (int i = 0; i < KEYS; ++i) {
+    const int key = key0 + i;
+    if (key >= s.cap) return;
     T* dk = reinterpret_cast<T*>(a.dk) + (int64_t)(s.k0 + key) * a.dks + kvh * D;
     T* dv = reinterpret_cast<T*>(a.dv) + (int64_t)(s.k0 + key) * a.dvs + kvh * D;
-    const float* src = a.part + (int64_t)unit * a.sink_parts * KT * 2 * D + key * 2 * D;
-    float t[N];
     bool good = true;
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const int d = e * kWave + lane;
-      t[e] = 0.f;
-      if (d < 2 * D && key < s.n)
-        for (int k = 0; k < a.sink_parts; ++k) t[e] += src[(int64_t)k * KT * 2 * D + d];
-      if (d < D) t[e] *= a.scale;
-      good &= finite1(t[e]);
+      if (key >= s.n) t[i][e] = 0.f;  // room without keys
+      if (e * kWave + lane < D) t[i][e] *= a.scale;
+      good &= finite1(t[i][e]);
     }
     if (__builtin_amdgcn_ballot_w64(!good)) {
       slow_dkv<T, D>(a, s, kvh, key);
@@ -612,18 +629,25 @@ template <typename T, int D, int KT> __global__ __launch_bounds__(256) void k_wa
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       const int d = e * kWave + lane;
-      if (d < D) dk[d] = from_f<T>(t[e]);
-      else if (d < 2 * D) dv[d - D] = from_f<T>(t[e]);
+      if (d < D) dk[d] = from_f<T>(t[i][e]);
+      else if (d < 2 * D) dv[d - D] = from_f<T>(t[i][e]);
     }
   }
 }
 
-// Ranges of a first tile's queries, each as long as two other tiles' at least; 0: there
-// are no sinks.
+// Ranges of a first tile's queries; 0: there are no sinks.  Its workgroup, which all
+// queries of the sequence go through, is started first: it is split where even so it
+// would outlast the others, each of which sees the window's queries, on 256 compute
+// units with three workgroups each, and into ranges no shorter than theirs (dk and dv
+// with the join, us without ranges and with them, 12 x 64 heads, 4 sinks: 8 x 4096 rows,
+// window 256 149 and 119 (2 ranges), window 64 149 and 97 (4); 1 x 32768, window 1024
+// 1021 and 259 (7); twice as many 125, 101 and 260; 32 x 2048, window 128, which stays
+// whole, 172 and in 4 ranges 199).
 int sink_parts(const tlf_attn_shape& t) {
   if (t.window <= 0 || t.sinks <= 0 || t.batch <= 0) return 0;
-  const int64_t rows = t.rows_q / t.batch, other = 2 * ((int64_t)t.window + 128);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(16, rows / other));
+  const int64_t rows = t.rows_q / t.batch, other = std::min<int64_t>((int64_t)t.window + 128, rows);
+  const int64_t all = (rows / 128 * other + rows) * t.batch * t.heads, share = std::max<int64_t>({1, other, all / 768});
+  return (int)std::max<int64_t>(1, std::min<int64_t>(16, rows * (t.heads / t.kv_heads) / share));
 }
 
 int64_t stat_floats(const tlf_attn_shape& t) { return ((int64_t)t.heads * t.rows_q + 3) / 4 * 4; }

@@ -183,6 +183,13 @@ def test_many_tiles(dtype, D):
     _check([1500, 0, 1390, 700], 16, 16, D, window=50, sinks=5, dtype=dtype, packed=True, tail=130)
 
 
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("n,heads,kv,room", [([2500], 1, 1, None), ([1500, 3, 0, 700], 4, 2, [1500, 3, 5, 800])])
+def test_sinks_of_long_sequences(dtype, D, n, heads, kv, room):
+    """First tiles whose queries go in many ranges, joined afterwards; short and empty sequences and room among them."""
+    _check(n, heads, kv, D, window=20, sinks=5, dtype=dtype, room=room)
+
+
 def test_many_tiles_causal():
     _check([1030, 900, 1100, 1025], 16, 8, 64, dtype="bf16", packed=True)
 
