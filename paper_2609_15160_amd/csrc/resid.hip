@@ -37,7 +37,9 @@ struct ResidArgs {
 
 __device__ __forceinline__ float dot4(f32x4 a, f32x4 b) { return (a[0] * b[0] + a[1] * b[1]) + (a[2] * b[2] + a[3] * b[3]); }
 
-// One wave per row, the row in registers: 4 NV elements of x and of y per lane.
+// One wave per row, the row in registers: 4 NV elements of x and of y per lane, so that
+// nothing is read twice and no row waits for another.  Bound by HBM: 32768 x 1024 bf16 y,
+// 8 groups 76 us, 5.3 TB/s (a copy of 1 GiB: 5.1); 9999 x 2048 float32, post_norm 69 us, 4.7.
 template <typename T, int NV, bool POST, bool PAST>
 __global__ __launch_bounds__(kRowWaves* kWave) void k_resid(ResidArgs a) {
   const int row = __builtin_amdgcn_readfirstlane(blockIdx.x * kRowWaves + threadIdx.x / kWave), lane = lane_id();
@@ -144,6 +146,8 @@ __global__ __launch_bounds__(kRowWaves* kWave) void k_resid_dx(ResidArgs a) {
 // registers of their own.  The rows' sums go over the waves through LDS, one barrier
 // for RU rows; the next RU rows are on their way meanwhile.  With more groups than
 // kMaxSums the pass is made again for those behind them, without the rows' gradients.
+// Bound by HBM, and by the loads' latency between two barriers: 32768 x 1024 bf16 y, 8
+// groups 122-125 us, 4.9 TB/s; 9999 x 2048 float32, post_norm, 3 groups 100 us, 4.9.
 template <typename T, int GMAX, int MAXT, int RU, bool POST, bool PAST>
 __global__ __launch_bounds__(MAXT) void k_resid_grad(ResidArgs a, int chunk, int first, float* part) {
   constexpr int SUMS = POST ? 3 : 1;
@@ -275,7 +279,8 @@ __global__ __launch_bounds__(MAXT) void k_resid_grad(ResidArgs a, int chunk, int
 
 // Rows of a workgroup: 8 waves per compute unit where the rows allow it, all that the
 // registers let run at a time, and 8 rows at least, so that the sums stay a small part
-// of the traffic and few rows still spread.
+// of the traffic and few rows still spread.  Twice as many workgroups write twice the
+// sums (32768 x 1024, 8 groups: the join 11.8 us, so 6.8; the rows' pass the same).
 int resid_chunk(int rows, int d) {
   const int waves = (d + kGammaCols - 1) / kGammaCols, most = 2048 / waves;
   const int c = (rows + most - 1) / most;
