@@ -321,7 +321,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 // over 512 keys with scores of variance 16: 0.0018, with whole bases 0.0019; of variance
 // 1 0.0023 and 0.0024).  Bound by HBM: every visible key and value is read once:
 // 256 rows x 516 keys x 12 heads x 64 72 us, 5.6 TB/s (heads of a row on one XCD; in the
-// order of the workgroups 73.3); 2 rows x 105 000 keys x 2 key heads x 128 22 us, 4.5 TB/s.
+// order of the workgroups 73.3); 2 rows x 49 000 keys x 2 key heads x 128 21 us, 4.7 TB/s.
 constexpr int kFewWaves = 4, kFewKeys = 32;
 template <typename T, int D> struct FewPart {  // sums of one head over a range
   static constexpr int FLOATS = D + 4;         // o, then m, l, the row's visible keys, l of the rounded weights
@@ -489,8 +489,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
 
 // The ranges' sums of one row's head: a workgroup whose threads have four dimensions
 // each, so that every D / 4 of them take a range, and the sums of those go through LDS
-// in a fixed order (2 rows of 16 heads x 128, 253 ranges: 5.8 us, most of it the trips to
-// memory; a wave each took 79).
+// in a fixed order (2 rows of 16 heads x 128, 128 ranges: 4 us, most of it the trips to
+// memory; a wave each took 79 with 253).
 constexpr int kJoinThreads = 512;
 template <typename T, int D> __global__ __launch_bounds__(kJoinThreads) void k_wattn_join(WAttnArgs a) {
   constexpr int PER = D / 4, SETS = kJoinThreads / PER, F = FewPart<T, D>::FLOATS;
