@@ -508,17 +508,17 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, k, v, offsets, k_offsets, k_lengths, heads, kv_heads, width, window, sinks, scale, grad):
         packed = k is None
+        qw, kw = heads * width, kv_heads * width
         q = _rows_of_heads(x, heads + 2 * kv_heads if packed else heads, width)
         if packed:
-            q, k, v = q, q[:, heads * width:], q[:, (heads + kv_heads) * width:]
+            k, v = _key_rows(q, qw, kw)
+            strides, rows_k = (_row_stride(q, qw + 2 * kw),) * 3, q.shape[0]
         else:
             k, v = _rows_of_heads(k, kv_heads, width), _rows_of_heads(v, kv_heads, width)
-        o = torch.empty((q.shape[0], heads * width) if packed else (q.shape[0], heads, width), dtype=q.dtype, device=q.device)
-        qw, kw = heads * width, kv_heads * width
-        strides = (_row_stride(q, qw + 2 * kw), _row_stride(q, qw + 2 * kw), _row_stride(q, qw + 2 * kw)) if packed else \
-            (_row_stride(q, qw), _row_stride(k, kw), _row_stride(v, kw))
-        ctx.numbers = (_DTYPE[q.dtype], offsets.numel() - 1, heads, kv_heads, width, q.shape[0], k.shape[0], window, sinks,
-                       scale, *strides, qw)
+            strides, rows_k = (_row_stride(q, qw), _row_stride(k, kw), _row_stride(v, kw)), k.shape[0]
+        o = torch.empty((q.shape[0], qw) if packed else (q.shape[0], heads, width), dtype=q.dtype, device=q.device)
+        ctx.numbers = (_DTYPE[q.dtype], offsets.numel() - 1, heads, kv_heads, width, q.shape[0], rows_k, window, sinks, scale,
+                       *strides, qw)
         shape = _attn_shape(ctx.numbers, offsets, k_offsets, k_lengths)
         lse = torch.empty((heads, q.shape[0]), dtype=torch.float32, device=q.device) if grad else None
         low = torch.empty_like(o) if grad and o.dtype == torch.bfloat16 else None  # what o's rounding takes
@@ -537,9 +537,9 @@ class _Attention(torch.autograd.Function):
         qw, kw = heads * width, kv_heads * width
         do = _aligned(do)
         if ctx.packed:
-            k, v = q[:, qw:], q[:, qw + kw:]
-            dx = torch.empty((q.shape[0], qw + 2 * kw), dtype=q.dtype, device=q.device)
-            dq, dk, dv, strides = dx, dx[:, qw:], dx[:, qw + kw:], (qw + 2 * kw,) * 3
+            k, v = _key_rows(q, qw, kw)
+            dq = torch.empty((q.shape[0], qw + 2 * kw), dtype=q.dtype, device=q.device)
+            (dk, dv), strides = _key_rows(dq, qw, kw), (qw + 2 * kw,) * 3
         else:
             dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
             strides = (qw, kw, kw)
@@ -547,8 +547,14 @@ class _Attention(torch.autograd.Function):
         ws, n = _workspace(tlf.load().tlf_attn_grad_ws_bytes, shape, device=q.device)
         _run(tlf.load().tlf_attn_grad, q.device, shape, do, q, k, v, o, lse, low, dq, strides[0], dk, strides[1], dv,
              strides[2], ws, n)
-        grads = (dx, None, None) if ctx.packed else (dq, dk, dv)
+        grads = (dq, None, None) if ctx.packed else (dq, dk, dv)
         return (*grads, *(None,) * 10)
+
+
+def _key_rows(rows: torch.Tensor, qw: int, kw: int):
+    """Where k and v begin in rows q | k | v: addresses, which cost the host less than tensors of their own."""
+    at, each = rows.data_ptr(), rows.element_size()
+    return at + qw * each, at + (qw + kw) * each
 
 
 def _attn_shape(numbers, offsets, k_offsets, k_lengths) -> tlf.AttnShape:
