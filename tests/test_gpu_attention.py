@@ -433,6 +433,36 @@ def test_no_rows_and_no_sequences():
     assert not o.any() and not torch.autograd.grad(o.sum(), t)[0].any()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_gradients_from_o_alone(D):
+    """The C entry points without what o's rounding takes: to the same bounds, which carry that rounding."""
+    import ctypes
+
+    from paper_2609_15160_amd import tlf
+    train, lib = _train(), tlf.load()
+    rng = np.random.default_rng(8)
+    n, heads, kv, window, sinks = 200, 4, 2, 50, 3
+    q, do = (_normal(rng, n, heads, D, dtype="bf16") for _ in range(2))
+    k, v = (_normal(rng, n, kv, D, dtype="bf16") for _ in range(2))
+    off = _offsets([n])
+    o, dq, dk, dv = (torch.full_like(t, float("nan")) for t in (q, q, k, v))
+    lse = torch.empty(heads, n, device="cuda")
+    shape = tlf.AttnShape(tlf.DTYPE_BF16, 1, heads, kv, D, n, n, window, sinks, D ** -0.5, heads * D, kv * D, kv * D, heads * D,
+                          off.data_ptr(), off.data_ptr(), None)
+    need = ctypes.c_size_t()
+    assert lib.tlf_attn_ws_bytes(shape, need) == tlf.OK and need.value == 0
+    train._run(lib.tlf_attn, q.device, shape, q, k, v, o, lse, None, None, 0)
+    assert lib.tlf_attn_grad_ws_bytes(shape, need) == tlf.OK
+    ws = torch.empty(need.value, dtype=torch.uint8, device="cuda")
+    train._run(lib.tlf_attn_grad, q.device, shape, do, q, k, v, o, lse, None, dq, heads * D, dk, kv * D, dv, kv * D, ws,
+               need.value)
+    arrays = [_np(t) for t in (q, k, v)]
+    r = O.attention(*arrays, window, sinks, None, _np(do))
+    lim = bounds(*arrays, r, window, sinks, D ** -0.5, "bf16", _np(do))
+    for name, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+        _within(t, r[name], lim[name], name)
+
+
 def test_gradients_of_gradients_are_refused():
     train = _train()
     t = torch.ones(5, 4, 64, device="cuda", requires_grad=True)
