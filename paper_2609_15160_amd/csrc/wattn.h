@@ -16,6 +16,7 @@
 
 #include "common.h"
 #include "stage.h"
+#include "visible.h"
 
 namespace tlf {
 

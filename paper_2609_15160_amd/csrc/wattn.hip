@@ -29,7 +29,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // The row again from the visible keys alone, for rows whose result is not finite:
 // in a product of tiles a weight of zero times an infinite or NaN value of a key
-// that the query does not see is NaN.
+// that the query does not see is NaN.  The row sees a key at least.
 template <typename T, int D>
 __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int h, int row) {
   const int kvh = h / (a.heads / a.kv_heads), p = row + s.n - s.nq;
@@ -38,16 +38,16 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
   LaneRow<T, D> q, x, o;
   q.load(reinterpret_cast<const T*>(a.q) + (int64_t)(s.q0 + row) * a.qs + h * D);
   o.zero();
-  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
+  const VisibleKeys keys(p, a.window, a.sinks);
   float m = -INFINITY, l = 0.f;
-  for (int i = 0; i < sinks + p + 1 - near; ++i) {
-    x.load(k + (int64_t)(i < sinks ? i : near + i - sinks) * a.ks);
+  for (int i = 0; i < keys.count; ++i) {
+    x.load(k + (int64_t)keys[i] * a.ks);
     const float t = q.dot(x) * a.scale_log2;
     m = t != t ? t : fmaxf(m, t);
     if (t != t) break;
   }
-  for (int i = 0; i < sinks + p + 1 - near; ++i) {
-    const int64_t j = i < sinks ? i : near + i - sinks;
+  for (int i = 0; i < keys.count; ++i) {
+    const int64_t j = keys[i];
     x.load(k + j * a.ks);
     const float w = __builtin_amdgcn_exp2f(q.dot(x) * a.scale_log2 - m);
     l += w;
@@ -282,11 +282,12 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
 #pragma unroll
   for (int qn = 0; qn < QN; ++qn) {
     const int row = r0 + qn * 16 + c16;
-    const float sum = sum_quads(ls[qn]), inv = p[qn] < 0 ? 0.f : 1.f / (kRounds ? lr[qn][0] : sum);
-    bool good = p[qn] < 0 || sum >= kSumMin;
+    const bool none = p[qn] < 0;  // sees no key: zeros, whatever its weights of zero were multiplied by
+    const float sum = sum_quads(ls[qn]), inv = 1.f / (kRounds ? lr[qn][0] : sum);
+    bool good = none || sum >= kSumMin;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      o[dt][qn] *= inv;
+      o[dt][qn] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt][qn] * inv;
       good &= finite4(o[dt][qn]);
     }
     uint64_t again = __builtin_amdgcn_ballot_w64(!good && row < s.nq);
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
       } else {
         Vec4<T>::store(dst + g * 4, o[0][qn]);
       }
-      if (a.lse && g == 0) a.lse[(int64_t)h * a.rows_q + s.q0 + row] = p[qn] < 0 ? INFINITY : base[qn] + log2f(sum);
+      if (a.lse && g == 0) a.lse[(int64_t)h * a.rows_q + s.q0 + row] = none ? INFINITY : base[qn] + log2f(sum);
     }
     for (; again; again &= again - 1) slow_row<T, D>(a, s, h, r0 + qn * 16 + __builtin_ctzll(again));
   }
@@ -360,8 +361,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
     s = load_seq(a, b);
   }
   const int p = row - s.q0 + s.n - s.nq;
-  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
-  const int nv = s.n > 0 && p >= 0 && (unsigned)(row - s.q0) < (unsigned)s.nq ? sinks + p + 1 - near : 0;
+  const VisibleKeys keys(p, a.window, a.sinks);
+  const int nv = s.n > 0 && (unsigned)(row - s.q0) < (unsigned)s.nq ? keys.count : 0;
   const int per = ((nv + kFewKeys - 1) / kFewKeys + a.splits - 1) / a.splits * kFewKeys;
   const int xa = min(nv, split * per), xb = min(nv, xa + per);  // of the visible keys, sinks first
 
@@ -372,18 +373,17 @@ __global__ __launch_bounds__(kFewWaves* kWave, (kRoom<T, D>)) void k_wattn_few(W
 
   Frag kf[NT][KSTEPS];
   uint4 vf[VN];
-  auto key = [&](int x) { return (int64_t)(x < sinks ? x : near + x - sinks); };
   auto load = [&](int x) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const T* src = k + key(min(x + 16 * t + c16, xb - 1)) * a.ks + g * H::EPC;
+      const T* src = k + (int64_t)keys[min(x + 16 * t + c16, xb - 1)] * a.ks + g * H::EPC;
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks) kf[t][ks] = *reinterpret_cast<const Frag*>(src + ks * 4 * H::EPC);
     }
 #pragma unroll
     for (int c = 0; c < VN; ++c) {
       const int e = c * kWave + lane;
-      vf[c] = *reinterpret_cast<const uint4*>(v + key(min(x + e / H::CPR, xb - 1)) * a.vs + e % H::CPR * H::EPC);
+      vf[c] = *reinterpret_cast<const uint4*>(v + (int64_t)keys[min(x + e / H::CPR, xb - 1)] * a.vs + e % H::CPR * H::EPC);
     }
   };
   f32x4 o[DT];

@@ -47,9 +47,9 @@ __device__ __forceinline__ void slow_dq(const GradArgs& a, const WSeq& s, int h,
   }
   const float lse = a.lse[(int64_t)h * a.rows_q + s.q0 + row];
   o.zero();
-  const int near = max(0, p - a.window + 1), sinks = min(a.sinks, near);
-  for (int i = 0; i < sinks + p + 1 - near; ++i) {
-    const int64_t j = i < sinks ? i : near + i - sinks;
+  const VisibleKeys keys(p, a.window, a.sinks);
+  for (int i = 0; i < keys.count; ++i) {
+    const int64_t j = keys[i];
     x.load(v + j * a.vs);
     const float dp = d.dot(x);
     x.load(k + j * a.ks);
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(G
     bool good = true;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      dq[dt][qn] *= a.scale;
+      dq[dt][qn] = p[qn] < 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : dq[dt][qn] * a.scale;  // sees no key: zeros
       good &= finite4(dq[dt][qn]);
     }
     uint64_t again = __builtin_amdgcn_ballot_w64(!good && row < s.nq);

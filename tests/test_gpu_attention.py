@@ -318,6 +318,60 @@ def test_values_that_are_not_finite_stay_where_they_are_seen(dtype, D, bad):
             assert same.any() == some and np.all(np.abs(have[same] - want[same]) <= lim[name][same]), (name, window)
 
 
+def _entry(q, k, v, do, offsets, k_offsets, window, sinks, scale=None):
+    """Through the C entry points, their outputs full of NaN before: a dict of o, lse, low (bfloat16) and the gradients."""
+    import ctypes
+
+    from paper_2609_15160_amd import tlf
+    train, lib = _train(), tlf.load()
+    (rows, heads, D), (k_rows, kv) = q.shape, k.shape[:2]
+    out = {name: torch.full_like(t, float("nan")) for name, t in (("o", q), ("dq", q), ("dk", k), ("dv", v))}
+    out["lse"] = torch.full((heads, rows), float("nan"), device="cuda")
+    out["low"] = torch.full_like(q, float("nan")) if q.dtype == torch.bfloat16 else None
+    wide, kv_wide = heads * D, kv * D
+    shape = tlf.AttnShape(train._DTYPE[q.dtype], len(offsets) - 1, heads, kv, D, rows, k_rows, window or 0, sinks,
+                          D ** -0.5 if scale is None else scale, wide, kv_wide, kv_wide, wide, offsets.data_ptr(),
+                          k_offsets.data_ptr(), None)
+    ws, need = train._workspace(lib.tlf_attn_ws_bytes, shape, device=q.device)
+    train._run(lib.tlf_attn, q.device, shape, q, k, v, out["o"], out["lse"], out["low"], ws, need)
+    ws, need = train._workspace(lib.tlf_attn_grad_ws_bytes, shape, device=q.device)
+    train._run(lib.tlf_attn_grad, q.device, shape, do, q, k, v, out["o"], out["lse"], out["low"], out["dq"], wide, out["dk"],
+               kv_wide, out["dv"], kv_wide, ws, need)
+    return out
+
+
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("nq,n", [(40, 7), (60, 40), (300, 130)])
+def test_queries_before_the_first_key_give_zeros_whatever_the_values(dtype, D, nq, n):
+    """Queries that see no key beside ones that do, in one tile and one wave; keys, values and the unseeing rows' own q
+    and gradients not finite: zeros, an lse of +inf, and no part in any gradient."""
+    rng = np.random.default_rng(27)
+    heads, before = 2, nq - n
+    q, do = (_normal(rng, nq, heads, D, dtype=dtype) for _ in range(2))
+    k, v = (_normal(rng, n, heads, D, dtype=dtype) for _ in range(2))
+    qb, kb, vb, db = (t.clone() for t in (q, k, v, do))
+    qb[0], qb[before - 1, 0, 1] = float("nan"), float("inf")
+    db[0, 0, 3], db[before - 1] = float("inf"), float("nan")
+    kb[n - 1, 0] = float("nan")
+    vb[0, 0, 5], vb[n // 2, 1, 2], vb[n // 2, 1, 3] = float("inf"), float("nan"), -float("inf")
+    for window, sinks in ((None, 0), (5, 0), (5, 2)):
+        _say("before the first key", dtype, D, nq, n, window, sinks)
+        got = _entry(qb, kb, vb, db, _offsets([nq]), _offsets([n]), window, sinks)
+        for name in ("o", "dq", "low"):
+            assert got[name] is None or not got[name][:before].any(), (name, window)  # NaN counts as some
+        assert bool((got["lse"][:, :before] == float("inf")).all()), window
+        r = O.attention(_np(qb), _np(kb), _np(vb), window, sinks, None, _np(db))
+        clean = O.attention(_np(q), _np(k), _np(v), window, sinks, None, _np(do))
+        lim = bounds(_np(q), _np(k), _np(v), clean, window, sinks, D ** -0.5, dtype, _np(do))
+        for name in ("o", "dq", "dk", "dv"):
+            have, want = _np(got[name]), r[name]
+            fine = np.isfinite(want)
+            assert not fine.all() and np.array_equal(np.isfinite(have), fine), (name, window)
+            with np.errstate(invalid="ignore"):
+                same = fine & (np.abs(want - clean[name]) <= 1e-12 * np.abs(clean[name]))
+            assert np.all(np.abs(have[same] - want[same]) <= lim[name][same]), (name, window)
+
+
 @pytest.mark.parametrize("nq", [1, 40])
 def test_rows_behind_a_caches_end_are_not_read(nq):
     """Room of a cache that is not used yet holds NaN."""
