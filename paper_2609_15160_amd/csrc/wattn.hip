@@ -75,11 +75,12 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // key of, or kLeast if that is less (its only key there may be one of little weight):
 // weights are exp2(s - base) at once, without a maximum per tile.  Where a
 // query's sum has grown past kSumMax the base moves up and the sums are scaled down,
-// exactly, by a power of two; o / l does not depend on it.  Weights that leave float32's
-// range within a tile (scores 127 above the base in base 2) make the row not finite, and
-// sums less than kSumMin are of weights near its end (scores of -112 and less, all of
-// them): such a row is done again by slow_row.  The sum of the rounded weights is a
-// product with ones.
+// exactly, by a power of two; o / l does not depend on it.  Within a tile weights, or only
+// their sums, may leave float32's range (scores some 120 above the base in base 2; sums of
+// weights times small values stay in it), and sums less than kSumMin are of weights near
+// its other end (scores of -112 and less, all of them): a row of which a sum or a result is
+// not finite, or whose sum is less, is done again by slow_row.  The sum of the rounded
+// weights is a product with ones.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 : kRoom<T, D>)) void k_wattn(WAttnArgs a) {
   using H = HeadRows<T, D>;
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(kTileWaves* kWave, (D == 64 && sizeof(T) == 2 ? 4 :
     const int row = r0 + qn * 16 + c16;
     const bool none = p[qn] < 0;  // sees no key: zeros, whatever its weights of zero were multiplied by
     const float sum = sum_quads(ls[qn]), inv = 1.f / (kRounds ? lr[qn][0] : sum);
-    bool good = none || sum >= kSumMin;
+    bool good = none || (sum >= kSumMin && finite1(sum) && finite1(lr[qn][0]));  // lr: zeros where nothing is rounded
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       o[dt][qn] = none ? f32x4{0.f, 0.f, 0.f, 0.f} : o[dt][qn] * inv;

@@ -233,6 +233,37 @@ def test_scores_far_from_zero(dtype, D, nq, scores):
             _within(got[name], r[name], lim[name], (name, window))
 
 
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("nq", [1, 200])
+@pytest.mark.parametrize("first", [0.0, -50.0])
+@pytest.mark.parametrize("up", [60.0, 80.0, 84.0, 86.0, 87.0, 88.0, 100.0])
+def test_scores_that_rise_between_tiles(dtype, D, nq, first, up):
+    """Scores far above those of a row's first keys, twice: weights relative to what the first keys give are up to the end of
+    float32's range, their sums beyond it, while sums of weights times small values, or values of both signs, are not."""
+    train = _train()
+    _say("rising scores", dtype, D, nq, first, up)
+    rng = np.random.default_rng(9)
+    n = 200
+    q = _normal(rng, nq, 1, D, std=0.1, dtype=dtype)
+    k = _normal(rng, n, 1, D, std=0.1, dtype=dtype)
+    do = _normal(rng, nq, 1, D, dtype=dtype)
+    at = torch.arange(n, device="cuda")
+    q[:, 0, 0] = 8.0
+    k[:, 0, 0] = ((first + up * ((at >= 40).float() + (at >= 120).float())) / 8).to(k.dtype)
+    small = 0.01 + _normal(rng, n, 1, D, std=0.001)
+    for v in (small, small * (1 - 2 * (at % 2))[:, None, None]):
+        v = v.to(k.dtype)
+        for window, sinks in ((None, 0), (51, 0), (30, 3)):
+            leaves = [t.detach().clone().requires_grad_() for t in (q, k, v)]
+            o = train.attention(*leaves, _offsets([nq]), _offsets([n]), window=window, sinks=sinks, scale=1.0)
+            got = dict(zip(("o", "dq", "dk", "dv"), (o, *torch.autograd.grad(o, leaves, do))))
+            arrays = [_np(t) for t in (q, k, v)]
+            r = O.attention(*arrays, window, sinks, 1.0, _np(do))
+            lim = bounds(*arrays, r, window, sinks, 1.0, dtype, _np(do))
+            for name in got:
+                _within(got[name], r[name], lim[name], (name, window))
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("nq,window,std", [(300, None, 1.0), (300, None, 2.0), (300, 40, 3.0), (4, None, 2.0), (1, None, 2.0)])
 def test_roundings_are_those_of_the_operands(D, nq, window, std):
