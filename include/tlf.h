@@ -531,7 +531,8 @@ int tlf_adamw(const tlf_adamw_tensor* h_tensors, int32_t count, double lr, doubl
  * p = n - nq + j.  The key at position x is visible to it when
  *   x <= p and (p - x < window or x < sinks)
  * and o = sum softmax(scale q . k) v over the visible keys.  A query that sees no
- * key, and a row behind the last sequence, gives zeros (and zero gradients).
+ * key, and a row ahead of the first sequence or behind the last, gives zeros (and
+ * zero gradients).
  * What a query does not see takes no part, whatever values it has. */
 #define TLF_ATTN_MAX_SINKS 64
 #define TLF_ATTN_MAX_HEADS 1024
@@ -555,7 +556,8 @@ typedef struct tlf_attn_shape {
   /* Elements between rows, multiples of 16 bytes; a row's heads lie one behind the
    * other.  do lies as o. */
   int64_t q_stride, k_stride, v_stride, o_stride;
-  /* Device arrays.  Offsets ascend from 0; they are clamped to the rows there are. */
+  /* Device arrays.  Offsets ascend (where they do not, rows may be left unwritten); they
+   * are clamped to the rows there are. */
   const int32_t* d_q_offsets; /* [batch + 1] */
   const int32_t* d_k_offsets; /* [batch + 1]; d_q_offsets itself where the rows are the same */
   const int32_t* d_k_lengths; /* [batch] keys that sequence b holds of the rows up to k_offsets[b + 1], or NULL: all */

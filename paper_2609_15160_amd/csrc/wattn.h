@@ -52,17 +52,18 @@ constexpr int kTileWaves = 4;
 
 __device__ __forceinline__ int clampi(int v, int lo, int hi) { return min(max(v, lo), hi); }
 
-// Tiles of STEP rows: sequence b's begin at slot off[b] / STEP + b, which leaves
-// each at least as many slots as it has tiles and needs no plan on the device.
-// The rows behind the last sequence are one more, without keys.
+// Tiles of STEP rows: sequence b's begin at slot off[b] / STEP + b + 1, which leaves
+// each at least as many slots as it has tiles and needs no plan on the device.  The rows
+// ahead of the first sequence are one more, number -1, and those behind the last are
+// number `batch`: sequences without keys.
 template <int STEP> __device__ __forceinline__ int slot_of(const int32_t* off, int rows, int b) {
-  return clampi(off[b], 0, rows) / STEP + b;
+  return b < 0 ? 0 : clampi(off[b], 0, rows) / STEP + b + 1;
 }
-template <int STEP> inline int64_t slots_of(int64_t rows, int64_t batch) { return rows / STEP + batch + 1; }
+template <int STEP> inline int64_t slots_of(int64_t rows, int64_t batch) { return rows / STEP + batch + 2; }
 
-// The last b in [0, batch] whose slots begin at or before `slot`, 64 at a time.
+// The last b in [-1, batch] whose slots begin at or before `slot`, 64 at a time.
 template <int STEP> __device__ __forceinline__ int seq_of(const int32_t* off, int rows, int batch, int slot) {
-  int lo = 0, hi = batch;
+  int lo = -1, hi = batch;
   while (hi > lo) {
     const int step = (hi - lo + kWave - 1) / kWave, b = lo + (lane_id() + 1) * step;
     const bool before = b <= hi && slot_of<STEP>(off, rows, min(b, hi)) <= slot;
@@ -74,12 +75,12 @@ template <int STEP> __device__ __forceinline__ int seq_of(const int32_t* off, in
 
 __device__ __forceinline__ WSeq load_seq(const WAttnArgs& a, int b) {
   WSeq s;
-  s.q0 = clampi(a.q_off[b], 0, a.rows_q);
-  s.k0 = clampi(a.k_off[b], 0, a.rows_k);
+  s.q0 = b < 0 ? 0 : clampi(a.q_off[b], 0, a.rows_q);
+  s.k0 = b < 0 ? 0 : clampi(a.k_off[b], 0, a.rows_k);
   if (b < a.batch) {
     s.nq = clampi(a.q_off[b + 1], s.q0, a.rows_q) - s.q0;
     s.cap = clampi(a.k_off[b + 1], s.k0, a.rows_k) - s.k0;
-    s.n = a.k_len ? clampi(a.k_len[b], 0, s.cap) : s.cap;
+    s.n = b < 0 ? 0 : a.k_len ? clampi(a.k_len[b], 0, s.cap) : s.cap;
   } else {
     s.nq = a.rows_q - s.q0;
     s.cap = a.rows_k - s.k0;

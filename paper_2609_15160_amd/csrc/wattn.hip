@@ -592,7 +592,7 @@ namespace {
 // row 26 and 25, 2 rows 38 and 25; 8 x 3000, 2 rows 23 and 64, 8 rows 52 and 64).
 bool is_few(const tlf_attn_shape& t) {
   if (t.rows_q <= t.batch) return true;
-  return t.rows_q <= 8 * (int64_t)t.batch && slots_of<128>(t.rows_q, t.batch) * t.heads < 256;
+  return t.rows_q <= 8 * (int64_t)t.batch && (t.rows_q / 128 + (int64_t)t.batch + 1) * t.heads < 256;
 }
 
 // Ranges of the keys of a row, for two workgroups on a compute unit, and 256 keys of a

@@ -587,10 +587,11 @@ def self_attention(qkv: torch.Tensor, offsets: torch.Tensor, heads: int, kv_head
     """Causal attention within each sequence of rows q | k | v (qkv [rows, (heads + 2 kv_heads) * width], as the block's
     QKV projection gives them), with the gradient to qkv, one tensor.  Returns [rows, heads * width].
 
-    offsets: int32, where each sequence's rows begin, and the total (LoopPlan.offsets).  With a `window` a row sees the
+    offsets: int32, ascending, where each sequence's rows begin, and their end (LoopPlan.offsets).  With a `window` a row sees the
     last `window` rows of its sequence, itself included, and the first `sinks` ones; without it every earlier row.  heads
     is a multiple of kv_heads (heads by default): consecutive heads share a key head.  Width 64 or 128 (16 too in
-    float32), sinks 64 at most, scale 1 / sqrt(width) by default.  Rows behind the last sequence give zeros.  What a row
+    float32), sinks 64 at most, scale 1 / sqrt(width) by default.  Rows of no sequence, ahead of the first or behind the
+    last, give zeros.  What a row
     does not see takes no part, whatever its values.  Scores, softmax and sums are float32; of bfloat16 tensors the
     weights, and in the backward pass the gradients of the scores, are rounded to bfloat16 as operands."""
     kv_heads = heads if kv_heads is None else kv_heads
@@ -605,8 +606,8 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.
     """Causal attention of each sequence's rows of q ([rows, heads, width]) to its rows of k and v ([k_rows, kv_heads,
     width]), with gradients to all three.  As self_attention; a sequence's last query stands at its last key.
 
-    offsets, k_offsets: int32, where each sequence's rows of q, and of k and v, begin, and their ends (k_offsets: as
-    offsets).  k_lengths: int32, how many rows each sequence holds of those up to the next one's begin (all by default):
+    offsets, k_offsets: int32, ascending, where each sequence's rows of q, and of k and v, begin, and their ends
+    (k_offsets: as offsets).  k_lengths: int32, how many rows each sequence holds of those up to the next one's begin (all by default):
     the new tokens' rows against a cache that has room for more.  A row that sees nothing gives zeros.  Rows of heads
     may lie in wider ones (a stride that is a multiple of 16 bytes); else they are copied."""
     if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:

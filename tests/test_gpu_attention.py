@@ -403,6 +403,46 @@ def test_queries_before_the_first_key_give_zeros_whatever_the_values(dtype, D, n
             assert np.all(np.abs(have[same] - want[same]) <= lim[name][same]), (name, window)
 
 
+@pytest.mark.parametrize("dtype,D", TYPES)
+@pytest.mark.parametrize("ahead,k_ahead", [(1, 0), (0, 1), (5, 63), (128, 64), (300, 200), (127, 129)])
+@pytest.mark.parametrize("nq", [[25, 0, 17], [1, 0, 1], [140, 3, 0]])
+def test_rows_ahead_of_the_first_sequence(dtype, D, ahead, k_ahead, nq):
+    """Offsets that begin behind row 0: the rows ahead, as those behind, are written as zeros, and the sequences are what they
+    are without them."""
+    _say("rows ahead", dtype, D, ahead, k_ahead, nq)
+    rng = np.random.default_rng(28)
+    n, heads, kv, tail = [30, 70, 17], 4, 2, 3
+    q, do = (_normal(rng, ahead + sum(nq) + tail, heads, D, dtype=dtype) for _ in range(2))
+    k, v = (_normal(rng, k_ahead + sum(n) + tail, kv, D, dtype=dtype) for _ in range(2))
+    for window, sinks in ((None, 0), (20, 3)):
+        got = _entry(q, k, v, do, _offsets(nq) + ahead, _offsets(n) + k_ahead, window, sinks)
+        a, b = ahead + np.cumsum([0] + nq), k_ahead + np.cumsum([0] + n)
+        for name, at in (("o", a), ("low", a), ("dq", a), ("dk", b), ("dv", b)):
+            assert got[name] is None or not (got[name][:at[0]].any() or got[name][at[-1]:].any()), (name, window)
+        assert bool((got["lse"][:, :ahead] == float("inf")).all() and (got["lse"][:, a[-1]:] == float("inf")).all())
+        for i in range(3):
+            mq, mk = slice(a[i], a[i + 1]), slice(b[i], b[i + 1])
+            arrays = [_np(t) for t in (q[mq], k[mk], v[mk])]
+            r = O.attention(*arrays, window, sinks, None, _np(do[mq]))
+            lim = bounds(*arrays, r, window, sinks, D ** -0.5, dtype, _np(do[mq]))
+            for name, m in (("o", mq), ("dq", mq), ("dk", mk), ("dv", mk)):
+                _within(got[name][m], r[name], lim[name], (name, i, window))
+
+
+def test_self_attention_of_a_sequence_behind_other_rows():
+    train = _train()
+    rng = np.random.default_rng(29)
+    qkv = _normal(rng, 500, 6 * 64, dtype="bf16")
+    a, b = qkv.clone().requires_grad_(), qkv[200:450].clone().requires_grad_()
+    oa, ob = (train.self_attention(t, torch.tensor(off, dtype=torch.int32, device="cuda"), 4, 1, window=40)
+              for t, off in ((a, (200, 300, 450)), (b, (0, 100, 250))))
+    do = _normal(rng, 500, 256, dtype="bf16")
+    ga, = torch.autograd.grad(oa, a, do)
+    gb, = torch.autograd.grad(ob, b, do[200:450])
+    for whole, part in ((oa, ob), (ga, gb)):
+        assert torch.equal(whole[200:450], part) and not whole[:200].any() and not whole[450:].any()
+
+
 @pytest.mark.parametrize("nq", [1, 40])
 def test_rows_behind_a_caches_end_are_not_read(nq):
     """Room of a cache that is not used yet holds NaN."""
