@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kRowWaves* kWave) void k_resid_dx(ResidArgs a) {
       hy += dot4(h[k], ya);
     }
   }
-  const float s = r * r * r * (wave_sum(uh) / (float)a.d);
+  const float s = r * (r * r * (wave_sum(uh) / (float)a.d));  // r's cube alone may leave float32's range
   float q = 0.f;
   if (POST) q = ry * ry * ((wave_sum(ey) - s * wave_sum(hy)) / (float)a.d);
 #pragma unroll
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(MAXT) void k_resid_grad(ResidArgs a, int chunk, int
 #pragma unroll
     for (int u = 0; u < RU; ++u) {
       if (row + u >= r1) break;
-      const float r = cur[u].r, ry = cur[u].ry, s = r * r * r * (m[u][0] / (float)a.d);
+      const float r = cur[u].r, ry = cur[u].ry, s = r * (r * r * (m[u][0] / (float)a.d));
       const f32x4 y = cur[u].y.get();
       e[u] -= cur[u].h * s;
       if (own && first == 0) {

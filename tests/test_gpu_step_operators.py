@@ -138,6 +138,23 @@ def test_residual_norm_zero_rows_and_empty_groups():
         _check_resid(6, 128, 4, "f32", post, x=x.clone(), y=y.clone(), group=group)
 
 
+@pytest.mark.parametrize("yt", ["f32", "bf16"])
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("groups", [0, 1, 5, 12])
+def test_residual_norm_gradients_of_small_eps_and_rows_far_from_one(monkeypatch, yt, post, groups):
+    """The cube of 1 / sqrt(mean + eps) leaves float32's range while the gradients do not: rows of zeros with a small eps,
+    rows of large values."""
+    rng = np.random.default_rng(14)
+    x, y = _normal(rng, 9, 260), _normal(rng, 9, 260, dtype=yt)
+    x[:2], y[0], y[2] = 0.0, 0.0, 0.0
+    with monkeypatch.context() as m:
+        m.setitem(globals(), "EPS", 1e-28)
+        _check_resid(9, 260, groups, yt, post, x=x.clone(), y=y.clone())
+        _check_resid(9, 260, groups, yt, post, x=torch.zeros_like(x), y=torch.zeros_like(y), use="z")
+    for std in (1e13, 1e16):
+        _check_resid(9, 260, groups, yt, post, x=_normal(rng, 9, 260, std=std), y=_normal(rng, 9, 260, std=std, dtype=yt), use="z")
+
+
 def test_residual_norm_without_rows():
     train = _train()
     x, y = torch.zeros(0, 128, device="cuda", requires_grad=True), torch.zeros(0, 128, device="cuda", requires_grad=True)
