@@ -619,8 +619,9 @@ int tlf_residual_norm_grad(const float* d_dh, const void* d_dz, const float* d_h
 /* The norm of all elements of many gradients, and the scale that clips them to
  * max_norm, few launches for all:
  *   *d_norm = sqrt(sum g^2),  *d_scale = 1 where that is at most max_norm, else max_norm / norm
- * Summed in float64.  A norm that is not finite gives a scale of 0 or NaN.  d_scale
- * may be NULL; max_norm > 0 may be infinite.  Gradients need the alignment of their
+ * Summed in float64.  Gradients that are not finite give a scale of 0 or NaN, whatever
+ * max_norm is; where only *d_norm is past float32's range the scale is right.
+ * d_scale may be NULL; max_norm > 0 may be infinite.  Gradients need the alignment of their
  * elements only and may overlap.
  *   h_grads: host array, read during the call.
  *   d_workspace: tlf_grad_norm_ws_bytes bytes, 8-byte aligned, used during the call only. */

@@ -145,7 +145,8 @@ __global__ __launch_bounds__(kTotalThreads) void k_grad_total(const double* part
   for (int w = 1; w < kTotalThreads / kWave; ++w) s += sums[w];
   s = sqrt(s);
   *norm = (float)s;
-  if (scale) *scale = s <= max_norm ? 1.f : (float)(max_norm / s);  // NaN stays one
+  // 0 or NaN of a sum that is not finite; NaN where the limit is infinite too
+  if (scale) *scale = s <= max_norm && s < INFINITY ? 1.f : (float)(max_norm / s);
 }
 
 template <typename T> __device__ __forceinline__ void scale_all(T* g, int64_t n, int64_t base, bool vec, float f) {

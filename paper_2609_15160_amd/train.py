@@ -665,8 +665,8 @@ def grad_norm(grads, max_norm: float = None):
     """(norm, scale) of a list of gradients (contiguous float32 or bfloat16 CUDA tensors), both float32 on the device: the
     norm of all their elements, summed in float64, and 1, or max_norm / norm where the norm is above max_norm (> 0).
 
-    The host does not wait.  adamw_ takes the scale as it is: clipping then costs no pass over the gradients.  A norm that
-    is not finite gives a scale of 0 or NaN."""
+    The host does not wait.  adamw_ takes the scale as it is: clipping then costs no pass over the gradients.  Gradients
+    that are not finite give a scale of 0 or NaN, without a max_norm too."""
     grads = list(grads)
     if not grads:
         raise ValueError("grad_norm: no gradients")

@@ -273,6 +273,20 @@ def test_norms_at_the_ends_of_the_range():
         assert not np.isfinite(float(norm)) and (float(scale) == 0.0 if bad == float("inf") else np.isnan(float(scale)))
 
 
+@pytest.mark.parametrize("limit", [None, float("inf"), 3.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scale_of_a_norm_that_is_not_finite(limit, dtype):
+    """0 or NaN, whatever the limit: what takes the scale cannot take such gradients for good ones."""
+    train = _train()
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        g = torch.ones(20000, device="cuda", dtype=_dt(dtype))
+        g[17] = bad
+        norm, scale = train.grad_norm([torch.ones(3, device="cuda"), g], limit)
+        assert not np.isfinite(float(norm)) and (np.isnan(float(scale)) or float(scale) == 0.0), (bad, float(scale))
+    norm, scale = train.grad_norm([torch.ones(9, device="cuda", dtype=_dt(dtype))], limit)
+    assert float(norm) == 3.0 and float(scale) == 1.0
+
+
 def test_norm_of_views_that_overlap_and_clip_refuses_them():
     train = _train()
     from paper_2609_15160_amd import tlf
