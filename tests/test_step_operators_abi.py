@@ -140,6 +140,17 @@ def test_attention_argument_errors(call):
         call()
 
 
+@pytest.mark.parametrize("sinks", [65, 1 << 31, (1 << 32) + 1, 1 << 40])
+@pytest.mark.parametrize("window", [None, 5, (1 << 32) + 5])
+def test_sinks_past_their_limit_are_refused_at_any_size(sinks, window):
+    """A number that 32 bits do not hold is not taken for what is left of it."""
+    for call in (lambda: train.attention(*[_t(3, 2, 64)] * 3, _off(0, 3), window=window, sinks=sinks),
+                 lambda: train.self_attention(_t(3, 384), _off(0, 3), 2, window=window, sinks=sinks)):
+        with pytest.raises(tlf.TlfError) as e:
+            call()
+        assert e.value.status == UNS
+
+
 def _resid(lib, **kw):
     a = dict(x=P, y=P, yt=BF16, alpha=P, gamma=P, group=P, groups=2, rows=3, d=8, post=0, eps=1e-5, h=P, z=P, rstd=P, ystd=P)
     a.update(kw)
