@@ -575,10 +575,11 @@ def _attend(name, q, k, v, offsets, k_offsets, k_lengths, heads, kv_heads, width
         raise ValueError(f"{name}: one offset more than sequences, one length each")
     if window is not None and window < 1 or sinks < 0:
         raise ValueError(f"{name}: window {window}, sinks {sinks}")
-    _int32(name, q, k, v)
+    _int32(name, q, k, v, offsets)
     _same_device(q, k, v, offsets, k_offsets, k_lengths)
+    window, sinks = (min(n, (1 << 31) - 1) for n in (window or 0, sinks))  # 32 bits each, as they are passed
     at = (offsets.contiguous(), k_offsets.contiguous(), None if k_lengths is None else k_lengths.contiguous())
-    return _Attention.apply(q, k, v, *at, heads, kv_heads, width, min(window or 0, (1 << 31) - 1), sinks,
+    return _Attention.apply(q, k, v, *at, heads, kv_heads, width, window, sinks,
                             width ** -0.5 if scale is None else float(scale), _wants_grad(q, k, v))
 
 

@@ -151,6 +151,12 @@ def test_sinks_past_their_limit_are_refused_at_any_size(sinks, window):
         assert e.value.status == UNS
 
 
+def test_offsets_past_32_bits_are_refused():
+    off = torch.zeros(1, dtype=torch.int32).expand((1 << 32) + 1).as_subclass(_Cuda)
+    with pytest.raises(ValueError, match="2.31"):
+        train.attention(*[_t(3, 2, 64)] * 3, off)
+
+
 def _resid(lib, **kw):
     a = dict(x=P, y=P, yt=BF16, alpha=P, gamma=P, group=P, groups=2, rows=3, d=8, post=0, eps=1e-5, h=P, z=P, rstd=P, ystd=P)
     a.update(kw)
