@@ -500,6 +500,48 @@ def test_self_attention_of_rows_inside_wider_ones():
     assert torch.equal(torch.autograd.grad(oa.sum(), a)[0], torch.autograd.grad(ob.sum(), b)[0])
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("nq", [[700, 400], [1, 1]])
+def test_rows_past_32_bits_of_elements(dtype, D, nq):
+    """Rows at the largest stride, the last of them more than 2^31 elements behind the first, inputs and gradients: the same
+    to the bit as rows that lie one behind the other."""
+    import ctypes
+
+    from paper_2609_15160_amd import tlf
+    train, lib = _train(), tlf.load()
+    _say("rows past 2^31 elements", dtype, D, nq)
+    rng = np.random.default_rng(30)
+    n, heads, kv, wide = [700, 400], 4, 2, tlf.ATTN_MAX_STRIDE
+    assert (sum(n) - 1) * wide > 1 << 31
+    q, do = (_normal(rng, sum(nq), heads, D, dtype=dtype) for _ in range(2))
+    k, v = (_normal(rng, sum(n), kv, D, dtype=dtype) for _ in range(2))
+    leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+    args = dict(window=90, sinks=3)
+    want = train.attention(*leaves, _offsets(nq), _offsets(n), **args)
+    grads = torch.autograd.grad(want, leaves, do)
+    space = torch.empty(sum(n), wide, dtype=q.dtype, device="cuda")
+    cut = lambda t, at: space[:len(t), at:at + t[0].numel()].view(t.shape)  # noqa: E731
+    far = [cut(t, 1024 * i) for i, t in enumerate((q, k, v))]
+    for t, f in zip((q, k, v), far):
+        f.copy_(t)
+    assert all(train._rows_of_heads(f, f.shape[1], D) is f for f in far)  # read as they lie
+    got = train.attention(*[f.detach().requires_grad_() for f in far], _offsets(nq), _offsets(n), **args)
+    assert torch.equal(got, want)
+    out = [cut(t, 4096 + 1024 * i) for i, t in enumerate((q, k, v, q, q))]  # dq, dk, dv, o, low
+    lse = torch.empty(heads, sum(nq), device="cuda")
+    d_o = cut(do, 16384)
+    d_o.copy_(do)
+    off, k_off = _offsets(nq), _offsets(n)
+    shape = tlf.AttnShape(train._DTYPE[q.dtype], 2, heads, kv, D, sum(nq), sum(n), 90, 3, D ** -0.5, wide, wide, wide, wide,
+                          off.data_ptr(), k_off.data_ptr(), None)
+    low = out[4] if dtype == "bf16" else None
+    ws, need = train._workspace(lib.tlf_attn_ws_bytes, ctypes.byref(shape), device=q.device)
+    train._run(lib.tlf_attn, q.device, shape, *far, out[3], lse, low, ws, need)
+    ws, need = train._workspace(lib.tlf_attn_grad_ws_bytes, ctypes.byref(shape), device=q.device)
+    train._run(lib.tlf_attn_grad, q.device, shape, d_o, *far, out[3], lse, low, out[0], wide, out[1], wide, out[2], wide, ws, need)
+    assert all(torch.equal(a, b) for a, b in zip((out[3], *out[:3]), (want, *grads)))
+
+
 def test_gradients_by_differences():
     train = _train()
     rng = np.random.default_rng(25)

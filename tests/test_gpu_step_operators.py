@@ -155,6 +155,43 @@ def test_residual_norm_gradients_of_small_eps_and_rows_far_from_one(monkeypatch,
         _check_resid(9, 260, groups, yt, post, x=_normal(rng, 9, 260, std=std), y=_normal(rng, 9, 260, std=std, dtype=yt), use="z")
 
 
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("groups", [0, 3])
+def test_residual_norm_past_32_bits_of_elements(post, groups):
+    """The last rows of tensors of more than 2^31 elements, zeros before them: h, z and the rows' gradients to the bit those
+    of the last rows alone; the scales' to the order of their sums, of which the zeros have no part."""
+    train = _train()
+    rows, few, d = 1060000, 100, 2048
+    assert (rows - few) * d > 1 << 31
+    _say("residual past 2^31 elements", rows, d, groups, post)
+    rng = np.random.default_rng(15)
+    part = [_normal(rng, few, d), _normal(rng, few, d, dtype="bf16"), _normal(rng, few, d), _normal(rng, few, d, dtype="bf16")]
+    scales = [_normal(rng, groups, d, std=0.3) if groups else None for _ in range(2)]
+    group = torch.from_numpy(rng.integers(0, groups, few).astype(np.int32)).cuda() if groups else None
+
+    def behind(t):
+        out = torch.zeros((rows, *t.shape[1:]), dtype=t.dtype, device="cuda")
+        out[-few:] = t
+        return out
+
+    def run(x, y, dh, dz, group):
+        leaves = [t.detach().clone().requires_grad_() if t is not None and t.shape[0] == groups else t for t in scales]
+        x.requires_grad_(), y.requires_grad_()
+        h, z = train.residual_norm(x, y, *leaves, group, post_norm=post)
+        return h.detach(), z.detach(), *torch.autograd.grad((h, z), [x, y] + [t for t in leaves if t is not None], (dh, dz))
+
+    want = run(*part, group)
+    got = run(*[behind(t.detach()) for t in part], None if group is None else behind(group))
+    for a, b in zip(got[:4], want[:4]):
+        assert torch.equal(a[-few:], b)
+    if groups:
+        x, y, dh, dz = map(_np, part)
+        w = O.residual_norm(x, y, *map(_np, scales), group.cpu().numpy(), EPS, post, dh, dz)
+        for a, b, each in ((got[4], want[4], w["dx"] * w["t"]), (got[5], want[5], dz * w["h"] * w["r"])):
+            mag = O.by_group(np.abs(each), group.cpu().numpy(), groups)
+            assert np.all(np.abs(_np(a) - _np(b)) <= 2 * (few + 2) * E32 * 1.01 * mag)
+
+
 def test_residual_norm_without_rows():
     train = _train()
     x, y = torch.zeros(0, 128, device="cuda", requires_grad=True), torch.zeros(0, 128, device="cuda", requires_grad=True)
@@ -295,6 +332,18 @@ def test_norm_of_views_that_overlap_and_clip_refuses_them():
     with pytest.raises(tlf.TlfError):
         train.clip_grad_norm_([t, t[50:]], 1.0)
     assert torch.equal(t, torch.ones_like(t))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_past_32_bits_of_elements(dtype):
+    """Ones around element 2^31 and at the end of a longer tensor: counted by the norm, scaled by the clipping."""
+    train = _train()
+    _say("gradient past 2^31 elements", dtype)
+    g = torch.zeros((1 << 31) + 20005, dtype=_dt(dtype), device="cuda")
+    g[(1 << 31) - 8:(1 << 31) + 9], g[-8:] = 1.0, 1.0
+    assert float(train.clip_grad_norm_([g], 2.5)) == 5.0
+    assert bool((g[(1 << 31) - 8:(1 << 31) + 9] == 0.5).all() and (g[-8:] == 0.5).all())
+    assert float(train.grad_norm([g])[0]) == 2.5
 
 
 @pytest.mark.parametrize("bits", [32, 8])
