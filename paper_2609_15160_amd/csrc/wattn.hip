@@ -65,11 +65,14 @@ __device__ __forceinline__ void slow_row(const WAttnArgs& a, const WSeq& s, int 
 // is used while the next arrives; one barrier a tile).  Tiles of 32 or of 128 keys,
 // three places, eight waves and raised priorities around the products were all slower.
 //
-// Bound by the issue of vector instructions beside the products: 32 keys x 32 queries
-// take 18 products (288 clocks of a SIMD's matrix cores at width 64) and 75 others, 16 of
-// them exponentials, which take four times as long (490).  8 x 4096 rows x 16 heads x 64,
-// window 1024, 4 sinks: 188-193 us, 640 TFLOP/s of the visible pairs; 4 x 4099 x 16 x 128:
-// 278-284 us, 730 TFLOP/s (matrix cores busy 33 and 34% of the time).
+// 32 keys x 32 queries take 18 products at width 64 (288 clocks of a SIMD's matrix cores;
+// 34 and 544 at 128) and 107 other vector instructions of 4 clocks, the 16 exponentials
+// among them of 8.  At width 64 their issue bounds it: it takes 75% of the clocks that a
+// compute unit has waves in, the matrix cores are busy 38%.  At 128 neither is full (48 and
+// 41%): there are two waves on a SIMD, which spend 29% of their time in waits for memory,
+// LDS and barriers and 30% waiting to issue.  8 x 4096 rows x 16 heads x 64, window 1024, 4
+// sinks: 188-197 us, 640 TFLOP/s of the visible pairs; 4 x 4099 x 16 x 128: 278-284 us, 730
+// TFLOP/s.
 //
 // The softmax base of a query is the largest score of the first tile that it sees a
 // key of, or kLeast if that is less (its only key there may be one of little weight):

@@ -85,8 +85,11 @@ __device__ __forceinline__ void slow_dkv(const GradArgs& a, const WSeq& s, int k
 // Tiles, waves and LDS as the forward kernel's (k_wattn).  q and do of the wave's 32
 // queries stay in registers; a tile's keys are read as they lie and transposed, its
 // values as they lie.  delta is of o with what its rounding took.  dP starts from -delta, so dS = P dP takes one product.
-// Bound as the forward kernel is: 8 x 4096 x 16 x 64, window 1024: 230 us, 790 TFLOP/s of
-// three products; 4 x 4099 x 16 x 128: 345-350 us, 880 TFLOP/s (matrix cores busy 37 and 39%).
+// Neither the issue of vector instructions (100 beside the 24 products of 32 keys x 32
+// queries at width 64, the 48 at 128) nor the matrix cores are full: 62 and 42% of the clocks
+// that a compute unit has waves in at 64, 42 and 49% at 128; waves spend a third of their
+// time in waits and a third waiting to issue.  8 x 4096 x 16 x 64, window 1024: 230-236 us,
+// 790 TFLOP/s of three products; 4 x 4099 x 16 x 128: 345-350 us, 880 TFLOP/s.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (kRoom<T, D>)) void k_wattn_dq(GradArgs a) {
   using H = HeadRows<T, D>;
@@ -309,10 +312,12 @@ template <typename T, int D> constexpr int key_tiles() { return sizeof(T) == 4 &
 // A tile's keys are seen by the queries from its first position to the window's end
 // behind its last; sinks by all from there: where a first tile has sinks, its queries
 // go in `sink_parts` ranges to workgroups of their own, whose sums k_wattn_sinks adds.
-// Bound by the issue of instructions and by the reads of LDS, where q and do are read
-// twice, as they lie and transposed: 8 x 4096 x 16 x 64, window 1024: 304-310 us, 780
-// TFLOP/s of four products; 4 x 4099 x 16 x 128: 473-478 us, 860 (matrix cores busy 37 and
-// 39%).  Width 64 with two waves on a SIMD and operands read ahead, and tiles of 128
+// Bound by latency: vector instructions (111 beside the 32 products of 32 keys x 32 queries
+// at width 64, 121 beside 64 at 128) take 53 and 38% of the clocks that a compute unit has
+// waves in, the matrix cores 43 and 48%; q and do are read twice from LDS, as they lie and
+// transposed right before their products, and waves spend 39 and 33% of their time in waits.
+// 8 x 4096 x 16 x 64, window 1024: 302-310 us, 780 TFLOP/s of four products; 4 x 4099 x 16 x
+// 128: 457-478 us, 860.  Width 64 with two waves on a SIMD and operands read ahead, and tiles of 128
 // queries, were slower.
 template <typename T, int D>
 __global__ __launch_bounds__(kTileWaves* kWave, (sizeof(T) == 4 ? kRoom<T, D> : D == 64 ? 3 : 2)) void k_wattn_dkv(GradArgs a) {
