@@ -10,8 +10,9 @@
 //
 // Bound by HBM: 176M bf16 elements 55 us (6.3 TB/s; what the memory-side cache still holds
 // of them helps), 4.6 us for the sums; a pass that does not clip ends with a launch that
-// reads one value (2.5-4.5 us), one that clips with 109 us more (6.5 TB/s).  4096 workgroups take the pieces of 8192 in turn: a
-// workgroup for each took 69 us in all against 64, with sums for 21000 workgroups.
+// reads one value (2.5-4.5 us), one that clips with one of 109 us (6.5 TB/s).  4096
+// workgroups take the pieces of 8192 in turn: a workgroup for each took 69 us in all
+// against 64, with sums for 21000 workgroups.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -588,13 +588,16 @@ def self_attention(qkv: torch.Tensor, offsets: torch.Tensor, heads: int, kv_head
     """Causal attention within each sequence of rows q | k | v (qkv [rows, (heads + 2 kv_heads) * width], as the block's
     QKV projection gives them), with the gradient to qkv, one tensor.  Returns [rows, heads * width].
 
-    offsets: int32, ascending, where each sequence's rows begin, and their end (LoopPlan.offsets).  With a `window` a row sees the
-    last `window` rows of its sequence, itself included, and the first `sinks` ones; without it every earlier row.  heads
-    is a multiple of kv_heads (heads by default): consecutive heads share a key head.  Width 64 or 128 (16 too in
-    float32), sinks 64 at most, scale 1 / sqrt(width) by default.  Rows of no sequence, ahead of the first or behind the
-    last, give zeros.  What a row
-    does not see takes no part, whatever its values.  Scores, softmax and sums are float32; of bfloat16 tensors the
-    weights, and in the backward pass the gradients of the scores, are rounded to bfloat16 as operands."""
+    offsets: int32, ascending, where each sequence's rows begin, and their end (LoopPlan.offsets).  With a `window` a row
+    sees the last `window` rows of its sequence, itself included, and the first `sinks` ones; without it every earlier
+    row.  heads is a multiple of kv_heads (heads by default): consecutive heads share a key head.  Width 64 or 128 (16 too
+    in float32), sinks 64 at most, scale 1 / sqrt(width) by default.  Rows of no sequence, ahead of the first or behind
+    the last, give zeros.  What a row does not see takes no part, whatever its values.  Scores, softmax and sums are
+    float32; of bfloat16 tensors the weights, and in the backward pass the gradients of the scores, are rounded to
+    bfloat16 as operands.
+
+    Rows whose result is not finite, whose scores rise by more than some 80 above those of the first keys that they see, or
+    whose scores are all below -78, are computed again one by one, which takes long where there are many of them."""
     kv_heads = heads if kv_heads is None else kv_heads
     if qkv.dim() != 2 or heads < 1 or kv_heads < 1 or qkv.shape[1] % (heads + 2 * kv_heads):
         raise ValueError(f"self_attention: qkv {tuple(qkv.shape)}, expected [rows, ({heads} + 2 x {kv_heads}) * width]")
